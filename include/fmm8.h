@@ -421,6 +421,115 @@ int fmm_e4m3_quantize(const float *dIn, uint8_t *dOut, int64_t n, void *stream);
  * dOut 4-byte aligned.  Asynchronous on stream. */
 int fmm_e4m3_quantize_pow2(const float *dIn, uint8_t *dOut, int64_t n, int32_t e, void *stream);
 
+/* ---- an 8-bit linear layer ------------------------------------------------
+ *
+ * The products above quantize both of their operands inside the call.  A
+ * layer's weights, and activations that a norm has just written, are
+ * quantized once and then multiplied, or kept, as they are; the calls below
+ * make such operands, multiply them, and give the gradients of what they
+ * stand for.
+ *
+ * Codes.  A matrix of `rows` x `cols` values is held as int8 codes q
+ * [rows][fmm_q8_pitch(cols)] and fp32 scales s [rows]; the values are q s.  The
+ * pitch is cols rounded up to 128, and codes past cols are zero: the calls that
+ * write codes write those zeros, the ones that read codes rely on them.
+ * Quantizing a row: a = max(amax |x|, 1e-12), q = the integer nearest
+ * fl32(x fl32(127 / a)), ties to even, in [-127, 127]; s = fl32(a / 127).  A row
+ * that holds a NaN or an infinity gets scale NaN and zero codes, so that what
+ * is computed from it is NaN.  Codes written by the caller may also be -128.
+ *
+ * Checkpoint.  The same rule over each group of 128 columns of a row: codes as
+ * above, scales [rows][pitch / 128].
+ *
+ * Types.  `type` names the activations' element type (FMM_F32, FMM_BF16,
+ * FMM_F16).  Every sum, statistic and scale is fp32 (products of codes: int32,
+ * exact), and a result is rounded once, to nearest even, when it is stored.
+ *
+ * Matrices are row-major and contiguous.  Codes must be 16-byte aligned, scales,
+ * bias and other fp32 arrays 4-byte, activations aligned to their element
+ * unless a call says more (FMM_ERR_ARG otherwise).  Unlike the calls above these
+ * define the result for NaN and infinities: they propagate as in the formulas.
+ * Asynchronous on `stream`; nothing is allocated or synchronized, so calls may
+ * be captured into a graph. */
+enum {
+  FMM_F32 = 0,
+  FMM_BF16 = 1,
+  FMM_F16 = 2
+};
+
+/* Bytes (= codes) of one row of codes: cols rounded up to 128 (-1 if cols < 0). */
+int64_t fmm_q8_pitch(int64_t cols);
+
+/* dCodes, dScales = the codes of dX (rows x cols).  rows, cols >= 0. */
+int fmm_q8_quantize(int type, int64_t rows, int64_t cols, const void *dX, int8_t *dCodes, float *dScales, void *stream);
+
+/* dOut (rows x cols, `type`) = the values that codes stand for: group 0, one
+ * scale per row; group 128, one per row and group (a checkpoint).  FMM_ERR_ARG
+ * for another group. */
+int fmm_q8_dequantize(int type, int64_t rows, int64_t cols, int group, const int8_t *dCodes, const float *dScales,
+                      void *dOut, void *stream);
+
+typedef struct {
+  int64_t rows, cols;   /* rows >= 0, cols >= 1 */
+  int32_t type;         /* FMM_F32, FMM_BF16 or FMM_F16: x, residual, h, gain and their gradients */
+  float eps;            /* >= 0, finite */
+} fmm_norm_desc;
+
+/* The RMS norm with the residual's addition and an 8-bit output:
+ *   h = x + residual (in fp32), rstd = (mean_j h_j^2 + eps)^-1/2, y = h rstd gain.
+ * dH (may be NULL) receives h rounded to the type, dCodes / dScales the codes of
+ * y, dRstd [rows] rstd, and dSaved / dSavedScales (both NULL or neither) the
+ * checkpoint of h.  The codes are those of the row h gain (the factor rstd is
+ * common to the row, and multiplies the scale only).  dResidual and dGain may be
+ * NULL (0 and 1).  dH may be dX or dResidual (FMM_ERR_UNSUPPORTED for rows of
+ * more than 32768 columns, which are read twice). */
+int fmm_rmsnorm_q8(const fmm_norm_desc *desc, const void *dX, const void *dResidual, const void *dGain, void *dH,
+                   int8_t *dCodes, float *dScales, int8_t *dSaved, float *dSavedScales, float *dRstd, void *stream);
+
+/* Its gradient, from dY = d loss / d y (through the rounding to codes as if it
+ * were the identity) and, where h was also used by others, dDh = d loss / d h:
+ *   xh = h rstd, c = mean_j(dY_j gain_j xh_j),
+ *   dDx = rstd (dY gain - xh c) + dDh   (the gradient of x and of the residual),
+ *   dDgain_j = sum over rows of dY_j xh_j   (fp32 [cols]; NULL: not wanted).
+ * h comes from dH, or, with dH NULL, from the checkpoint dSaved / dSavedScales.
+ * dDh and dGain may be NULL.  dDx may be dDh, and must not overlap the other
+ * inputs.  The sums over rows go through dScratch (16-byte aligned, at least
+ * the size below; FMM_ERR_WORKSPACE) in a fixed order: repeated calls agree bit
+ * for bit. */
+int fmm_rmsnorm_q8_backward_scratch_size(const fmm_norm_desc *desc, size_t *bytes);
+int fmm_rmsnorm_q8_backward(const fmm_norm_desc *desc, const void *dDy, const void *dDh, const void *dH,
+                            const int8_t *dSaved, const float *dSavedScales, const float *dRstd, const void *dGain,
+                            void *dDx, float *dDgain, void *dScratch, size_t scratch_bytes, void *stream);
+
+typedef struct {
+  int64_t M, N, K;   /* tokens, output channels, input channels; each >= 0, K <= 131071 */
+  int32_t type;      /* FMM_F32, FMM_BF16 or FMM_F16: the output, or its gradient and the gradients from it */
+} fmm_q8_desc;
+
+/* dC (M x N, `type`) = dSa[m] dSw[n] sum_k qa[m][k] qw[n][k] + dBias[n]: the codes
+ * dA of the activations (M rows, a scale for each token) against the codes dW of
+ * the weights (N rows, a scale for each output channel); dBias (fp32 [N]) may be
+ * NULL.  The sum over k is exact.  dScratch: 256-byte aligned, at least the size
+ * below (FMM_ERR_WORKSPACE; NULL is fine where that is 0). */
+int fmm_q8_matmul_scratch_size(const fmm_q8_desc *desc, size_t *bytes);
+int fmm_q8_matmul(const fmm_q8_desc *desc, const int8_t *dA, const float *dSa, const int8_t *dW, const float *dSw,
+                  const float *dBias, void *dC, void *dScratch, size_t scratch_bytes, void *stream);
+
+/* The gradients of that product from dDy = d loss / d C (M x N, 16-byte aligned)
+ * and the layer's 8-bit operands, the checkpoint of its input among them:
+ *   dDx (M x K) = (dDy * sw) qw,  dDw (N x K) = (dDy * sa)^T qa,
+ *   dDbias[n] = sum_m dDy[m][n] (fp32).
+ * Any of the three may be NULL (not wanted), and the operands that only it needs
+ * (dW, dSw; dA, dSa) with it.  The products run on the bf16 matrix cores with
+ * fp32 sums.  FMM_BF16 rounds the values q s to bf16, its dY being exact; FMM_F16
+ * carries dY s to 16 bits and FMM_F32 to 24, the codes being exact, at two and
+ * three times the matrix work.  M, N and K at most 4194304
+ * (FMM_ERR_UNSUPPORTED).  dScratch as above. */
+int fmm_q8_linear_backward_scratch_size(const fmm_q8_desc *desc, size_t *bytes);
+int fmm_q8_linear_backward(const fmm_q8_desc *desc, const void *dDy, const int8_t *dA, const float *dSa,
+                           const int8_t *dW, const float *dSw, void *dDx, void *dDw, float *dDbias, void *dScratch,
+                           size_t scratch_bytes, void *stream);
+
 /* ---- misc ---------------------------------------------------------------- */
 
 const char *fmm_status_string(int status);

@@ -67,6 +67,10 @@ FMM_RULE_POW2_OCP = 2
 RULES = {"fp32_amax": FMM_RULE_FP32_AMAX, "pow2_ceil": FMM_RULE_POW2_CEIL,
          "pow2_ocp": FMM_RULE_POW2_OCP}
 
+FMM_F32 = 0
+FMM_BF16 = 1
+FMM_F16 = 2
+
 _vp = ctypes.c_void_p
 _i64 = ctypes.c_int64
 _dp = ctypes.POINTER(ctypes.c_double)
@@ -85,6 +89,18 @@ class fmm_view(ctypes.Structure):
                 ("kdim", ctypes.c_int64), ("kblocks", ctypes.c_int64),
                 ("scale_bytes", ctypes.c_int32), ("code_layout", ctypes.c_int32)]
 
+
+class fmm_norm_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("type", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class fmm_q8_desc(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64), ("N", ctypes.c_int64), ("K", ctypes.c_int64), ("type", ctypes.c_int32)]
+
+
+_norm_p = ctypes.POINTER(fmm_norm_desc)
+_q8_p = ctypes.POINTER(fmm_q8_desc)
+_size_p = ctypes.POINTER(ctypes.c_size_t)
 
 _SIGS = {
     "fmm_realization_builtin": (ctypes.c_int, [ctypes.c_int, ctypes.POINTER(_vp)]),
@@ -126,6 +142,16 @@ _SIGS = {
     "fmm_e4m3_quantize_pow2": (ctypes.c_int, [_vp, _vp, _i64, ctypes.c_int32, _vp]),
     "fmm_encode_noise_scratch_size": (ctypes.c_int, [_vp, ctypes.POINTER(ctypes.c_size_t)]),
     "fmm_encode_noise": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]),
+    "fmm_q8_pitch": (_i64, [_i64]),
+    "fmm_q8_quantize": (ctypes.c_int, [ctypes.c_int, _i64, _i64, _vp, _vp, _vp, _vp]),
+    "fmm_q8_dequantize": (ctypes.c_int, [ctypes.c_int, _i64, _i64, ctypes.c_int, _vp, _vp, _vp, _vp]),
+    "fmm_rmsnorm_q8": (ctypes.c_int, [_norm_p] + [_vp] * 10),
+    "fmm_rmsnorm_q8_backward_scratch_size": (ctypes.c_int, [_norm_p, _size_p]),
+    "fmm_rmsnorm_q8_backward": (ctypes.c_int, [_norm_p] + [_vp] * 10 + [ctypes.c_size_t, _vp]),
+    "fmm_q8_matmul_scratch_size": (ctypes.c_int, [_q8_p, _size_p]),
+    "fmm_q8_matmul": (ctypes.c_int, [_q8_p] + [_vp] * 7 + [ctypes.c_size_t, _vp]),
+    "fmm_q8_linear_backward_scratch_size": (ctypes.c_int, [_q8_p, _size_p]),
+    "fmm_q8_linear_backward": (ctypes.c_int, [_q8_p] + [_vp] * 9 + [ctypes.c_size_t, _vp]),
     "fmm_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "fmm_last_error_detail": (ctypes.c_char_p, []),
     "fmm_device_check": (ctypes.c_int, [ctypes.c_int]),
@@ -466,6 +492,67 @@ def fmm_e4m3_quantize(x, out, n, stream=None) -> None:
 def fmm_e4m3_quantize_pow2(x, out, n, e, stream=None) -> None:
     _check(_lib.fmm_e4m3_quantize_pow2(_ptr(x), _ptr(out), int(n), int(e), _stream(stream)),
            "fmm_e4m3_quantize_pow2")
+
+
+# ---------------------------------------------------------------------------
+# The 8-bit linear layer (descriptors are held by the caller; q8.py wraps these)
+# ---------------------------------------------------------------------------
+
+def fmm_q8_pitch(cols: int) -> int:
+    return _lib.fmm_q8_pitch(int(cols))
+
+
+def fmm_q8_quantize(type, rows, cols, X, codes, scales, stream=None) -> None:
+    _check(_lib.fmm_q8_quantize(type, rows, cols, _ptr(X), _ptr(codes), _ptr(scales), _stream(stream)),
+           "fmm_q8_quantize")
+
+
+def fmm_q8_dequantize(type, rows, cols, group, codes, scales, out, stream=None) -> None:
+    _check(_lib.fmm_q8_dequantize(type, rows, cols, group, _ptr(codes), _ptr(scales), _ptr(out), _stream(stream)),
+           "fmm_q8_dequantize")
+
+
+def fmm_rmsnorm_q8(desc: fmm_norm_desc, X, residual, gain, H, codes, scales, saved, saved_scales, rstd,
+                   stream=None) -> None:
+    _check(_lib.fmm_rmsnorm_q8(desc, _ptr(X), _ptr(residual), _ptr(gain), _ptr(H), _ptr(codes), _ptr(scales),
+                               _ptr(saved), _ptr(saved_scales), _ptr(rstd), _stream(stream)), "fmm_rmsnorm_q8")
+
+
+def fmm_rmsnorm_q8_backward_scratch_size(desc: fmm_norm_desc) -> int:
+    n = ctypes.c_size_t()
+    _check(_lib.fmm_rmsnorm_q8_backward_scratch_size(desc, ctypes.byref(n)), "fmm_rmsnorm_q8_backward_scratch_size")
+    return n.value
+
+
+def fmm_rmsnorm_q8_backward(desc: fmm_norm_desc, dY, dH_in, H, saved, saved_scales, rstd, gain, dX, dgain, scratch,
+                            scratch_bytes: int, stream=None) -> None:
+    _check(_lib.fmm_rmsnorm_q8_backward(desc, _ptr(dY), _ptr(dH_in), _ptr(H), _ptr(saved), _ptr(saved_scales),
+                                        _ptr(rstd), _ptr(gain), _ptr(dX), _ptr(dgain), _ptr(scratch), scratch_bytes,
+                                        _stream(stream)), "fmm_rmsnorm_q8_backward")
+
+
+def fmm_q8_matmul_scratch_size(desc: fmm_q8_desc) -> int:
+    n = ctypes.c_size_t()
+    _check(_lib.fmm_q8_matmul_scratch_size(desc, ctypes.byref(n)), "fmm_q8_matmul_scratch_size")
+    return n.value
+
+
+def fmm_q8_matmul(desc: fmm_q8_desc, A, sa, W, sw, bias, C, scratch, scratch_bytes: int, stream=None) -> None:
+    _check(_lib.fmm_q8_matmul(desc, _ptr(A), _ptr(sa), _ptr(W), _ptr(sw), _ptr(bias), _ptr(C), _ptr(scratch),
+                              scratch_bytes, _stream(stream)), "fmm_q8_matmul")
+
+
+def fmm_q8_linear_backward_scratch_size(desc: fmm_q8_desc) -> int:
+    n = ctypes.c_size_t()
+    _check(_lib.fmm_q8_linear_backward_scratch_size(desc, ctypes.byref(n)), "fmm_q8_linear_backward_scratch_size")
+    return n.value
+
+
+def fmm_q8_linear_backward(desc: fmm_q8_desc, dY, A, sa, W, sw, dX, dW, dbias, scratch, scratch_bytes: int,
+                           stream=None) -> None:
+    _check(_lib.fmm_q8_linear_backward(desc, _ptr(dY), _ptr(A), _ptr(sa), _ptr(W), _ptr(sw), _ptr(dX), _ptr(dW),
+                                       _ptr(dbias), _ptr(scratch), scratch_bytes, _stream(stream)),
+           "fmm_q8_linear_backward")
 
 
 def fmm_status_string(status: int) -> str:

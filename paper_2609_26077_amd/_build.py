@@ -14,7 +14,8 @@ ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 HIPCC = os.path.join(ROCM, "bin", "hipcc")
 
 SOURCES = ["realization.cpp", "optimize.cpp", "plan.cpp", "kernels_encode.hip", "kernels_gemm.hip",
-           "kernels_terms.hip", "kernels_split.hip", "kernels_measure.hip", "kernels_cross.hip"]
+           "kernels_terms.hip", "kernels_split.hip", "kernels_measure.hip", "kernels_cross.hip", "q8.cpp",
+           "kernels_q8_rows.hip", "kernels_q8_matmul.hip", "kernels_q8_grad.hip"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-ffp-contract=off", "-Wall",
           "-Wno-unused-function", "-Wno-unused-variable"]

@@ -207,4 +207,8 @@ int static_error_scratch(void **ptr);
 int launch_e4m3_quantize(const float *in, uint8_t *out, int64_t n, void *stream);
 int launch_e4m3_quantize_pow2(const float *in, uint8_t *out, int64_t n, int e, void *stream);
 
+// ---- shared by the host files (plan.cpp) ----------------------------------
+int hip_status(int e);     // a hipError_t as a status; its text becomes the calling thread's detail
+int compute_units();       // of the current device
+
 }  // namespace fmm

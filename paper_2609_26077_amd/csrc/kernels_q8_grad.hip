@@ -1,0 +1,280 @@
+// The linear layer's gradients from its 8-bit operands:
+//   dX = (dY * sw) Qw   (M x K, contracted over N),
+//   dW = (dY * sa)^T Qa (N x K, contracted over M),  dbias = column sums of dY.
+//
+// int8 codes are exact in bfloat16, so the bf16 matrix cores multiply them by
+// dY directly; what has to be rounded is a product with a scale.
+//   bf16 dY: the scale goes to the codes, bf16(q s), dY itself being exact (one
+//     rounding, half an ulp of bf16, of one operand: the error is about that of
+//     rounding the result to bf16).
+//   fp16 and fp32 dY: the scale goes to dY, and dY s is written as the sum of two
+//     or three bfloat16 parts (16 and 24 significant bits) along a longer
+//     contracted axis, the codes staying exact.
+//
+// Two launches.  The first lays the operands out along the contracted axes
+// (transposes through LDS, converted on the way, padded with zeros to the
+// product's 64-position step) and leaves dY's column sums by 64-row tiles; it
+// moves about 14 bytes for each element of dY and the codes, a tenth of the
+// products' time.  The second runs both products' tiles and adds up the column
+// sums.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "q8_gemm.h"
+
+namespace fmm {
+namespace q8 {
+namespace {
+
+constexpr int kPos = 64;   // bf16 positions of a step
+
+template <int T>
+constexpr int kParts = T == FMM_BF16 ? 1 : T == FMM_F16 ? 2 : 3;
+
+struct LayoutArgs {
+  const void *dy;
+  const int8_t *a, *w;
+  const float *sa, *sw;
+  uint16_t *dyt;      // [parts][N][Mp]: dY^T
+  uint16_t *dyr;      // [parts][M][Np]: dY by rows (null: dY itself serves)
+  uint16_t *at, *wt;  // [K][Mp], [K][Np]
+  float *colsum;      // [M / 64][N]
+  int64_t M, N, K, Mp, Np, pitch;
+  int bm, bn, bk;     // 64-wide tiles of each axis
+  int jobs_dy, jobs_a, jobs_w;   // blocks of each job
+  int want_dx, want_dw, want_db;
+};
+
+__device__ __forceinline__ uint16_t bf16_bits(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
+__device__ __forceinline__ float bf16_value(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
+
+// part p of v: bf16 of what the parts before leave
+template <int P>
+__device__ __forceinline__ void split_parts(float v, uint16_t (&out)[P]) {
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    out[p] = bf16_bits(v);
+    const float r = v - bf16_value(out[p]);
+    v = (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u ? 0.0f : r;   // (nothing is left of NaN and infinity)
+  }
+}
+
+// 16 consecutive values of each part to dst + part * plane
+template <int P>
+__device__ __forceinline__ void store_parts(const float (&v)[16], uint16_t *dst, int64_t plane) {
+  uint16_t b[16][P];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) split_parts<P>(v[i], b[i]);
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    u32x4 o[2];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i / 4][i % 4] = (uint32_t)b[2 * i][p] | (uint32_t)b[2 * i + 1][p] << 16;
+    u32x4 *out = reinterpret_cast<u32x4 *>(dst + p * plane);
+    out[0] = o[0];
+    out[1] = o[1];
+  }
+}
+
+// One 64 x 64 tile a workgroup: thread t reads 16 columns of row t / 4 and
+// writes 16 rows of column t / 4.  LDS rows of 65 floats: both directions fall
+// on distinct banks.
+template <int T>
+__global__ __launch_bounds__(256) void layout_kernel(LayoutArgs g) {
+  constexpr int P = kParts<T>;
+  __shared__ float tile[64][65];
+  const int t = threadIdx.x, r = t >> 2, c = (t & 3) * 16;
+  int id = blockIdx.x;
+  if (id < g.jobs_dy) {
+    // dY: rows m, columns n
+    using E = elem_t<T>;
+    const int64_t m0 = 64 * (int64_t)(id / g.bn), n0 = 64 * (int64_t)(id % g.bn);
+    float v[16];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      float x[8];
+      const int64_t n = n0 + c + 8 * u;
+      load8<T>(static_cast<const E *>(g.dy) + (m0 + r) * g.N + n, m0 + r < g.M ? g.N - n : 0, x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[8 * u + i] = x[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) tile[r][c + i] = v[i];
+    if (g.dyr && g.want_dx && m0 + r < g.M) {
+      if (P > 1) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] *= n0 + c + i < g.N ? g.sw[n0 + c + i] : 0.0f;
+      }
+      store_parts<P>(v, g.dyr + (m0 + r) * g.Np + n0 + c, g.M * g.Np);
+    }
+    __syncthreads();
+    const int64_t n = n0 + r;
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      v[i] = tile[c + i][r];
+      s += v[i];
+    }
+    s += __shfl_xor(s, 1);
+    s += __shfl_xor(s, 2);
+    if (g.want_db && (t & 3) == 0 && n < g.N) g.colsum[(m0 / 64) * g.N + n] = s;
+    if (g.want_dw && n < g.N) {
+      if (P > 1) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] *= m0 + c + i < g.M ? g.sa[m0 + c + i] : 0.0f;
+      }
+      store_parts<P>(v, g.dyt + n * g.Mp + m0 + c, g.N * g.Mp);
+    }
+    return;
+  }
+  // codes: rows x K -> K x rows
+  id -= g.jobs_dy;
+  const bool is_a = id < g.jobs_a;
+  if (!is_a) id -= g.jobs_a;
+  const int8_t *q = is_a ? g.a : g.w;
+  const float *sc = is_a ? g.sa : g.sw;
+  uint16_t *out = is_a ? g.at : g.wt;
+  const int64_t rows = is_a ? g.M : g.N, rp = is_a ? g.Mp : g.Np;
+  const int64_t r0 = 64 * (int64_t)(id / g.bk), k0 = 64 * (int64_t)(id % g.bk);
+  float v[16];
+  if (r0 + r < rows) {
+    const u32x4 w = *reinterpret_cast<const u32x4 *>(q + (r0 + r) * g.pitch + k0 + c);
+    const float s = P == 1 ? sc[r0 + r] : 1.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = (float)(int8_t)(w[i / 4] >> (8 * (i % 4))) * s;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) tile[r][c + i] = v[i];
+  __syncthreads();
+  const int64_t k = k0 + r;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = tile[c + i][r];
+  if (k < g.K) store_parts<1>(v, out + k * rp + r0 + c, 0);
+}
+
+struct GradGemms {
+  GemmProblem p[2];
+  int items0, items;         // blocks of p[0], of both
+  const float *colsum;
+  float *dbias;
+  int64_t N;
+  int tiles;                 // rows of colsum
+};
+
+template <class T, int OUT>
+__global__ __launch_bounds__(T::kThreads, T::kThreads == 512 ? 2 : 1) void grad_kernel(GradGemms g) {
+  __shared__ uint4 lds[2 * T::kSlot / 16];
+  const int id = blockIdx.x;
+  if (id < g.items) {
+    if (id < g.items0) gemm_tile<Bf16, T, OUT>(g.p[0], id, lds);
+    else gemm_tile<Bf16, T, OUT>(g.p[1], id - g.items0, lds);
+    return;
+  }
+  const int64_t n = (int64_t)(id - g.items) * T::kThreads + threadIdx.x;
+  if (n >= g.N) return;
+  float s = 0.0f;
+#pragma unroll 4
+  for (int i = 0; i < g.tiles; ++i) s += g.colsum[(int64_t)i * g.N + n];
+  g.dbias[n] = s;
+}
+
+size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+
+struct Layout {
+  size_t dyt, dyr, at, wt, colsum, total;
+  bool rows;   // dY is laid out by rows too
+};
+Layout layout_of(int type, int64_t M, int64_t N, int64_t K) {
+  const int64_t Mp = round_up(M, kPos), Np = round_up(N, kPos);
+  const int parts = type == FMM_BF16 ? 1 : type == FMM_F16 ? 2 : 3;
+  Layout l;
+  size_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const size_t here = at;
+    at = align256(at + (size_t)bytes);
+    return here;
+  };
+  l.rows = parts > 1 || N % kPos != 0;
+  l.dyt = take(2 * parts * N * Mp);
+  l.dyr = take(l.rows ? 2 * parts * M * Np : 0);
+  l.at = take(2 * K * Mp);
+  l.wt = take(2 * K * Np);
+  l.colsum = take(4 * (Mp / 64) * N);
+  l.total = at;
+  return l;
+}
+
+template <int T, class TL>
+void launch_gemms(GradGemms g, const GradArgs &a, hipStream_t s) {
+  for (int i = 0; i < 2; ++i) {
+    g.p[i].tiles_m = (g.p[i].M + TL::TM - 1) / TL::TM;
+    g.p[i].tiles_n = (g.p[i].N + TL::TN - 1) / TL::TN;
+    g.p[i].splits = 1;
+  }
+  const int64_t dx = a.dx ? (int64_t)g.p[0].tiles_m * g.p[0].tiles_n : 0;
+  const int64_t dw = a.dw ? (int64_t)g.p[1].tiles_m * g.p[1].tiles_n : 0;
+  const int64_t db = a.dbias ? (a.N + TL::kThreads - 1) / TL::kThreads : 0;
+  g.items0 = (int)dx;
+  g.items = (int)(dx + dw);
+  if (dx + dw + db > 0) grad_kernel<TL, T><<<dim3((unsigned)(dx + dw + db)), TL::kThreads, 0, s>>>(g);
+}
+
+template <int T>
+int launch(const GradArgs &a, int ncu, hipStream_t s) {
+  const Layout l = layout_of(T, a.M, a.N, a.K);
+  LayoutArgs g = {};
+  g.dy = a.dy; g.a = a.a; g.w = a.w; g.sa = a.sa; g.sw = a.sw;
+  g.dyt = reinterpret_cast<uint16_t *>(a.ws + l.dyt);
+  g.dyr = l.rows ? reinterpret_cast<uint16_t *>(a.ws + l.dyr) : nullptr;
+  g.at = reinterpret_cast<uint16_t *>(a.ws + l.at);
+  g.wt = reinterpret_cast<uint16_t *>(a.ws + l.wt);
+  g.colsum = reinterpret_cast<float *>(a.ws + l.colsum);
+  g.M = a.M; g.N = a.N; g.K = a.K;
+  g.Mp = round_up(a.M, kPos); g.Np = round_up(a.N, kPos); g.pitch = pitch_of(a.K);
+  g.bm = (int)(g.Mp / 64); g.bn = (int)(g.Np / 64); g.bk = (int)((a.K + 63) / 64);
+  g.want_dx = a.dx != nullptr; g.want_dw = a.dw != nullptr; g.want_db = a.dbias != nullptr;
+  g.jobs_dy = g.want_dw || g.want_db || (g.want_dx && l.rows) ? g.bm * g.bn : 0;
+  g.jobs_a = g.want_dw ? g.bm * g.bk : 0;
+  g.jobs_w = g.want_dx ? g.bn * g.bk : 0;
+  const int jobs = g.jobs_dy + g.jobs_a + g.jobs_w;
+  if (jobs > 0) layout_kernel<T><<<dim3((unsigned)jobs), 256, 0, s>>>(g);
+
+  constexpr int P = kParts<T>;
+  GradGemms q = {};
+  GemmProblem &x = q.p[0], &w = q.p[1];
+  x.A = l.rows ? reinterpret_cast<const uint8_t *>(g.dyr) : static_cast<const uint8_t *>(a.dy);
+  x.pitch_a = 2 * g.Np; x.part_a = 2 * a.M * g.Np;
+  x.B = reinterpret_cast<const uint8_t *>(g.wt); x.pitch_b = 2 * g.Np;
+  x.C = a.dx; x.M = (int)a.M; x.N = (int)a.K; x.steps = g.bn; x.parts = P;
+  w.A = reinterpret_cast<const uint8_t *>(g.dyt);
+  w.pitch_a = 2 * g.Mp; w.part_a = 2 * a.N * g.Mp;
+  w.B = reinterpret_cast<const uint8_t *>(g.at); w.pitch_b = 2 * g.Mp;
+  w.C = a.dw; w.M = (int)a.N; w.N = (int)a.K; w.steps = g.bm; w.parts = P;
+  q.colsum = g.colsum; q.dbias = a.dbias; q.N = a.N; q.tiles = g.bm;
+  auto tiles = [&](int64_t edge) {
+    auto up = [&](int64_t v) { return (v + edge - 1) / edge; };
+    return (a.dx ? up(a.M) * up(a.K) : 0) + (a.dw ? up(a.N) * up(a.K) : 0);
+  };
+  if (tiles(256) >= ncu) launch_gemms<T, Tile256>(q, a, s);
+  else if (tiles(128) >= ncu) launch_gemms<T, Tile128>(q, a, s);
+  else launch_gemms<T, Tile64>(q, a, s);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t grad_scratch(int type, int64_t M, int64_t N, int64_t K, int) { return layout_of(type, M, N, K).total; }
+
+int launch_linear_grad(int type, const GradArgs &a, int ncu, void *stream) {
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (type == FMM_F32) return launch<FMM_F32>(a, ncu, s);
+  if (type == FMM_BF16) return launch<FMM_BF16>(a, ncu, s);
+  return launch<FMM_F16>(a, ncu, s);
+}
+
+}  // namespace q8
+}  // namespace fmm

@@ -1,0 +1,565 @@
+// Rows of 8-bit codes: quantize, dequantize, the RMS norm with the residual's
+// addition and an 8-bit output, and that norm's gradient.
+//
+// All of these move a few bytes an element and compute a few operations on
+// them, so HBM bounds them: a row is read once into registers as fp32, its
+// statistics are reduced across the row's threads, and its outputs are written
+// from the same registers.
+//
+//   v_j = x_j (quantize) or h_j g_j with h = x + res in fp32 (norm)
+//   a = max(amax |v|, 1e-12),  q_j = rne(v_j (127 / a)),  s = a / 127
+//   norm: rstd = (mean h^2 + eps)^-1/2, and the stored scale is s rstd: the
+//   factor rstd of y = h rstd g is common to the row, so it cancels in the
+//   codes, which therefore do not depend on the order the squares are summed in.
+//   The checkpoint of h: the same rule over each group of 128 columns.
+//
+// A magnitude is compared by its bits, where NaN exceeds infinity exceeds every
+// finite value: a row (or group) that holds one of the two gets scale NaN and
+// zero codes.
+//
+// Geometry: TPR threads share a row and hold C chunks of eight consecutive
+// columns each, chunk c of thread t at column 8 (c TPR + t), so that a wave
+// reads consecutive 16-byte vectors and a checkpoint group is 16 consecutive
+// lanes.  Rows of up to 2048 columns take a wave each (no barrier); many rows
+// of more take 256 threads, 16 or 32 elements a thread; few rows take as many
+// threads as the row has chunks, up to 1024, which is what a single token's
+// latency wants.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "q8.h"
+#include "q8_types.h"
+
+namespace fmm {
+namespace q8 {
+namespace {
+
+constexpr uint32_t kInfBits = 0x7f800000u;
+
+__device__ __forceinline__ uint32_t mag(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+struct RowScale {
+  float r;         // 127 / a
+  float s;         // a / 127, NaN where the row holds NaN or infinity
+  uint32_t keep;   // all ones, or zero there
+};
+__device__ __forceinline__ RowScale row_scale(uint32_t amax_bits) {
+  RowScale k;
+  const bool bad = amax_bits >= kInfBits;
+  const float a = bad ? 1.0f : fmaxf(__uint_as_float(amax_bits), 1e-12f);
+  k.r = 127.0f / a;
+  k.s = bad ? __uint_as_float(0x7fc00000u) : a / 127.0f;
+  k.keep = bad ? 0u : ~0u;
+  return k;
+}
+
+// Eight codes.  |v r| <= 127 (1 + 2^-23): adding 1.5 2^23 leaves the nearest
+// integer (ties to even) in the low byte of the sum, in two's complement.
+__device__ __forceinline__ u32x2 codes_of(const float (&v)[8], const RowScale &k) {
+  uint32_t b[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(v[i] * k.r + 12582912.0f);
+  u32x2 w;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t lo = __builtin_amdgcn_perm(b[4 * i + 1], b[4 * i], 0x0c0c0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(b[4 * i + 3], b[4 * i + 2], 0x0c0c0400u);
+    w[i] = (lo | hi << 16) & k.keep;
+  }
+  return w;
+}
+
+// the row's (sum, largest magnitude) from each thread's part
+template <int TPR>
+__device__ __forceinline__ void reduce_row(float &sum, uint32_t &m) {
+  sum = sum64(sum);
+  m = max64(m);
+  if constexpr (TPR > 64) {
+    constexpr int W = TPR / 64;
+    __shared__ float ssum[W];
+    __shared__ uint32_t smax[W];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __syncthreads();   // the last row's reads are done
+    if (lane == 0) {
+      ssum[wave] = sum;
+      smax[wave] = m;
+    }
+    __syncthreads();
+    sum = ssum[0];
+    m = smax[0];
+#pragma unroll
+    for (int i = 1; i < W; ++i) {
+      sum += ssum[i];
+      m = max(m, smax[i]);
+    }
+  }
+}
+
+// The checkpoint of one chunk of h (16 lanes hold a group).
+__device__ __forceinline__ void save_chunk(const float (&h)[8], int8_t *codes, float *scales, int64_t col, int64_t pitch) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, mag(h[i]));
+  const RowScale k = row_scale(max16(m));
+  if (col < pitch) {
+    *reinterpret_cast<u32x2 *>(codes + col) = codes_of(h, k);
+    if ((threadIdx.x & 15) == 0) scales[col / kGroup] = k.s;
+  }
+}
+
+template <int T, int TPR, int C, bool NORM>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rows_kernel(RowArgs a) {
+  constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
+  using E = elem_t<T>;
+  const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  const E *gain = static_cast<const E *>(a.gain);
+  for (int64_t row0 = (int64_t)blockIdx.x * RPB; row0 < a.rows; row0 += (int64_t)gridDim.x * RPB) {
+    const bool live = row0 + sub < a.rows;   // (waves past the last row repeat it and store nothing)
+    const int64_t row = live ? row0 + sub : a.rows - 1;
+    const E *x = static_cast<const E *>(a.x) + row * a.cols;
+    const E *res = static_cast<const E *>(a.res) + row * a.cols;
+    float h[C][8];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int64_t col = 8 * (int64_t)(c * TPR + t);
+      load8<T>(x + col, a.cols - col, h[c]);
+    }
+    if (NORM && a.res) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int64_t col = 8 * (int64_t)(c * TPR + t);
+        float r[8];
+        load8<T>(res + col, a.cols - col, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[c][i] += r[i];
+      }
+    }
+    if (NORM && a.h && live) {
+      E *out = static_cast<E *>(a.h) + row * a.cols;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int64_t col = 8 * (int64_t)(c * TPR + t);
+        store8<T>(out + col, a.cols - col, h[c]);
+      }
+    }
+    float sum = 0.0f;
+    uint32_t m = 0;
+    if (NORM) {
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += h[c][i] * h[c][i];
+      if (a.saved) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+          save_chunk(h[c], a.saved + row * a.pitch, a.saved_scales + row * (a.pitch / kGroup), 8 * (int64_t)(c * TPR + t),
+                     live ? a.pitch : 0);
+      }
+      if (gain) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const int64_t col = 8 * (int64_t)(c * TPR + t);
+          float g[8];
+          load8<T>(gain + col, a.cols - col, g);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) h[c][i] *= g[i];
+        }
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m = max(m, mag(h[c][i]));
+    reduce_row<TPR>(sum, m);
+    const RowScale k = row_scale(m);
+    if (live) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int64_t col = 8 * (int64_t)(c * TPR + t);
+        if (col < a.pitch) *reinterpret_cast<u32x2 *>(a.codes + row * a.pitch + col) = codes_of(h[c], k);
+      }
+      if (t == 0) {
+        if (NORM) {
+          const float rstd = 1.0f / sqrtf(sum / (float)a.cols + a.eps);
+          a.rstd[row] = rstd;
+          a.scales[row] = k.s * rstd;
+        } else {
+          a.scales[row] = k.s;
+        }
+      }
+    }
+  }
+}
+
+// Rows too long for registers: the statistics (and h and its checkpoint) in one
+// walk over the row, the codes in a second.
+template <int T, bool NORM>
+__global__ __launch_bounds__(1024) void long_rows_kernel(RowArgs a) {
+  using E = elem_t<T>;
+  const E *gain = static_cast<const E *>(a.gain);
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const E *x = static_cast<const E *>(a.x) + row * a.cols;
+    const E *res = static_cast<const E *>(a.res) + row * a.cols;
+    auto chunk = [&](int64_t col, float (&h)[8]) {
+      load8<T>(x + col, a.cols - col, h);
+      if (NORM && a.res) {
+        float r[8];
+        load8<T>(res + col, a.cols - col, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] += r[i];
+      }
+    };
+    auto gained = [&](int64_t col, float (&h)[8]) {
+      if (NORM && gain) {
+        float g[8];
+        load8<T>(gain + col, a.cols - col, g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] *= g[i];
+      }
+    };
+    float sum = 0.0f;
+    uint32_t m = 0;
+    for (int64_t col0 = 0; col0 < a.pitch; col0 += 8 * 1024) {   // (whole waves: the groups' reductions need their 16 lanes)
+      const int64_t col = col0 + 8 * (int64_t)threadIdx.x;
+      float h[8];
+      chunk(col, h);
+      if (NORM) {
+        if (a.h) store8<T>(static_cast<E *>(a.h) + row * a.cols + col, a.cols - col, h);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += h[i] * h[i];
+        if (a.saved) save_chunk(h, a.saved + row * a.pitch, a.saved_scales + row * (a.pitch / kGroup), col, a.pitch);
+        gained(col, h);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m = max(m, mag(h[i]));
+    }
+    reduce_row<1024>(sum, m);
+    const RowScale k = row_scale(m);
+    for (int64_t col = 8 * (int64_t)threadIdx.x; col < a.pitch; col += 8 * 1024) {
+      float h[8];
+      chunk(col, h);
+      gained(col, h);
+      *reinterpret_cast<u32x2 *>(a.codes + row * a.pitch + col) = codes_of(h, k);
+    }
+    if (threadIdx.x == 0) {
+      if (NORM) {
+        const float rstd = 1.0f / sqrtf(sum / (float)a.cols + a.eps);
+        a.rstd[row] = rstd;
+        a.scales[row] = k.s * rstd;
+      } else {
+        a.scales[row] = k.s;
+      }
+    }
+  }
+}
+
+// ---- dequantize: eight columns a thread ------------------------------------------
+template <int T>
+__global__ __launch_bounds__(256) void dequantize_kernel(DequantArgs a) {
+  using E = elem_t<T>;
+  const int64_t chunks = (a.cols + 7) / 8, total = a.rows * chunks;
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < total; e += (int64_t)gridDim.x * 256) {
+    const int64_t row = e / chunks, col = 8 * (e - row * chunks);
+    float v[8];
+    codes8(*reinterpret_cast<const u32x2 *>(a.codes + row * a.pitch + col), v);
+    const float s = a.grouped ? a.scales[row * (a.pitch / kGroup) + col / kGroup] : a.scales[row];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= s;
+    store8<T>(static_cast<E *>(a.out) + row * a.cols + col, a.cols - col, v);
+  }
+}
+
+// ---- the norm's gradient ---------------------------------------------------------
+// With xh = h rstd and w = dy g:  c = mean_j(w_j xh_j),
+//   dx = rstd (w - xh c) + dh,   dg_j = sum over rows of dy_j xh_j.
+// A workgroup keeps its columns' sums of dg in registers over the rows it
+// walks; the workgroups' sums are added in order by a second kernel.
+
+// h of one chunk: stored, or codes times their group's scale
+template <int T, bool SAVED>
+__device__ __forceinline__ void grad_h(const NormGradArgs &a, int64_t row, int64_t col, float (&h)[8]) {
+  if (SAVED) {
+    if (col < a.pitch) {
+      codes8(*reinterpret_cast<const u32x2 *>(a.saved + row * a.pitch + col), h);
+      const float s = a.saved_scales[row * (a.pitch / kGroup) + col / kGroup];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[i] = col + i < a.cols ? h[i] * s : 0.0f;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[i] = 0.0f;
+    }
+  } else {
+    load8<T>(static_cast<const elem_t<T> *>(a.h) + row * a.cols + col, a.cols - col, h);
+  }
+}
+
+template <int TPR>
+__device__ __forceinline__ float reduce_sum(float v) {
+  uint32_t none = 0;
+  reduce_row<TPR>(v, none);
+  return v;
+}
+
+template <int T, int TPR, int C, bool SAVED>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(NormGradArgs a) {
+  constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
+  using E = elem_t<T>;
+  const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  const E *gain = static_cast<const E *>(a.gain);
+  float g[C][8], dg[C][8];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int64_t col = 8 * (int64_t)(c * TPR + t);
+    if (gain) {
+      load8<T>(gain + col, a.cols - col, g[c]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[c][i] = 1.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dg[c][i] = 0.0f;
+  }
+  const float inv = 1.0f / (float)a.cols;
+  for (int64_t row0 = (int64_t)blockIdx.x * RPB; row0 < a.rows; row0 += (int64_t)gridDim.x * RPB) {
+    const bool live = row0 + sub < a.rows;
+    const int64_t row = live ? row0 + sub : a.rows - 1;
+    const float rstd = a.rstd[row];
+    float dy[C][8], xh[C][8], dot = 0.0f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int64_t col = 8 * (int64_t)(c * TPR + t);
+      load8<T>(static_cast<const E *>(a.dy) + row * a.cols + col, a.cols - col, dy[c]);
+      grad_h<T, SAVED>(a, row, col, xh[c]);
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        xh[c][i] *= rstd;
+        const float p = dy[c][i] * xh[c][i];
+        if (live) dg[c][i] += p;
+        dot += p * g[c][i];
+      }
+    const float m = reduce_sum<TPR>(dot) * inv;
+    if (live) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int64_t col = 8 * (int64_t)(c * TPR + t);
+        float o[8];
+        if (a.dh) {
+          load8<T>(static_cast<const E *>(a.dh) + row * a.cols + col, a.cols - col, o);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) o[i] = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] += rstd * (dy[c][i] * g[c][i] - xh[c][i] * m);
+        store8<T>(static_cast<E *>(a.dx) + row * a.cols + col, a.cols - col, o);
+      }
+    }
+  }
+  if (a.dgain) {
+    float *out = a.partial + ((int64_t)blockIdx.x * RPB + sub) * a.cols;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int64_t col = 8 * (int64_t)(c * TPR + t);
+      store8<FMM_F32>(out + col, a.cols - col, dg[c]);
+    }
+  }
+}
+
+// Long rows: two walks for dx; the gain's sums come from a kernel of their own.
+template <int T, bool SAVED>
+__global__ __launch_bounds__(1024) void long_norm_grad_kernel(NormGradArgs a) {
+  using E = elem_t<T>;
+  const E *gain = static_cast<const E *>(a.gain);
+  const float inv = 1.0f / (float)a.cols;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const float rstd = a.rstd[row];
+    auto chunk = [&](int64_t col, float (&w)[8], float (&xh)[8]) {
+      load8<T>(static_cast<const E *>(a.dy) + row * a.cols + col, a.cols - col, w);
+      grad_h<T, SAVED>(a, row, col, xh);
+      if (gain) {
+        float g[8];
+        load8<T>(gain + col, a.cols - col, g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] *= g[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) xh[i] *= rstd;
+    };
+    float dot = 0.0f;
+    for (int64_t col = 8 * (int64_t)threadIdx.x; col < a.cols; col += 8 * 1024) {
+      float w[8], xh[8];
+      chunk(col, w, xh);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) dot += w[i] * xh[i];
+    }
+    const float m = reduce_sum<1024>(dot) * inv;
+    for (int64_t col = 8 * (int64_t)threadIdx.x; col < a.cols; col += 8 * 1024) {
+      float w[8], xh[8], o[8];
+      chunk(col, w, xh);
+      if (a.dh) {
+        load8<T>(static_cast<const E *>(a.dh) + row * a.cols + col, a.cols - col, o);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] += rstd * (w[i] - xh[i] * m);
+      store8<T>(static_cast<E *>(a.dx) + row * a.cols + col, a.cols - col, o);
+    }
+  }
+}
+
+// the sums of dy xh over each block's rows, columns 2048 blockIdx.y + 8 t ..
+template <int T, bool SAVED>
+__global__ __launch_bounds__(256) void long_gain_grad_kernel(NormGradArgs a) {
+  const int64_t col = 2048 * (int64_t)blockIdx.y + 8 * (int64_t)threadIdx.x;
+  if (col >= a.cols) return;
+  float dg[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) dg[i] = 0.0f;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    float dy[8], h[8];
+    load8<T>(static_cast<const elem_t<T> *>(a.dy) + row * a.cols + col, a.cols - col, dy);
+    grad_h<T, SAVED>(a, row, col, h);
+    const float rstd = a.rstd[row];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dg[i] += dy[i] * (h[i] * rstd);
+  }
+  store8<FMM_F32>(a.partial + (int64_t)blockIdx.x * a.cols + col, a.cols - col, dg);
+}
+
+// out[j] = sum over n rows of partial[row][j], in ascending order within each
+// of eight interleaved sets of rows, which are then added in order
+__global__ __launch_bounds__(256) void sum_partials_kernel(const float *__restrict__ partial, float *__restrict__ out,
+                                                           int64_t n, int64_t cols) {
+  __shared__ float part[8][32];
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+  const int64_t col = 32 * (int64_t)blockIdx.x + x;
+  float s = 0.0f;
+  if (col < cols) {
+#pragma unroll 4
+    for (int64_t r = y; r < n; r += 8) s += partial[r * cols + col];
+  }
+  part[y][x] = s;
+  __syncthreads();
+  if (y == 0 && col < cols) {
+#pragma unroll
+    for (int i = 1; i < 8; ++i) s += part[i][x];
+    out[col] = s;
+  }
+}
+
+// ---- geometry --------------------------------------------------------------------
+constexpr int64_t kMaxBlocks = 1 << 20;   // (blocks times 1024 threads stay under the launch limit)
+constexpr int64_t kFewRows = 512;         // up to two rows a compute unit: a row takes all the threads it can use
+
+struct Geometry {
+  int tpr, c;
+};
+Geometry geometry(int64_t rows, int64_t cols) {
+  if (cols > kMaxHeldCols) return {0, 0};
+  const bool few = rows <= kFewRows;
+  if (cols <= 512) return {64, 1};
+  if (cols <= 2048) return few ? Geometry{256, 1} : Geometry{64, 4};
+  if (cols <= 8192 && few) return {1024, 1};
+  if (cols <= 4096) return {256, 2};
+  if (cols <= 8192) return {256, 4};
+  return {1024, 4};
+}
+
+template <int T, bool NORM>
+void launch_rows(const RowArgs &a, hipStream_t s) {
+  const Geometry g = geometry(a.rows, a.cols);
+  const int rpb = g.tpr == 64 ? 4 : 1;
+  const dim3 grid((unsigned)std::min<int64_t>((a.rows + rpb - 1) / rpb, kMaxBlocks));
+  if (g.tpr == 0) long_rows_kernel<T, NORM><<<grid, 1024, 0, s>>>(a);
+  else if (g.tpr == 64 && g.c == 1) rows_kernel<T, 64, 1, NORM><<<grid, 256, 0, s>>>(a);
+  else if (g.tpr == 64) rows_kernel<T, 64, 4, NORM><<<grid, 256, 0, s>>>(a);
+  else if (g.tpr == 256 && g.c == 1) rows_kernel<T, 256, 1, NORM><<<grid, 256, 0, s>>>(a);
+  else if (g.tpr == 256 && g.c == 2) rows_kernel<T, 256, 2, NORM><<<grid, 256, 0, s>>>(a);
+  else if (g.tpr == 256) rows_kernel<T, 256, 4, NORM><<<grid, 256, 0, s>>>(a);
+  else if (g.c == 1) rows_kernel<T, 1024, 1, NORM><<<grid, 1024, 0, s>>>(a);
+  else rows_kernel<T, 1024, 4, NORM><<<grid, 1024, 0, s>>>(a);
+}
+
+template <bool NORM>
+int launch_rows_typed(int type, const RowArgs &a, void *stream) {
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (type == FMM_F32) launch_rows<FMM_F32, NORM>(a, s);
+  else if (type == FMM_BF16) launch_rows<FMM_BF16, NORM>(a, s);
+  else launch_rows<FMM_F16, NORM>(a, s);
+  return hipGetLastError();
+}
+
+// the workgroups that share the rows of a gradient
+int64_t grad_blocks(int64_t rows, int64_t cols) {
+  const Geometry g = geometry(rows, cols);
+  const int64_t rpb = g.tpr == 64 ? 4 : 1;
+  const int64_t most = g.tpr == 1024 ? 256 : g.tpr == 0 ? 64 : 512;
+  return std::max<int64_t>(1, std::min((rows + rpb - 1) / rpb, most));
+}
+
+template <int T, bool SAVED>
+void launch_grad(const NormGradArgs &a, hipStream_t s) {
+  const Geometry g = geometry(a.rows, a.cols);
+  const int64_t blocks = a.rows > 0 ? grad_blocks(a.rows, a.cols) : 0;
+  const dim3 grid((unsigned)blocks);
+  if (blocks == 0) {
+    // no rows: the gain's sums are empty
+  } else if (g.tpr == 0) {
+    const int64_t rb = std::min<int64_t>(a.rows, kMaxBlocks);
+    long_norm_grad_kernel<T, SAVED><<<dim3((unsigned)rb), 1024, 0, s>>>(a);
+    if (a.dgain)
+      long_gain_grad_kernel<T, SAVED><<<dim3((unsigned)blocks, (unsigned)((a.cols + 2047) / 2048)), 256, 0, s>>>(a);
+  } else if (g.tpr == 64 && g.c == 1) norm_grad_kernel<T, 64, 1, SAVED><<<grid, 256, 0, s>>>(a);
+  else if (g.tpr == 64) norm_grad_kernel<T, 64, 4, SAVED><<<grid, 256, 0, s>>>(a);
+  else if (g.tpr == 256 && g.c == 1) norm_grad_kernel<T, 256, 1, SAVED><<<grid, 256, 0, s>>>(a);
+  else if (g.tpr == 256 && g.c == 2) norm_grad_kernel<T, 256, 2, SAVED><<<grid, 256, 0, s>>>(a);
+  else if (g.tpr == 256) norm_grad_kernel<T, 256, 4, SAVED><<<grid, 256, 0, s>>>(a);
+  else if (g.c == 1) norm_grad_kernel<T, 1024, 1, SAVED><<<grid, 1024, 0, s>>>(a);
+  else norm_grad_kernel<T, 1024, 4, SAVED><<<grid, 1024, 0, s>>>(a);
+  if (a.dgain) {
+    const int64_t n = blocks * (g.tpr == 64 ? 4 : 1);
+    sum_partials_kernel<<<dim3((unsigned)((a.cols + 31) / 32)), 256, 0, s>>>(a.partial, a.dgain, n, a.cols);
+  }
+}
+
+template <int T>
+void launch_grad_source(const NormGradArgs &a, hipStream_t s) {
+  if (a.h) launch_grad<T, false>(a, s);
+  else launch_grad<T, true>(a, s);
+}
+
+}  // namespace
+
+int launch_quantize(int type, const RowArgs &a, void *stream) { return launch_rows_typed<false>(type, a, stream); }
+int launch_rmsnorm(int type, const RowArgs &a, void *stream) { return launch_rows_typed<true>(type, a, stream); }
+
+int launch_dequantize(int type, const DequantArgs &a, void *stream) {
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const int64_t total = a.rows * ((a.cols + 7) / 8);
+  const dim3 grid((unsigned)std::min<int64_t>((total + 255) / 256, kMaxBlocks));
+  if (type == FMM_F32) dequantize_kernel<FMM_F32><<<grid, 256, 0, s>>>(a);
+  else if (type == FMM_BF16) dequantize_kernel<FMM_BF16><<<grid, 256, 0, s>>>(a);
+  else dequantize_kernel<FMM_F16><<<grid, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+int64_t norm_grad_partials(int64_t rows, int64_t cols) {
+  return grad_blocks(rows, cols) * (geometry(rows, cols).tpr == 64 ? 4 : 1);
+}
+
+int launch_rmsnorm_grad(int type, const NormGradArgs &a, void *stream) {
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (type == FMM_F32) launch_grad_source<FMM_F32>(a, s);
+  else if (type == FMM_BF16) launch_grad_source<FMM_BF16>(a, s);
+  else launch_grad_source<FMM_F16>(a, s);
+  return hipGetLastError();
+}
+
+}  // namespace q8
+}  // namespace fmm

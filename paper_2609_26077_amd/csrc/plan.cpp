@@ -14,11 +14,28 @@ namespace {
 
 thread_local std::string g_detail;
 
-int hip_status(int e) {
+}  // namespace
+
+int fmm::hip_status(int e) {
   if (e == hipSuccess) return FMM_OK;
   g_detail = hipGetErrorString(static_cast<hipError_t>(e));
   return FMM_ERR_HIP;
 }
+
+// The compute units of the current device (256, gfx950's, if there is none:
+// the layout is chosen before the device is checked).
+int fmm::compute_units() {
+  int dev = 0, ncu = 0;
+  if (hipGetDevice(&dev) != hipSuccess ||
+      hipDeviceGetAttribute(&ncu, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || ncu <= 0)
+    return 256;
+  return ncu;
+}
+
+namespace {
+
+using fmm::compute_units;
+using fmm::hip_status;
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
@@ -26,16 +43,6 @@ bool is_gfx950(int dev) {
   hipDeviceProp_t prop;
   if (hipGetDeviceProperties(&prop, dev) != hipSuccess) return false;
   return std::strncmp(prop.gcnArchName, "gfx950", 6) == 0;
-}
-
-// The compute units of the current device (256, gfx950's, if there is none:
-// the layout is chosen before the device is checked).
-int compute_units() {
-  int dev = 0, ncu = 0;
-  if (hipGetDevice(&dev) != hipSuccess ||
-      hipDeviceGetAttribute(&ncu, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || ncu <= 0)
-    return 256;
-  return ncu;
 }
 
 // Whether the fused 128 x 128 kernel beats the large tiles and their W-combine

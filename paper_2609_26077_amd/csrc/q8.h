@@ -1,0 +1,90 @@
+// The 8-bit linear layer: what its host side and its kernels share.
+#pragma once
+
+#include <cstddef>
+#include <cstdint>
+
+#include "../../include/fmm8.h"
+
+namespace fmm {
+namespace q8 {
+
+constexpr int kGroup = 128;              // code rows are padded to, and checkpoints scaled by, groups of this many columns
+constexpr int64_t kMaxK = 131071;        // int8 products: K 2^14 < 2^31, so an int32 sum cannot overflow
+constexpr int64_t kMaxGradDim = 1 << 22; // gradients: 32-bit byte offsets inside a tile's rows
+constexpr int64_t kMaxRows = (1ll << 31) - 4096;
+
+inline int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+inline int64_t pitch_of(int64_t cols) { return round_up(cols, kGroup); }
+inline int type_bytes(int type) { return type == FMM_F32 ? 4 : 2; }
+
+// ---- rows: quantize, dequantize, RMS norm (kernels_q8_rows.hip) -------------
+struct RowArgs {
+  const void *x, *res, *gain;   // rows x cols, rows x cols or null, cols or null
+  void *h;                      // rows x cols or null: x + res rounded to the type
+  int8_t *codes;                // rows x pitch
+  float *scales;                // rows
+  int8_t *saved;                // rows x pitch or null: the checkpoint of x + res
+  float *saved_scales;          // rows x pitch / 128
+  float *rstd;                  // rows (norm only)
+  int64_t rows, cols, pitch;
+  float eps;
+};
+int launch_quantize(int type, const RowArgs &a, void *stream);
+int launch_rmsnorm(int type, const RowArgs &a, void *stream);
+// widest row that stays in registers (longer ones are read twice)
+constexpr int64_t kMaxHeldCols = 32768;
+
+struct DequantArgs {
+  const int8_t *codes;
+  const float *scales;   // one per row, or one per row and group
+  void *out;             // rows x cols
+  int64_t rows, cols, pitch;
+  int grouped;
+};
+int launch_dequantize(int type, const DequantArgs &a, void *stream);
+
+struct NormGradArgs {
+  const void *dy, *dh, *h, *gain;   // dh, gain may be null; h null: saved
+  const int8_t *saved;
+  const float *saved_scales, *rstd;
+  void *dx;
+  float *dgain;       // cols or null
+  float *partial;     // blocks x cols
+  int64_t rows, cols, pitch;
+};
+// rows of partial sums that the gradient of the gain goes through
+int64_t norm_grad_partials(int64_t rows, int64_t cols);
+int launch_rmsnorm_grad(int type, const NormGradArgs &a, void *stream);
+
+// ---- products (q8_gemm.h, kernels_q8_matmul.hip, kernels_q8_grad.hip) -------
+// C = A B^T over K-contiguous rows: `parts` planes of A (one after the other
+// along the contracted axis) against the same B.
+struct GemmProblem {
+  const uint8_t *A, *B;             // M rows of pitch_a bytes, N rows of pitch_b bytes
+  int64_t pitch_a, pitch_b, part_a; // part_a: bytes from one plane of A to the next
+  const float *sa, *sw, *bias;      // C = acc sa[m] sw[n] + bias[n] (null: 1, 1, 0)
+  void *C;                          // M x N
+  void *partial;                    // splits > 1: [splits][M][N] raw sums
+  int M, N;
+  int steps, parts;                 // 128-byte steps of a plane, planes
+  int tiles_m, tiles_n, splits;
+};
+
+int launch_matmul(int type, const GemmProblem &p, int ncu, void *stream);
+size_t matmul_scratch(int64_t M, int64_t N, int64_t K, int ncu);
+
+struct GradArgs {
+  const void *dy;
+  const int8_t *a, *w;
+  const float *sa, *sw;
+  void *dx, *dw;
+  float *dbias;
+  uint8_t *ws;
+  int64_t M, N, K;
+};
+size_t grad_scratch(int type, int64_t M, int64_t N, int64_t K, int ncu);
+int launch_linear_grad(int type, const GradArgs &a, int ncu, void *stream);
+
+}  // namespace q8
+}  // namespace fmm

@@ -1,0 +1,485 @@
+"""The 8-bit linear layer on the GPU against binary64 (tests/q8_reference.py).
+
+Bars.  u = 2^-24 is half an ulp of binary32, u_T that of the output's type.
+* codes, stored h: equal (the rule is a sequence of binary32 operations, none
+  of which depends on an order of summation);
+* 1 / rms: a row's squares are summed by threads (at most 40 in a chain) and
+  then across them (6 + 16 steps): 64 u relative, and 4 u for the root and
+  division; a norm's scale 4 u more;
+* the norm's gradients: the same sum inside c, then a handful of operations:
+  80 u times the sum of the terms' magnitudes, and u_T |dx| for the store; the
+  gain's sum over rows (rows + 16) u times its terms' magnitudes;
+* the product: the integer sum is exact; its conversion, two scales and the
+  bias's addition each cost u: 4 u |acc sa sw| + 2 u |bias|, and u_T |C|;
+* the linear gradients, S = the sum of the terms' magnitudes: n u S for adding n
+  terms in any order, 2^-19 S for the matrix core's own sums (as in
+  gpu_helpers), and the operand's rounding: 2^-8 S for bf16 (one operand to 8
+  bits), 2^-16 S for fp16 (two parts), 2^-23 S for
+  fp32 (three), and u_T |result|.
+"""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+import q8_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+U = ref.EPS32
+TYPES = ["fp32", "bf16", "fp16"]
+ROUNDING = {"fp32": 2.0 ** -23, "bf16": 2.0 ** -8, "fp16": 2.0 ** -16}
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    return torch
+
+
+@pytest.fixture(scope="module")
+def q8():
+    from paper_2609_26077_amd import q8
+    return q8
+
+
+def dtype_of(torch, t):
+    return {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[t]
+
+
+def randn(torch, seed, *shape, t="fp32", scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (scale * torch.randn(*shape, generator=g)).to(dtype_of(torch, t)).cuda()
+
+
+def f32(x):
+    return x.detach().float().cpu().numpy()
+
+
+def f64(x):
+    return x.detach().double().cpu().numpy()
+
+
+def within(got, want, bound, what):
+    err = np.abs(got - want)
+    bad = ~(err <= bound)
+    assert not bad.any(), f"{what}: {bad.sum()} outside, worst {np.max(err / np.maximum(bound, 1e-300)):.3g} of the bound"
+
+
+def codes(torch, seed, rows, cols):
+    """Codes over the whole int8 range, -128 included, and scales."""
+    g = torch.Generator().manual_seed(seed)
+    q = torch.zeros((rows, ref.pitch(cols)), dtype=torch.int8)
+    q[:, :cols] = torch.randint(-128, 128, (rows, cols), generator=g, dtype=torch.int8)
+    s = torch.rand(rows, generator=g) * 0.05 + 1e-3
+    return q.cuda(), s.cuda()
+
+
+# ---- rows -------------------------------------------------------------------------
+WIDTHS = [1, 7, 8, 127, 128, 129, 511, 513, 1301, 2048, 2056, 4096, 4100, 8192, 8200, 16385, 32768, 32771]
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("rows,cols", [(1, c) for c in WIDTHS] + [(5, 129), (515, 513), (515, 2047), (515, 4095),
+                                                                  (515, 8191), (70, 9001), (9, 40000), (0, 100), (3, 0)])
+def test_quantize_codes(torch, q8, t, rows, cols):
+    x = randn(torch, rows * 7 + cols, rows, cols, t=t, scale=3.0)
+    q, s = q8.quantize(x)
+    want_q, want_s = ref.padded_codes(f32(x))
+    assert np.array_equal(q.cpu().numpy(), want_q)
+    assert np.array_equal(s.cpu().numpy(), want_s)
+    # nearest multiples of the scale, in binary64
+    if rows and cols:
+        v = ref.values(want_q, s.cpu().numpy(), cols)
+        within(v, f64(x), (0.5 + 2.0 ** -15) * f64(s)[:, None], "half a step")
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("cols", [1, 130, 2047, 4097, 33000])
+def test_quantize_rows_without_a_scale(torch, q8, t, cols):
+    """Zero rows, tiny rows, the type's largest values, NaN and infinities (each in a row of its own), ties."""
+    x = randn(torch, 3, 9, cols, t=t)
+    x[0] = 0
+    x[1] = 1e-20 if t != "fp16" else 6e-8
+    x[2, cols // 2] = float("nan")
+    x[3, cols - 1] = float("inf")
+    x[4, 0] = float("-inf")
+    x[5] = torch.finfo(x.dtype).max
+    x[6] = torch.finfo(x.dtype).min
+    x[7] = 0.5
+    x[7, 0] = 127.0          # x 127 / a = 0.5 exactly: to even, 0
+    q, s = q8.quantize(x)
+    want_q, want_s = ref.padded_codes(f32(x))
+    assert np.array_equal(q.cpu().numpy(), want_q)
+    assert np.array_equal(s.cpu().numpy(), want_s, equal_nan=True)
+    assert np.isnan(want_s[2:5]).all() and np.isfinite(np.delete(want_s, [2, 3, 4])).all()
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("offset", [1, 2, 3, 5])
+def test_rows_off_vector_alignment(torch, q8, t, offset):
+    """Matrices that begin at any element of a buffer; outputs stay inside theirs."""
+    rows, cols = 6, 1301
+    buf = randn(torch, 9, rows * cols + 16, t=t)
+    x = buf[offset:offset + rows * cols].view(rows, cols)
+    q, s = q8.quantize(x)
+    want_q, want_s = ref.padded_codes(f32(x))
+    assert np.array_equal(q.cpu().numpy(), want_q) and np.array_equal(s.cpu().numpy(), want_s)
+    out = torch.full((rows * cols + 16,), 7.0, dtype=x.dtype, device="cuda")
+    q8.dequantize(q, s, cols, x.dtype, out=out[offset:offset + rows * cols].view(rows, cols))
+    o = f64(out)
+    assert (o[:offset] == 7).all() and (o[offset + rows * cols:] == 7).all()
+    v = ref.values(want_q, want_s, cols)
+    within(o[offset:offset + rows * cols].reshape(rows, cols), v, (ref.HALF_ULP[t] + U) * np.abs(v), "values")
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 127), (4, 128), (33, 1301), (2, 20000)])
+def test_dequantize(torch, q8, t, rows, cols):
+    q, s = codes(torch, 5, rows, cols)
+    v = ref.values(q.cpu().numpy(), s.cpu().numpy(), cols)
+    within(f64(q8.dequantize(q, s, cols, dtype_of(torch, t))), v, (ref.HALF_ULP[t] + U) * np.abs(v), "rows")
+    sg = torch.rand((rows, ref.pitch(cols) // 128), generator=torch.Generator().manual_seed(1)).cuda()
+    v = ref.values(q.cpu().numpy(), sg.cpu().numpy(), cols)
+    within(f64(q8.dequantize(q, sg, cols, dtype_of(torch, t))), v,
+           (ref.HALF_ULP[t] + U) * np.abs(v) + ref.SMALLEST[t], "groups")
+
+
+NORMS = ([(1, c) for c in WIDTHS]
+         + [(5, 129), (515, 513), (515, 2047), (515, 4095), (515, 8191), (70, 9001), (9, 40000)])
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("rows,cols", NORMS)
+@pytest.mark.parametrize("parts", ["all", "bare"])
+def test_norm(torch, q8, t, rows, cols, parts):
+    """parts: residual, gain and checkpoint, or none of them."""
+    x = randn(torch, rows + cols, rows, cols, t=t, scale=2.0)
+    n = q8.RMSNormQ8(rows, cols, x.dtype, eps=1e-5)
+    res = gain = None
+    h = f32(x)
+    if parts == "all":
+        res, gain = randn(torch, 11, rows, cols, t=t), 1 + randn(torch, 12, cols, t=t, scale=0.2)
+        h = h + f32(res)                                           # binary32
+    o = n.forward(x, res, gain, checkpoint=parts == "all")
+    v = h * f32(gain) if gain is not None else h                   # binary32
+    want_q, want_s = ref.padded_codes(v)
+    assert np.array_equal(o.codes.cpu().numpy(), want_q)
+    h64 = h.astype(np.float64)
+    rstd = ((h64 ** 2).mean(axis=1) + np.float64(np.float32(1e-5))) ** -0.5
+    within(f64(o.rstd), rstd, 68 * U * rstd, "rstd")
+    within(f64(o.scales), want_s * rstd, 72 * U * want_s * rstd, "scales")
+    if parts == "all":
+        assert torch.equal(o.h.cpu(), torch.from_numpy(h).to(x.dtype))
+        cq, cs = ref.checkpoint(h)
+        assert np.array_equal(o.saved_codes.cpu().numpy(), cq)
+        assert np.array_equal(o.saved_scales.cpu().numpy(), cs)
+        if cols > 32768:                                           # (refused: the next test)
+            return
+        again = n.forward(x, res, gain, inplace=True)              # h over the residual
+        assert again.h is res and torch.equal(res, o.h) and torch.equal(again.codes, o.codes)
+        assert torch.equal(again.rstd, o.rstd) and again.saved_codes is None
+    else:
+        assert o.h is x and o.saved_codes is None
+
+
+def test_norm_inplace_is_refused_where_rows_are_read_twice(torch, q8):
+    from paper_2609_26077_amd import FMM_ERR_UNSUPPORTED, FmmError
+    x = randn(torch, 1, 2, 40000)
+    with pytest.raises(FmmError) as e:
+        q8.RMSNormQ8(2, 40000, x.dtype).forward(x, x.clone(), inplace=True)
+    assert e.value.status == FMM_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("t", TYPES)
+def test_norm_rows_that_cannot_be_normalized(torch, q8, t):
+    """A zero row stays zero under eps; NaN and infinity give NaN rows and NaN groups, and leave the other rows alone."""
+    rows, cols = 5, 300
+    x = randn(torch, 2, rows, cols, t=t)
+    x[1] = 0
+    x[2, 299] = float("nan")
+    x[3, 130] = float("inf")
+    o = q8.RMSNormQ8(rows, cols, x.dtype).forward(x, checkpoint=True)
+    y = f64(q8.dequantize(o.codes, o.scales, cols))
+    assert (y[1] == 0).all() and np.isnan(y[2]).all() and np.isnan(y[3]).all()
+    alone = q8.RMSNormQ8(1, cols, x.dtype)
+    for r in (0, 4):
+        p = alone.forward(x[r:r + 1])
+        assert torch.equal(p.codes[0], o.codes[r]) and torch.equal(p.scales[0], o.scales[r])
+    s = f64(o.saved_scales)
+    assert np.isnan(s[2]).tolist() == [False, False, True] and np.isnan(s[3]).tolist() == [False, True, False]
+    assert np.isfinite(s[[0, 1, 4]]).all()
+
+
+def norm_case(torch, q8, t, rows, cols, gain=True, dh=True):
+    x = randn(torch, rows + cols, rows, cols, t=t, scale=2.0)
+    g = 1 + randn(torch, 21, cols, t=t, scale=0.3) if gain else None
+    if gain:
+        g[cols // 2] = 0
+    n = q8.RMSNormQ8(rows, cols, x.dtype, eps=1e-5)
+    o = n.forward(x, None, g, checkpoint=True)
+    dy = randn(torch, 22, rows, cols, t=t, scale=0.1)
+    d = randn(torch, 23, rows, cols, t=t, scale=0.1) if dh else None
+    return n, x, g, o, dy, d
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("source", ["h", "saved"])
+@pytest.mark.parametrize("rows,cols", NORMS + [(2100, 320), (1100, 1000)])
+def test_norm_gradient(torch, q8, t, source, rows, cols):
+    more = (rows + cols) % 2 == 0                        # with gain and dh, or without
+    n, x, g, o, dy, dh = norm_case(torch, q8, t, rows, cols, more, more)
+    if source == "h":
+        h, given = f64(x), {"h": x}
+    else:
+        h, given = ref.values(o.saved_codes.cpu().numpy(), o.saved_scales.cpu().numpy(), cols), \
+            {"saved": (o.saved_codes, o.saved_scales)}
+    dx, dgain = n.backward(dy, o.rstd, g, dh=dh, **given)
+    want, want_g, terms, terms_g = ref.norm_gradient(h, f64(o.rstd), f64(dy), f64(g) if more else 1.0,
+                                                     f64(dh) if more else 0.0)
+    within(f64(dx), want, 80 * U * terms + ref.HALF_ULP[t] * np.abs(want) + ref.SMALLEST[t], "dx")
+    within(f64(dgain), want_g, (rows + 16) * U * terms_g, "dgain")
+    again, again_g = n.backward(dy, o.rstd, g, dh=dh, **given)
+    assert torch.equal(again, dx) and torch.equal(again_g, dgain)
+    bare, none = n.backward(dy, o.rstd, g, dh=dh, need_gain=False, **given)
+    assert none is None and torch.equal(bare, dx)
+
+
+def test_norm_gradient_against_differences(torch, q8):
+    """L(h, g) = sum dy y(h, g) + sum dh h in binary64, differenced along random
+    directions: a central difference of step e is off by e^2 of third
+    derivatives, here under 1e-6 of the sum of magnitudes."""
+    rows, cols = 7, 200
+    n, x, g, o, dy, dh = norm_case(torch, q8, "fp32", rows, cols)
+    dx, dgain = n.backward(dy, o.rstd, g, h=x, dh=dh)
+    rng = np.random.default_rng(0)
+    h0, g0, DY, DH = f64(x), f64(g), f64(dy), f64(dh)
+
+    def loss(h, gain):
+        rstd = ((h ** 2).mean(axis=1, keepdims=True) + np.float64(np.float32(1e-5))) ** -0.5
+        return (DY * h * rstd * gain).sum() + (DH * h).sum()
+
+    e = 1e-4
+    for _ in range(8):
+        d, dg = rng.standard_normal((rows, cols)), rng.standard_normal(cols)
+        num = (loss(h0 + e * d, g0) - loss(h0 - e * d, g0)) / (2 * e)
+        assert abs(num - (f64(dx) * d).sum()) <= 1e-5 * np.abs(f64(dx) * d).sum()
+        num = (loss(h0, g0 + e * dg) - loss(h0, g0 - e * dg)) / (2 * e)
+        assert abs(num - (f64(dgain) * dg).sum()) <= 1e-5 * np.abs(f64(dgain) * dg).sum()
+
+
+def test_norm_gradient_of_no_rows(torch, q8):
+    n = q8.RMSNormQ8(0, 50, torch.float32)
+    e = torch.empty((0, 50), device="cuda")
+    dx, dgain = n.backward(e, torch.empty(0, device="cuda"), h=e)
+    assert dx.shape == (0, 50) and (dgain == 0).all()
+
+
+# ---- the product ---------------------------------------------------------------------
+def check_matmul(torch, q8, t, M, N, K, bias, seed=1):
+    a, sa = codes(torch, seed, M, K)
+    w, sw = codes(torch, seed + 1, N, K)
+    b = randn(torch, seed + 2, N, scale=5.0) if bias else None
+    C = q8.LinearQ8(M, N, K, dtype_of(torch, t)).matmul(a, sa, w, sw, b)
+    acc = a.cpu().numpy().astype(np.int64) @ w.cpu().numpy().astype(np.int64).T
+    p = acc * f64(sa)[:, None] * f64(sw)
+    want = p + (f64(b) if bias else 0.0)
+    assert tuple(C.shape) == (M, N)
+    within(f64(C), want, 4 * U * np.abs(p) + (2 * U * np.abs(f64(b)) if bias else 0.0)
+           + ref.HALF_ULP[t] * np.abs(want) + ref.SMALLEST[t], "C")
+
+
+MATMULS = [(1, 1, 1), (1, 16, 128), (1, 1000, 4096), (2, 33, 129), (3, 64, 1000), (4, 130, 640), (5, 257, 2049),
+           (8, 48, 8192), (15, 17, 100), (16, 512, 512), (17, 1, 127), (31, 300, 384), (33, 96, 2000), (48, 1031, 256),
+           (64, 2048, 1024), (65, 65, 65), (100, 4100, 300), (127, 129, 128), (128, 128, 4096), (129, 200, 1301),
+           (255, 257, 256), (300, 4097, 640), (1000, 1302, 1472), (513, 8200, 130), (2049, 2050, 200), (4096, 4096, 256)]
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("M,N,K", MATMULS)
+def test_matmul(torch, q8, t, M, N, K):
+    check_matmul(torch, q8, t, M, N, K, bias=(M + N + K) % 2 == 0)
+
+
+@pytest.mark.parametrize("M,N,K", [(0, 5, 7), (5, 0, 7), (4, 6, 0), (40, 70, 0)])
+def test_matmul_of_nothing(torch, q8, M, N, K):
+    check_matmul(torch, q8, "fp32", M, N, K, bias=True)
+
+
+@pytest.mark.parametrize("M", [1, 3, 20, 70, 200])
+def test_matmul_longest_sum(torch, q8, M):
+    """Every code -128 over the longest contracted axis: the largest int32 sum, 131071 2^14."""
+    K, N = 131071, 40
+    a = torch.zeros((M, ref.pitch(K)), dtype=torch.int8, device="cuda")
+    w = torch.zeros((N, ref.pitch(K)), dtype=torch.int8, device="cuda")
+    a[:, :K] = -128
+    w[:, :K] = -128
+    C = q8.LinearQ8(M, N, K, torch.float32).matmul(a, torch.ones(M, device="cuda"), w, torch.ones(N, device="cuda"))
+    assert (f64(C) == 131071.0 * 2 ** 14).all()
+
+
+def test_matmul_propagates_rows_without_a_scale(torch, q8):
+    M, N, K = 5, 70, 300
+    x, v = randn(torch, 1, M, K), randn(torch, 2, N, K)
+    x[3, 7] = float("inf")
+    v[11, 0] = float("nan")
+    C = f64(q8.LinearQ8(M, N, K, torch.float32).matmul(*q8.quantize(x), *q8.quantize(v)))
+    nan = np.zeros((M, N), bool)
+    nan[3] = True
+    nan[:, 11] = True
+    assert np.array_equal(np.isnan(C), nan)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 100, 300), (20, 33, 500), (70, 130, 256), (300, 257, 384)])
+def test_matmul_writes_only_its_output(torch, q8, M, N, K):
+    a, sa = codes(torch, 1, M, K)
+    w, sw = codes(torch, 2, N, K)
+    for t in TYPES:
+        buf = torch.full((M * N + 64,), 3.0, dtype=dtype_of(torch, t), device="cuda")
+        C = buf[7:7 + M * N].view(M, N)
+        lin = q8.LinearQ8(M, N, K, C.dtype)
+        lin.matmul(a, sa, w, sw, C=C)
+        assert (buf[:7] == 3).all() and (buf[7 + M * N:] == 3).all()
+        assert torch.equal(C, lin.matmul(a, sa, w, sw))
+
+
+# ---- the linear gradients --------------------------------------------------------------
+GRADS = [(1, 1, 1), (1, 100, 300), (2, 64, 64), (7, 130, 65), (33, 1, 200), (64, 64, 128), (65, 63, 1), (100, 257, 129),
+         (128, 512, 256), (256, 2048, 2048), (300, 200, 1000), (1000, 1302, 1472), (2050, 130, 260), (130, 4100, 520),
+         (640, 4096, 4160)]
+
+
+def check_grad(torch, q8, t, M, N, K, need_x=True, need_w=True, bias=True):
+    a, sa = codes(torch, 1, M, K)
+    w, sw = codes(torch, 2, N, K)
+    dy = randn(torch, 3, M, N, t=t, scale=0.1)
+    lin = q8.LinearQ8(M, N, K, dy.dtype)
+    dx, dw, db = lin.backward(dy, a, sa, w, sw, need_x=need_x, need_w=need_w, bias=bias)
+    DY, A, W = f64(dy), ref.values(a.cpu().numpy(), f64(sa), K), ref.values(w.cpu().numpy(), f64(sw), K)
+    r = ROUNDING[t] + 2.0 ** -19
+    for got, P, Q, name in ((dx, DY, W, "dX"), (dw, DY.T, A, "dW")):
+        if got is None:
+            continue
+        want, S = P @ Q, np.abs(P) @ np.abs(Q)
+        within(f64(got), want, (r + P.shape[1] * U) * S + ref.HALF_ULP[t] * np.abs(want) + ref.SMALLEST[t], name)
+    if bias:
+        within(f64(db), DY.sum(axis=0), (M + 4) * U * np.abs(DY).sum(axis=0), "dbias")
+    assert (dx is not None) == need_x and (dw is not None) == need_w and (db is not None) == bias
+    return lin, (dy, a, sa, w, sw), (dx, dw, db)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("M,N,K", GRADS)
+def test_linear_gradient(torch, q8, t, M, N, K):
+    lin, args, first = check_grad(torch, q8, t, M, N, K)
+    for got, again in zip(first, lin.backward(*args, bias=True)):
+        assert torch.equal(got, again)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("x,w,b", [(True, False, False), (False, True, False), (False, False, True), (True, False, True),
+                                   (False, True, True), (False, False, False)])
+def test_linear_gradient_of_what_is_wanted(torch, q8, t, x, w, b):
+    check_grad(torch, q8, t, 70, 130, 200, need_x=x, need_w=w, bias=b)
+
+
+@pytest.mark.parametrize("M,N,K", [(0, 5, 7), (5, 0, 7), (4, 6, 0)])
+def test_linear_gradient_of_nothing(torch, q8, M, N, K):
+    check_grad(torch, q8, "bf16", M, N, K)
+
+
+def test_linear_gradient_against_differences(torch, q8):
+    """The layer is bilinear in the values its operands stand for, so a central difference of its loss is exact."""
+    M, N, K = 40, 33, 50
+    lin, (dy, a, sa, w, sw), (dx, dw, db) = check_grad(torch, q8, "fp32", M, N, K)
+    DY, A, W = f64(dy), ref.values(a.cpu().numpy(), f64(sa), K), ref.values(w.cpu().numpy(), f64(sw), K)
+    rng = np.random.default_rng(0)
+
+    def loss(A, W, b):
+        return (DY * (A @ W.T + b)).sum()
+
+    b0, e = np.zeros(N), 1e-2
+    for _ in range(4):
+        d = rng.standard_normal((M, K))
+        num = (loss(A + e * d, W, b0) - loss(A - e * d, W, b0)) / (2 * e)
+        assert abs(num - (f64(dx) * d).sum()) <= 1e-5 * np.abs(f64(dx) * d).sum()
+        d = rng.standard_normal((N, K))
+        num = (loss(A, W + e * d, b0) - loss(A, W - e * d, b0)) / (2 * e)
+        assert abs(num - (f64(dw) * d).sum()) <= 1e-5 * np.abs(f64(dw) * d).sum()
+        d = rng.standard_normal(N)
+        num = (loss(A, W, b0 + e * d) - loss(A, W, b0 - e * d)) / (2 * e)
+        assert abs(num - (f64(db) * d).sum()) <= 1e-5 * np.abs(f64(db) * d).sum()
+
+
+@pytest.mark.parametrize("t", TYPES)
+def test_linear_gradient_propagates_what_is_not_finite(torch, q8, t):
+    """An infinity of dY reaches its row of dX, its column's row of dW and its bias entry, and nothing else."""
+    M, N, K = 70, 66, 100
+    a, sa = codes(torch, 1, M, K)
+    w, sw = codes(torch, 2, N, K)
+    a[:, :K].clamp_(min=1)     # no 0 x infinity among the terms
+    w[:, :K].clamp_(min=1)
+    dy = randn(torch, 3, M, N, t=t)
+    dy[5, 9] = float("inf")
+    dy[64, 65] = float("nan")
+    dx, dw, db = (f64(v) for v in q8.LinearQ8(M, N, K, dy.dtype).backward(dy, a, sa, w, sw, bias=True))
+    assert (dx[5] == np.inf).all() and np.isnan(dx[64]).all() and np.isfinite(np.delete(dx, [5, 64], axis=0)).all()
+    assert (dw[9] == np.inf).all() and np.isnan(dw[65]).all() and np.isfinite(np.delete(dw, [9, 65], axis=0)).all()
+    assert db[9] == np.inf and np.isnan(db[65]) and np.isfinite(np.delete(db, [9, 65])).all()
+
+
+# ---- streams and graphs ------------------------------------------------------------------
+def layer(torch, q8, M, N, K):
+    norm, lin = q8.RMSNormQ8(M, K, torch.bfloat16), q8.LinearQ8(M, N, K, torch.bfloat16)
+    w, sw = q8.quantize(randn(torch, 5, N, K, t="bf16"))
+    gain = 1 + randn(torch, 6, K, t="bf16", scale=0.1)
+
+    def step(x, res, dc, stream=None):
+        o = norm.forward(x, res, gain, checkpoint=True, stream=stream)
+        c = lin.matmul(o.codes, o.scales, w, sw, stream=stream)
+        dy, dw, db = lin.backward(dc, o.codes, o.scales, w, sw, bias=True, stream=stream)
+        dx, dgain = norm.backward(dy, o.rstd, gain, saved=(o.saved_codes, o.saved_scales), dh=res, stream=stream)
+        return o.h, c, dw, db, dx, dgain
+
+    return step
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 300, 520), (200, 300, 520)])
+def test_streams(torch, q8, M, N, K):
+    """The same results on a stream other than the inputs' own, given by name or made current."""
+    step = layer(torch, q8, M, N, K)
+    args = [randn(torch, s, M, K, t="bf16") for s in (1, 2)] + [randn(torch, 3, M, N, t="bf16")]
+    want = step(*args)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    named = step(*args, stream=side)
+    side.synchronize()
+    by_handle = step(*args, stream=side.cuda_stream)
+    side.synchronize()
+    with torch.cuda.stream(side):
+        current = step(*args)
+    side.synchronize()
+    for got in (named, by_handle, current):
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 300, 520), (200, 300, 520)])
+def test_graph_replays(torch, q8, M, N, K):
+    """Captured once, replayed on new inputs with eager work between, each replay against the eager result."""
+    step = layer(torch, q8, M, N, K)
+    args = [randn(torch, s, M, K, t="bf16") for s in (1, 2)] + [randn(torch, 3, M, N, t="bf16")]
+    step(*args)               # (the workspaces come with the first call)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(*args)
+    for k in range(4):
+        for i, x in enumerate(args):
+            x.copy_(randn(torch, 100 * k + i, *x.shape, t="bf16"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [v.clone() for v in out]
+        want = step(*args)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), k
