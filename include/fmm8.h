@@ -460,7 +460,8 @@ enum {
 /* Bytes (= codes) of one row of codes: cols rounded up to 128 (-1 if cols < 0). */
 int64_t fmm_q8_pitch(int64_t cols);
 
-/* dCodes, dScales = the codes of dX (rows x cols).  rows, cols >= 0. */
+/* dCodes, dScales = the codes of dX (rows x cols).  rows, cols >= 0; more than
+ * 2^30 rows or 2^24 columns: FMM_ERR_UNSUPPORTED, as in the calls below. */
 int fmm_q8_quantize(int type, int64_t rows, int64_t cols, const void *dX, int8_t *dCodes, float *dScales, void *stream);
 
 /* dOut (rows x cols, `type`) = the values that codes stand for: group 0, one
@@ -502,7 +503,9 @@ int fmm_rmsnorm_q8_backward(const fmm_norm_desc *desc, const void *dDy, const vo
                             void *dDx, float *dDgain, void *dScratch, size_t scratch_bytes, void *stream);
 
 typedef struct {
-  int64_t M, N, K;   /* tokens, output channels, input channels; each >= 0, K <= 131071 */
+  /* tokens, output channels, input channels; each >= 0.  K <= 131071, M and N at
+   * most 2^30, M N at most 2^37 (FMM_ERR_UNSUPPORTED) */
+  int64_t M, N, K;
   int32_t type;      /* FMM_F32, FMM_BF16 or FMM_F16: the output, or its gradient and the gradients from it */
 } fmm_q8_desc;
 
@@ -523,8 +526,8 @@ int fmm_q8_matmul(const fmm_q8_desc *desc, const int8_t *dA, const float *dSa, c
  * (dW, dSw; dA, dSa) with it.  The products run on the bf16 matrix cores with
  * fp32 sums.  FMM_BF16 rounds the values q s to bf16, its dY being exact; FMM_F16
  * carries dY s to 16 bits and FMM_F32 to 24, the codes being exact, at two and
- * three times the matrix work.  M, N and K at most 4194304
- * (FMM_ERR_UNSUPPORTED).  dScratch as above. */
+ * three times the matrix work.  M and N at most 2^22, and M N, M K and N K at
+ * most 2^34 (FMM_ERR_UNSUPPORTED).  dScratch as above. */
 int fmm_q8_linear_backward_scratch_size(const fmm_q8_desc *desc, size_t *bytes);
 int fmm_q8_linear_backward(const fmm_q8_desc *desc, const void *dDy, const int8_t *dA, const float *dSa,
                            const int8_t *dW, const float *dSw, void *dDx, void *dDw, float *dDbias, void *dScratch,

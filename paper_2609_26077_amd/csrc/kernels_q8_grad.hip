@@ -166,8 +166,8 @@ struct GradGemms {
 };
 
 template <class T, int OUT>
-__global__ __launch_bounds__(T::kThreads, T::kThreads == 512 ? 2 : 1) void grad_kernel(GradGemms g) {
-  __shared__ uint4 lds[2 * T::kSlot / 16];
+__global__ __launch_bounds__(T::kThreads, 2) void grad_kernel(GradGemms g) {
+  __shared__ uint4 lds[T::kLds / 16];
   const int id = blockIdx.x;
   if (id < g.items) {
     if (id < g.items0) gemm_tile<Bf16, T, OUT>(g.p[0], id, lds);
@@ -213,7 +213,6 @@ void launch_gemms(GradGemms g, const GradArgs &a, hipStream_t s) {
   for (int i = 0; i < 2; ++i) {
     g.p[i].tiles_m = (g.p[i].M + TL::TM - 1) / TL::TM;
     g.p[i].tiles_n = (g.p[i].N + TL::TN - 1) / TL::TN;
-    g.p[i].splits = 1;
   }
   const int64_t dx = a.dx ? (int64_t)g.p[0].tiles_m * g.p[0].tiles_n : 0;
   const int64_t dw = a.dw ? (int64_t)g.p[1].tiles_m * g.p[1].tiles_n : 0;
@@ -221,6 +220,33 @@ void launch_gemms(GradGemms g, const GradArgs &a, hipStream_t s) {
   g.items0 = (int)dx;
   g.items = (int)(dx + dw);
   if (dx + dw + db > 0) grad_kernel<TL, T><<<dim3((unsigned)(dx + dw + db)), TL::kThreads, 0, s>>>(g);
+}
+
+// The tile that both products take: t = start + max(chain steps, work steps
+// tiles / CUs) us, as for the int8 product, whose fits of these three these are
+// (a step moves and multiplies as much).
+int pick(const GradGemms &q, const GradArgs &a, int ncu) {
+  constexpr int kEdge[3] = {64, 128, 256};
+  constexpr double kStart[3] = {3.2, 4.5, 7.5}, kChain[3] = {0.20, 0.47, 1.05}, kWork[3] = {0.29, 0.76, 2.45};
+  int best = 0;
+  double least = 1e300;
+  for (int i = 0; i < 3; ++i) {
+    double chain = 0, work = 0;
+    for (int k = 0; k < 2; ++k) {
+      const GemmProblem &p = q.p[k];
+      if (!(k == 0 ? a.dx : a.dw)) continue;
+      const double steps = (double)p.steps * p.parts;
+      const double tiles = (double)((p.M + kEdge[i] - 1) / kEdge[i]) * ((p.N + kEdge[i] - 1) / kEdge[i]);
+      chain = std::max(chain, steps);
+      work += steps * tiles;
+    }
+    const double t = kStart[i] + std::max(kChain[i] * chain, kWork[i] * work / ncu);
+    if (t < least) {
+      best = i;
+      least = t;
+    }
+  }
+  return best;
 }
 
 template <int T>
@@ -255,13 +281,11 @@ int launch(const GradArgs &a, int ncu, hipStream_t s) {
   w.B = reinterpret_cast<const uint8_t *>(g.at); w.pitch_b = 2 * g.Mp;
   w.C = a.dw; w.M = (int)a.N; w.N = (int)a.K; w.steps = g.bm; w.parts = P;
   q.colsum = g.colsum; q.dbias = a.dbias; q.N = a.N; q.tiles = g.bm;
-  auto tiles = [&](int64_t edge) {
-    auto up = [&](int64_t v) { return (v + edge - 1) / edge; };
-    return (a.dx ? up(a.M) * up(a.K) : 0) + (a.dw ? up(a.N) * up(a.K) : 0);
-  };
-  if (tiles(256) >= ncu) launch_gemms<T, Tile256>(q, a, s);
-  else if (tiles(128) >= ncu) launch_gemms<T, Tile128>(q, a, s);
-  else launch_gemms<T, Tile64>(q, a, s);
+  switch (pick(q, a, ncu)) {
+    case 0: launch_gemms<T, Tile64>(q, a, s); break;
+    case 1: launch_gemms<T, Tile128>(q, a, s); break;
+    default: launch_gemms<T, Tile256>(q, a, s);
+  }
   return hipGetLastError();
 }
 

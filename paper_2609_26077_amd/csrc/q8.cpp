@@ -25,20 +25,23 @@ int check_norm(const fmm_norm_desc *d) {
   if (!d || !is_type(d->type) || d->rows < 0 || d->cols < 0) return FMM_ERR_ARG;
   if (!(d->eps >= 0.0f) || !std::isfinite(d->eps)) return FMM_ERR_ARG;
   if (d->cols == 0) return FMM_ERR_SHAPE;
-  if (d->rows > kMaxRows || d->cols > kMaxRows) return FMM_ERR_UNSUPPORTED;
+  if (d->rows > kMaxRows || d->cols > kMaxCols) return FMM_ERR_UNSUPPORTED;
   return FMM_OK;
 }
 
 int check_linear(const fmm_q8_desc *d) {
   if (!d || !is_type(d->type) || d->M < 0 || d->N < 0 || d->K < 0) return FMM_ERR_ARG;
   if (d->K > kMaxK || d->M > kMaxRows || d->N > kMaxRows) return FMM_ERR_UNSUPPORTED;
+  if (d->M * d->N > kMaxOutputs) return FMM_ERR_UNSUPPORTED;
   return FMM_OK;
 }
 
 int check_grad(const fmm_q8_desc *d) {
   const int st = check_linear(d);
   if (st != FMM_OK) return st;
-  return d->M > kMaxGradDim || d->N > kMaxGradDim ? FMM_ERR_UNSUPPORTED : FMM_OK;
+  if (d->M > kMaxGradDim || d->N > kMaxGradDim) return FMM_ERR_UNSUPPORTED;
+  const int64_t most = kMaxGradElements;
+  return d->M * d->N > most || d->M * d->K > most || d->N * d->K > most ? FMM_ERR_UNSUPPORTED : FMM_OK;
 }
 
 size_t norm_grad_scratch(const fmm_norm_desc &d) {
@@ -53,7 +56,7 @@ int64_t fmm_q8_pitch(int64_t cols) { return cols < 0 ? -1 : pitch_of(cols); }
 
 int fmm_q8_quantize(int type, int64_t rows, int64_t cols, const void *dX, int8_t *dCodes, float *dScales, void *stream) {
   if (!is_type(type) || rows < 0 || cols < 0) return FMM_ERR_ARG;
-  if (rows > kMaxRows || cols > kMaxRows) return FMM_ERR_UNSUPPORTED;
+  if (rows > kMaxRows || cols > kMaxCols) return FMM_ERR_UNSUPPORTED;
   if (rows == 0) return FMM_OK;
   if (!good(dScales, 4)) return FMM_ERR_ARG;
   if (cols > 0 && (!good(dX, type_bytes(type)) || !good(dCodes, 16))) return FMM_ERR_ARG;
@@ -70,7 +73,7 @@ int fmm_q8_quantize(int type, int64_t rows, int64_t cols, const void *dX, int8_t
 int fmm_q8_dequantize(int type, int64_t rows, int64_t cols, int group, const int8_t *dCodes, const float *dScales,
                       void *dOut, void *stream) {
   if (!is_type(type) || rows < 0 || cols < 0 || (group != 0 && group != kGroup)) return FMM_ERR_ARG;
-  if (rows > kMaxRows || cols > kMaxRows) return FMM_ERR_UNSUPPORTED;
+  if (rows > kMaxRows || cols > kMaxCols) return FMM_ERR_UNSUPPORTED;
   if (rows == 0 || cols == 0) return FMM_OK;
   if (!good(dCodes, 16) || !good(dScales, 4) || !good(dOut, type_bytes(type))) return FMM_ERR_ARG;
   DequantArgs a = {dCodes, dScales, dOut, rows, cols, pitch_of(cols), group};
@@ -147,7 +150,6 @@ int fmm_q8_matmul(const fmm_q8_desc *desc, const int8_t *dA, const float *dSa, c
   p.sw = dSw;
   p.bias = dBias;
   p.C = dC;
-  p.partial = dScratch;
   p.M = (int)M;
   p.N = (int)N;
   p.steps = (int)(pitch_of(K) / kGroup);

@@ -11,8 +11,10 @@ namespace q8 {
 
 constexpr int kGroup = 128;              // code rows are padded to, and checkpoints scaled by, groups of this many columns
 constexpr int64_t kMaxK = 131071;        // int8 products: K 2^14 < 2^31, so an int32 sum cannot overflow
-constexpr int64_t kMaxGradDim = 1 << 22; // gradients: 32-bit byte offsets inside a tile's rows
-constexpr int64_t kMaxRows = (1ll << 31) - 4096;
+// what keeps every launch under 2^32 threads and a tile's byte offsets in 32 bits
+constexpr int64_t kMaxRows = 1ll << 30, kMaxCols = 1ll << 24;
+constexpr int64_t kMaxOutputs = 1ll << 37;
+constexpr int64_t kMaxGradDim = 1ll << 22, kMaxGradElements = 1ll << 34;
 
 inline int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 inline int64_t pitch_of(int64_t cols) { return round_up(cols, kGroup); }
@@ -63,12 +65,11 @@ int launch_rmsnorm_grad(int type, const NormGradArgs &a, void *stream);
 struct GemmProblem {
   const uint8_t *A, *B;             // M rows of pitch_a bytes, N rows of pitch_b bytes
   int64_t pitch_a, pitch_b, part_a; // part_a: bytes from one plane of A to the next
-  const float *sa, *sw, *bias;      // C = acc sa[m] sw[n] + bias[n] (null: 1, 1, 0)
+  const float *sa, *sw, *bias;      // int8: C = acc sa[m] sw[n] + bias[n] (bias null: 0)
   void *C;                          // M x N
-  void *partial;                    // splits > 1: [splits][M][N] raw sums
   int M, N;
   int steps, parts;                 // 128-byte steps of a plane, planes
-  int tiles_m, tiles_n, splits;
+  int tiles_m, tiles_n;
 };
 
 int launch_matmul(int type, const GemmProblem &p, int ncu, void *stream);

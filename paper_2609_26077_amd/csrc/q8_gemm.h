@@ -3,12 +3,19 @@
 // (fp32 sums).
 //
 // Both element types share one data path.  A step is 128 bytes of every row of
-// the tile (128 int8 or 64 bfloat16 positions) in LDS, two slots, filled by
-// global_load_lds one step ahead; a matrix instruction takes 16 bytes a lane
-// of 32 rows of each side (v_mfma_i32_32x32x32_i8, v_mfma_f32_32x32x16_bf16),
-// so a step is four instructions per 32 x 32 tile.  Which positions a lane's
-// 16 bytes are does not matter as long as both sides agree: instruction t of a
-// step takes chunk 2 t + h of the row in lane half h.
+// the tile (128 int8 or 64 bfloat16 positions) in LDS; a matrix instruction takes
+// 16 bytes a lane of 32 rows of each side (v_mfma_i32_32x32x32_i8,
+// v_mfma_f32_32x32x16_bf16), so a step is four instructions per 32 x 32 tile.
+// Which positions a lane's 16 bytes are does not matter as long as both sides
+// agree: instruction t of a step takes chunk 2 t + h of the row in lane half h.
+//
+// A ring of 2 H + 1 half-slots (one side's rows of one step each) is filled by
+// global_load_lds: while step s is multiplied, steps s + 1 to s + H - 1 and the A
+// side of s + H are on their way, a quarter of a step's transfers started after
+// each half of the step's instructions, so that no wave queues behind a burst of
+// them.  Fragments are read one instruction ahead of the one that takes
+// them, across the barrier too: it stands in the middle of a step's last
+// instructions, when the step has been read and the next one has landed.
 //
 // LDS rows are 128 bytes; 16-byte chunk c of row r sits at chunk
 // c ^ (r & 7) ^ ((r >> 3) & 1), so that the lanes of a fragment read fall on
@@ -39,6 +46,7 @@ constexpr int kStep = 128;   // bytes of a row per step
 struct Int8 {
   typedef v4i frag;
   typedef v16i acc;
+  static constexpr bool kScaled = true;
   static __device__ __forceinline__ acc mma(frag a, frag b, acc c) {
     return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0);
   }
@@ -46,105 +54,199 @@ struct Int8 {
 struct Bf16 {
   typedef v8bf frag;
   typedef v16f acc;
+  static constexpr bool kScaled = false;
   static __device__ __forceinline__ acc mma(frag a, frag b, acc c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
   }
 };
 
-// Tile of TM x TN outputs, WM x WN waves.
-template <int TM_, int TN_, int WM_, int WN_>
+// Tile of TM x TN outputs, WM x WN waves, H steps ahead.
+template <int TM_, int TN_, int WM_, int WN_, int H_>
 struct Tile {
-  static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_;
+  static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, H = H_;
   static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
   static constexpr int MI = TM / WM / 32, NI = TN / WN / 32;   // 32 x 32 tiles of a wave
-  static constexpr int kSlot = (TM + TN) * kStep;
+  static constexpr int kHalf = TM * kStep;                     // one side's rows of one step
+  static constexpr int kLds = (2 * H + 1) * kHalf;
+  static constexpr bool kWhole = MI * NI == 1;   // fragments are read a whole step ahead
   static constexpr int JA = TM / 8 / kWaves, JB = TN / 8 / kWaves;   // transfers of a wave per step and side
+  static_assert(TM == TN && JA % 2 == 0, "equal sides, whole transfers in half of one");
   static_assert(MI * 32 * WM == TM && NI * 32 * WN == TN && JA * 8 * kWaves == TM && JB * 8 * kWaves == TN, "tile");
 };
-typedef Tile<256, 256, 2, 4> Tile256;
-typedef Tile<128, 128, 2, 2> Tile128;
-typedef Tile<64, 64, 2, 2> Tile64;
+typedef Tile<256, 256, 2, 4, 2> Tile256;   // one workgroup a CU
+typedef Tile<128, 128, 2, 2, 2> Tile128;   // two
+typedef Tile<64, 64, 2, 2, 4> Tile64;      // two
 
 __device__ __forceinline__ int swz128(int row) { return (row & 7) ^ ((row >> 3) & 1); }
 
-// Which tile and split item `id` of a problem is.  Workgroups are dispatched
+// Which tile item `id` of a problem is.  Workgroups are dispatched
 // round-robin over the eight XCDs, each with an L2 of its own: the ids of one
 // XCD get a contiguous range of items, and tiles run in groups of GM tile rows,
 // so that the workgroups that share an L2 share rows of A and B.
 template <int GM>
-__device__ __forceinline__ void item_of(int id, int items, int tiles_m, int tiles_n, int &tm, int &tn, int &split) {
+__device__ __forceinline__ void item_of(int id, int items, int tiles_m, int tiles_n, int &tm, int &tn) {
   if (items >= 8) {
     // XCD x takes items base(x) .. : the first `extra` XCDs one more than the others
     const int per = items / 8, extra = items - 8 * per, x = id & 7;
     id = x * per + min(x, extra) + (id >> 3);
   }
-  const int tiles = tiles_m * tiles_n;
-  split = id / tiles;
-  const int tile = id - split * tiles;
   const int per_group = GM * tiles_n;
-  const int group = tile / per_group;
+  const int group = id / per_group;
   const int first = group * GM;
   const int gm = min(tiles_m - first, GM);
-  const int in = tile - group * per_group;
+  const int in = id - group * per_group;
   tm = first + in % gm;
   tn = in / gm;
 }
 
-// Writes (or, for splits, stores raw) a lane's four consecutive columns.
-template <int OUT>
-__device__ __forceinline__ void finish4(const GemmProblem &g, int m, int n, const float (&acc)[4]) {
-  const float sa = g.sa ? g.sa[m] : 1.0f;
-  float v[4];
+// four consecutive floats of p, of which the first n exist (the others: the last one again)
+__device__ __forceinline__ void load4(const float *p, int n, float (&v)[4]) {
+  if (n >= 4) {
+    const u32x4 w = *reinterpret_cast<const u32x4_a4 *>(p);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int c = min(n + i, g.N - 1);
-    v[i] = acc[i] * sa;
-    if (g.sw) v[i] *= g.sw[c];
-    if (g.bias) v[i] += g.bias[c];
+    for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(w[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = p[min(i, n - 1)];
   }
-  store4<OUT>(static_cast<elem_t<OUT> *>(g.C) + (int64_t)m * g.N + n, g.N - n, v);
+}
+
+// What leaves a wave: its MI x NI tiles of 32 x 32 sums, scaled, converted and
+// stored.  A lane holds four consecutive columns of 32 rows apart, which would
+// reach memory as 8-byte pieces of 32 lines at a time (16 us a 256 x 256 tile,
+// as much as ten steps); so the tiles pass through the wave's own part of LDS,
+// free once every wave has read the last step, and leave in rows of 16 bytes a
+// lane (5 us).  16-byte chunk c of a row sits at chunk c ^ (row mod the row's
+// chunks).  FULL: the whole wave tile lies inside C.
+template <class E, class T, int OUT, bool FULL>
+__device__ __forceinline__ void store_tile(const GemmProblem &g, typename E::acc (&acc)[T::MI][T::NI], int m0, int n0,
+                                           uint8_t *lds) {
+  constexpr int B = OUT == FMM_F32 ? 4 : 2, EPC = 16 / B;          // bytes of an element, elements of a chunk
+  constexpr int CH = T::NI * 32 / EPC;                             // chunks of a row
+  constexpr int kRow = CH * 16;
+  constexpr int kPasses = T::kWaves * T::MI * 32 * kRow > T::kLds ? 2 : 1;
+  constexpr int MP = T::MI / kPasses;                              // tile rows of a pass
+  static_assert(MP * kPasses == T::MI && T::kWaves * MP * 32 * kRow <= T::kLds, "the tile passes through LDS");
+  const int lane = threadIdx.x & 63, r32 = lane & 31, h = lane >> 5;
+  float sa[T::MI];
+  if (E::kScaled) {
+#pragma unroll
+    for (int i = 0; i < T::MI; ++i) sa[i] = g.sa[FULL ? m0 + 32 * i + r32 : min(m0 + 32 * i + r32, g.M - 1)];
+  }
+#pragma unroll
+  for (int pass = 0; pass < kPasses; ++pass) {
+#pragma unroll
+    for (int j = 0; j < T::NI; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int n = 32 * j + 8 * q + 4 * h;
+        float sw[4] = {}, bias[4] = {};
+        if (E::kScaled) {
+          const int left = FULL ? 4 : g.N - n0 - n;
+          if (left > 0) {
+            load4(g.sw + n0 + n, left, sw);
+            if (g.bias) load4(g.bias + n0 + n, left, bias);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < MP; ++i) {
+          const int row = 32 * i + r32;
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            v[e] = (float)acc[pass * MP + i][j][4 * q + e];
+            if (E::kScaled) v[e] = v[e] * sa[pass * MP + i] * sw[e] + bias[e];
+          }
+          uint8_t *at = lds + row * kRow + 16 * ((n / EPC) ^ (row & (CH - 1))) + n % EPC * B;
+          if constexpr (OUT == FMM_F32) {
+            *reinterpret_cast<float4 *>(at) = make_float4(v[0], v[1], v[2], v[3]);
+          } else {
+            *reinterpret_cast<uint2 *>(at) = make_uint2(pack2<OUT>(v[0], v[1]), pack2<OUT>(v[2], v[3]));
+          }
+        }
+      }
+    const int lrow = lane / CH, c = lane % CH;
+    const int n = n0 + c * EPC;
+    elem_t<OUT> *out = static_cast<elem_t<OUT> *>(g.C) + (int64_t)(m0 + 32 * pass * MP + lrow) * g.N + n;
+#pragma unroll
+    for (int e = 0; e < MP * 32 * CH / 64; ++e) {
+      const int row = (64 / CH) * e + lrow;
+      const u32x4 v = *reinterpret_cast<const u32x4 *>(lds + row * kRow + 16 * (c ^ (row & (CH - 1))));
+      if (FULL) {
+        *reinterpret_cast<u32x4_a2 *>(out) = v;
+      } else if (m0 + 32 * pass * MP + row < g.M && n < g.N) {
+        if (n + EPC <= g.N) {
+          *reinterpret_cast<u32x4_a2 *>(out) = v;
+        } else {
+#pragma unroll
+          for (int k = 0; k < EPC; ++k)
+            if (n + k < g.N) {
+              if constexpr (B == 4) reinterpret_cast<uint32_t *>(out)[k] = v[k];
+              else reinterpret_cast<uint16_t *>(out)[k] = (uint16_t)(v[k / 2] >> (16 * (k % 2)));
+            }
+        }
+      }
+      out += (int64_t)(64 / CH) * g.N;
+    }
+  }
 }
 
 template <class E, class T, int OUT>
 __device__ __forceinline__ void gemm_tile(const GemmProblem &g, int id, uint4 *lds_raw) {
+  constexpr int J = T::JA;
   const uint8_t *lds = reinterpret_cast<const uint8_t *>(lds_raw);
-  const uint32_t lds_base = dma::lds_addr(lds_raw);
   const int t = threadIdx.x, lane = t & 63;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = wave / T::WN, wn = wave % T::WN;
   const int r32 = lane & 31, h = lane >> 5;
-  int tm, tn, split;
-  item_of<T::TM == 256 ? 4 : 8>(id, g.tiles_m * g.tiles_n * g.splits, g.tiles_m, g.tiles_n, tm, tn, split);
+  int tm, tn;
+  item_of<T::TM == 256 ? 4 : 8>(id, g.tiles_m * g.tiles_n, g.tiles_m, g.tiles_n, tm, tn);
   const int m0 = tm * T::TM, n0 = tn * T::TN;
 
-  // what this wave transfers: rows 8 (wave J + j) + lane / 8 of each side; rows
-  // past the end repeat the last one
+  // what this wave transfers of each side: rows 8 (wave J + j) + lane / 8, j < J;
+  // rows past the end repeat the last one
   const int lrow = lane >> 3, lpos = lane & 7;
-  uint32_t offa[T::JA], offb[T::JB];
+  uint32_t offa[J], offb[J];
 #pragma unroll
-  for (int j = 0; j < T::JA; ++j) {
-    const int row = 8 * (wave * T::JA + j) + lrow;
-    offa[j] = (uint32_t)(min(row, g.M - 1 - m0) * g.pitch_a) + 16u * (uint32_t)(lpos ^ swz128(row));
+  for (int j = 0; j < J; ++j) {
+    const int row = 8 * (wave * J + j) + lrow;
+    const uint32_t c = 16u * (uint32_t)(lpos ^ swz128(row));
+    offa[j] = (uint32_t)(min(row, g.M - 1 - m0) * g.pitch_a) + c;
+    offb[j] = (uint32_t)(min(row, g.N - 1 - n0) * g.pitch_b) + c;
   }
+  const uint8_t *pa = g.A + (int64_t)m0 * g.pitch_a, *pb = g.B + (int64_t)n0 * g.pitch_b;   // the next step's
+  const uint8_t *const pb0 = pb;
+  const int64_t next_part = g.part_a - (int64_t)g.steps * kStep;
+  int ka = 0, kb = 0;                                 // its place in its plane
+  const uint32_t base = dma::lds_addr(lds_raw) + wave * J * 1024;
+  uint32_t wa = 0, wb = T::kHalf, ra = 0, rb = T::kHalf;   // half-slots to fill and to read next, in bytes
+  auto turn = [](uint32_t &x) {
+    x += 2 * T::kHalf;
+    if (x >= T::kLds) x -= T::kLds;
+  };
+  // half q of the next step's rows of A, of B
+  auto start_a = [&](int q) {
 #pragma unroll
-  for (int j = 0; j < T::JB; ++j) {
-    const int row = 8 * (wave * T::JB + j) + lrow;
-    offb[j] = (uint32_t)(min(row, g.N - 1 - n0) * g.pitch_b) + 16u * (uint32_t)(lpos ^ swz128(row));
-  }
-  const int total = g.steps * g.parts;
-  const int s0 = (int)((int64_t)total * split / g.splits), s1 = (int)((int64_t)total * (split + 1) / g.splits);
-  const uint8_t *a0 = g.A + (int64_t)m0 * g.pitch_a, *b0 = g.B + (int64_t)n0 * g.pitch_b;
-  int part = g.parts == 1 ? 0 : s0 / max(g.steps, 1), k = s0 - part * g.steps;   // of the next step to transfer
-  auto issue = [&](int s) {
-    const uint32_t dst = lds_base + (uint32_t)(s & 1) * T::kSlot;
-    const uint8_t *a = a0 + part * g.part_a + (int64_t)k * kStep, *b = b0 + (int64_t)k * kStep;
+    for (int j = q * J / 2; j < (q + 1) * J / 2; ++j) dma::copy16(offa[j], pa, base + wa + j * 1024);
+    if (q == 1) {
+      turn(wa);
+      pa += kStep;
+      if (++ka == g.steps) {
+        ka = 0;
+        pa += next_part;
+      }
+    }
+  };
+  auto start_b = [&](int q) {
 #pragma unroll
-    for (int j = 0; j < T::JA; ++j) dma::copy16(offa[j], a, dst + (wave * T::JA + j) * 1024);
-#pragma unroll
-    for (int j = 0; j < T::JB; ++j) dma::copy16(offb[j], b, dst + T::TM * kStep + (wave * T::JB + j) * 1024);
-    if (++k == g.steps) {
-      k = 0;
-      ++part;
+    for (int j = q * J / 2; j < (q + 1) * J / 2; ++j) dma::copy16(offb[j], pb, base + wb + j * 1024);
+    if (q == 1) {
+      turn(wb);
+      pb += kStep;
+      if (++kb == g.steps) {
+        kb = 0;
+        pb = pb0;
+      }
     }
   };
 
@@ -156,81 +258,143 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem &g, int id, uint4 *l
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
 
-  // byte of chunk 2 t + h of the lane's row in the first 32-row tile of each side
+  // byte of chunk 2 u + h of the lane's row in the first 32-row tile of each side
   // (the rows of the others are 32 further on: the same swizzle)
   uint32_t ca[4], cb[4];
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     const uint32_t c = 16u * (uint32_t)((2 * u + h) ^ swz128(r32));
     ca[u] = (uint32_t)(wm * T::MI * 32 + r32) * kStep + c;
-    cb[u] = (uint32_t)(T::TM + wn * T::NI * 32 + r32) * kStep + c;
+    cb[u] = (uint32_t)(wn * T::NI * 32 + r32) * kStep + c;
   }
+  constexpr int kBufs = T::kWhole ? 8 : 2;
+  typename E::frag fa[kBufs][T::MI], fb[kBufs][T::NI];
+  auto load = [&](int u, int buf) {
+#pragma unroll
+    for (int j = 0; j < T::NI; ++j)
+      fb[buf][j] = *reinterpret_cast<const typename E::frag *>(lds + rb + cb[u] + j * 32 * kStep);
+#pragma unroll
+    for (int i = 0; i < T::MI; ++i)
+      fa[buf][i] = *reinterpret_cast<const typename E::frag *>(lds + ra + ca[u] + i * 32 * kStep);
+    __builtin_amdgcn_sched_barrier(0);   // (left to itself the compiler reads a fragment just before it is used)
+  };
+  auto multiply = [&](int buf, int i0, int i1) {
+#pragma unroll
+    for (int i = i0; i < i1; ++i)
+#pragma unroll
+      for (int j = 0; j < T::NI; ++j) acc[i][j] = E::mma(fb[buf][j], fa[buf][i], acc[i][j]);
+  };
+  // every wave's transfers of the next step have landed (where `later`, kLater of
+  // this wave's may be on their way) and its reads of this one are done
+  auto next_step = [&](bool later) {
+    constexpr int kLater = 2 * J * (T::H - 2) + J;   // H - 2 whole steps, and A of one more
+    if (later) dma::wait_vmcnt<kLater>(); else dma::wait_vmcnt<0>();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
 
-  // Step s: its transfers were issued a step ago; wait for this wave's, barrier
-  // (all have landed, and every wave has read step s - 1), start step s + 1 into
-  // the slot of step s - 1, multiply step s.
-  if (s0 < s1) issue(s0);
-  for (int s = s0; s < s1; ++s) {
-    dma::wait_vmcnt<0>();
-    __syncthreads();
-    if (s + 1 < s1) issue(s + 1);
-    const uint8_t *slot = lds + (s & 1) * T::kSlot;
+  const int ns = g.steps * g.parts;
+  if (ns > 0) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      typename E::frag fa[T::MI], fb[T::NI];
-#pragma unroll
-      for (int j = 0; j < T::NI; ++j) fb[j] = *reinterpret_cast<const typename E::frag *>(slot + cb[u] + j * 32 * kStep);
-#pragma unroll
-      for (int i = 0; i < T::MI; ++i) fa[i] = *reinterpret_cast<const typename E::frag *>(slot + ca[u] + i * 32 * kStep);
-#pragma unroll
-      for (int i = 0; i < T::MI; ++i)
-#pragma unroll
-        for (int j = 0; j < T::NI; ++j) acc[i][j] = E::mma(fb[j], fa[i], acc[i][j]);
+    for (int s = 0; s < T::H - 1; ++s)
+      if (s < ns) {
+        start_a(0); start_a(1); start_b(0); start_b(1);
+      }
+    if (T::H - 1 < ns) {
+      start_a(0); start_a(1);
     }
+    next_step(T::H - 1 < ns);
+    if constexpr (T::kWhole) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) load(u, u);
+      if (T::H - 1 < ns) {
+        start_b(0); start_b(1);
+      }
+      if (T::H < ns) {
+        start_a(0); start_a(1);
+      }
+    } else {
+      if (T::H - 1 < ns) start_b(0);
+      load(0, 0);
+    }
+  }
+  // A step; FULL: H + 1 steps or more come after it.  The steps of the loop are
+  // FULL ones without a branch: where control flow joins, the compiler waits for
+  // every LDS read that is under way, the next step's fragments among them.
+  auto step = [&](int s, auto BUF, auto FULL) {
+    constexpr bool full = decltype(FULL)::value;
+    const bool one = full || s + 1 < ns, more = full || s + T::H - 1 < ns, far = full || s + T::H < ns,
+               far1 = full || s + T::H + 1 < ns;
+    if constexpr (T::kWhole) {
+      // Small tiles: a step's matrix instructions take no longer than reading a
+      // fragment does, so all of a step's fragments are read while the step before
+      // is multiplied.  B of s + H and A of s + H + 1 go where A and B of s were.
+      constexpr int b = decltype(BUF)::value;
+      if (one) {
+        next_step(far);
+        turn(ra);
+        turn(rb);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) load(u, 4 * (1 - b) + u);
+        if (far) {
+          start_b(0); start_b(1);
+        }
+        if (far1) {
+          start_a(0); start_a(1);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) multiply(4 * b + u, 0, T::MI);
+    } else {
+      load(1, 1);
+      multiply(0, 0, T::MI / 2);
+      if (more) start_b(1);
+      multiply(0, T::MI / 2, T::MI);
+      load(2, 0);
+      multiply(1, 0, T::MI / 2);
+      if (far) start_a(0);
+      multiply(1, T::MI / 2, T::MI);
+      load(3, 1);
+      multiply(0, 0, T::MI / 2);
+      if (far) start_a(1);
+      multiply(0, T::MI / 2, T::MI);
+      multiply(1, 0, T::MI / 2);
+      if (one) {
+        // B of s + H may fill A's half-slot of s, and A of s + H + 1 then B's
+        next_step(far);
+        turn(ra);
+        turn(rb);
+        load(0, 0);
+        if (far) start_b(0);
+      }
+      multiply(1, T::MI / 2, T::MI);
+    }
+  };
+  const std::integral_constant<int, 0> even;
+  const std::integral_constant<int, 1> odd;
+  int s = 0;
+  if constexpr (T::kWhole) {
+    for (; s + 1 + T::H + 1 < ns; s += 2) {
+      step(s, even, std::true_type{});
+      step(s + 1, odd, std::true_type{});
+    }
+    for (; s < ns; s += 2) {
+      step(s, even, std::false_type{});
+      if (s + 1 < ns) step(s + 1, odd, std::false_type{});
+    }
+  } else {
+    for (; s + T::H + 1 < ns; ++s) step(s, even, std::true_type{});
+    for (; s < ns; ++s) step(s, even, std::false_type{});
   }
 
   // lane l, accumulator e of tile (i, j): row 32 i + l % 32 of C, column 32 j + 8 (e / 4) + 4 h + e % 4
-#pragma unroll
-  for (int i = 0; i < T::MI; ++i) {
-    const int m = m0 + (wm * T::MI + i) * 32 + r32;
-    if (m >= g.M) continue;
-#pragma unroll
-    for (int j = 0; j < T::NI; ++j)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int n = n0 + (wn * T::NI + j) * 32 + 8 * q + 4 * h;
-        if (n >= g.N) continue;
-        if (g.splits > 1) {
-          // raw sums: int32 bits or fp32
-          uint32_t *p = static_cast<uint32_t *>(g.partial) + ((int64_t)split * g.M + m) * g.N + n;
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (n + e < g.N) p[e] = __builtin_bit_cast(uint32_t, acc[i][j][4 * q + e]);
-        } else {
-          float v[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = (float)acc[i][j][4 * q + e];
-          finish4<OUT>(g, m, n, v);
-        }
-      }
-  }
-}
-
-// The sums of a split problem's parts (in order; int32 sums are exact in any
-// order), four columns a thread.
-template <class E, int OUT>
-__device__ __forceinline__ void finish_splits(const GemmProblem &g, int64_t e, int64_t n4) {
-  const int m = (int)(e / n4), n = 4 * (int)(e - m * n4);
-  float v[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t at = (int64_t)m * g.N + min(n + i, g.N - 1);
-    decltype(typename E::acc()[0] + 0) s = 0;
-    for (int p = 0; p < g.splits; ++p)
-      s += static_cast<const decltype(s) *>(g.partial)[(int64_t)p * g.M * g.N + at];
-    v[i] = (float)s;
-  }
-  finish4<OUT>(g, m, n, v);
+  __syncthreads();
+  const int mw = m0 + wm * T::MI * 32, nw = n0 + wn * T::NI * 32;
+  uint8_t *share = reinterpret_cast<uint8_t *>(lds_raw) + wave * (T::kLds / T::kWaves);
+  if (mw + T::MI * 32 <= g.M && nw + T::NI * 32 <= g.N) store_tile<E, T, OUT, true>(g, acc, mw, nw, share);
+  else store_tile<E, T, OUT, false>(g, acc, mw, nw, share);
 }
 
 }  // namespace q8
