@@ -512,11 +512,9 @@ typedef struct {
 /* dC (M x N, `type`) = dSa[m] dSw[n] sum_k qa[m][k] qw[n][k] + dBias[n]: the codes
  * dA of the activations (M rows, a scale for each token) against the codes dW of
  * the weights (N rows, a scale for each output channel); dBias (fp32 [N]) may be
- * NULL.  The sum over k is exact.  dScratch: 256-byte aligned, at least the size
- * below (FMM_ERR_WORKSPACE; NULL is fine where that is 0). */
-int fmm_q8_matmul_scratch_size(const fmm_q8_desc *desc, size_t *bytes);
+ * NULL.  The sum over k is exact. */
 int fmm_q8_matmul(const fmm_q8_desc *desc, const int8_t *dA, const float *dSa, const int8_t *dW, const float *dSw,
-                  const float *dBias, void *dC, void *dScratch, size_t scratch_bytes, void *stream);
+                  const float *dBias, void *dC, void *stream);
 
 /* The gradients of that product from dDy = d loss / d C (M x N, 16-byte aligned)
  * and the layer's 8-bit operands, the checkpoint of its input among them:
@@ -527,7 +525,8 @@ int fmm_q8_matmul(const fmm_q8_desc *desc, const int8_t *dA, const float *dSa, c
  * fp32 sums.  FMM_BF16 rounds the values q s to bf16, its dY being exact; FMM_F16
  * carries dY s to 16 bits and FMM_F32 to 24, the codes being exact, at two and
  * three times the matrix work.  M and N at most 2^22, and M N, M K and N K at
- * most 2^34 (FMM_ERR_UNSUPPORTED).  dScratch as above. */
+ * most 2^34 (FMM_ERR_UNSUPPORTED).  dScratch: 256-byte aligned, at least the
+ * size below (FMM_ERR_WORKSPACE). */
 int fmm_q8_linear_backward_scratch_size(const fmm_q8_desc *desc, size_t *bytes);
 int fmm_q8_linear_backward(const fmm_q8_desc *desc, const void *dDy, const int8_t *dA, const float *dSa,
                            const int8_t *dW, const float *dSw, void *dDx, void *dDw, float *dDbias, void *dScratch,

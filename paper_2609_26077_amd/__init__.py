@@ -148,8 +148,7 @@ _SIGS = {
     "fmm_rmsnorm_q8": (ctypes.c_int, [_norm_p] + [_vp] * 10),
     "fmm_rmsnorm_q8_backward_scratch_size": (ctypes.c_int, [_norm_p, _size_p]),
     "fmm_rmsnorm_q8_backward": (ctypes.c_int, [_norm_p] + [_vp] * 10 + [ctypes.c_size_t, _vp]),
-    "fmm_q8_matmul_scratch_size": (ctypes.c_int, [_q8_p, _size_p]),
-    "fmm_q8_matmul": (ctypes.c_int, [_q8_p] + [_vp] * 7 + [ctypes.c_size_t, _vp]),
+    "fmm_q8_matmul": (ctypes.c_int, [_q8_p] + [_vp] * 7),
     "fmm_q8_linear_backward_scratch_size": (ctypes.c_int, [_q8_p, _size_p]),
     "fmm_q8_linear_backward": (ctypes.c_int, [_q8_p] + [_vp] * 9 + [ctypes.c_size_t, _vp]),
     "fmm_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -531,15 +530,9 @@ def fmm_rmsnorm_q8_backward(desc: fmm_norm_desc, dY, dH_in, H, saved, saved_scal
                                         _stream(stream)), "fmm_rmsnorm_q8_backward")
 
 
-def fmm_q8_matmul_scratch_size(desc: fmm_q8_desc) -> int:
-    n = ctypes.c_size_t()
-    _check(_lib.fmm_q8_matmul_scratch_size(desc, ctypes.byref(n)), "fmm_q8_matmul_scratch_size")
-    return n.value
-
-
-def fmm_q8_matmul(desc: fmm_q8_desc, A, sa, W, sw, bias, C, scratch, scratch_bytes: int, stream=None) -> None:
-    _check(_lib.fmm_q8_matmul(desc, _ptr(A), _ptr(sa), _ptr(W), _ptr(sw), _ptr(bias), _ptr(C), _ptr(scratch),
-                              scratch_bytes, _stream(stream)), "fmm_q8_matmul")
+def fmm_q8_matmul(desc: fmm_q8_desc, A, sa, W, sw, bias, C, stream=None) -> None:
+    _check(_lib.fmm_q8_matmul(desc, _ptr(A), _ptr(sa), _ptr(W), _ptr(sw), _ptr(bias), _ptr(C), _stream(stream)),
+           "fmm_q8_matmul")
 
 
 def fmm_q8_linear_backward_scratch_size(desc: fmm_q8_desc) -> int:

@@ -291,7 +291,7 @@ int launch(const GradArgs &a, int ncu, hipStream_t s) {
 
 }  // namespace
 
-size_t grad_scratch(int type, int64_t M, int64_t N, int64_t K, int) { return layout_of(type, M, N, K).total; }
+size_t grad_scratch(int type, int64_t M, int64_t N, int64_t K) { return layout_of(type, M, N, K).total; }
 
 int launch_linear_grad(int type, const GradArgs &a, int ncu, void *stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);

@@ -194,8 +194,6 @@ void launch(const GemmProblem &g, int ncu, hipStream_t s) {
 
 }  // namespace
 
-size_t matmul_scratch(int64_t, int64_t, int64_t, int) { return 0; }
-
 int launch_matmul(int type, const GemmProblem &p, int ncu, void *stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (type == FMM_F32) launch<FMM_F32>(p, ncu, s);

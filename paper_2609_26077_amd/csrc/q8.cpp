@@ -123,25 +123,14 @@ int fmm_rmsnorm_q8_backward(const fmm_norm_desc *desc, const void *dDy, const vo
   return fmm::hip_status(launch_rmsnorm_grad(desc->type, a, stream));
 }
 
-int fmm_q8_matmul_scratch_size(const fmm_q8_desc *desc, size_t *bytes) {
-  if (!bytes) return FMM_ERR_ARG;
-  const int st = check_linear(desc);
-  if (st != FMM_OK) return st;
-  *bytes = matmul_scratch(desc->M, desc->N, desc->K, fmm::compute_units());
-  return FMM_OK;
-}
-
 int fmm_q8_matmul(const fmm_q8_desc *desc, const int8_t *dA, const float *dSa, const int8_t *dW, const float *dSw,
-                  const float *dBias, void *dC, void *dScratch, size_t scratch_bytes, void *stream) {
+                  const float *dBias, void *dC, void *stream) {
   const int st = check_linear(desc);
   if (st != FMM_OK) return st;
   const int64_t M = desc->M, N = desc->N, K = desc->K;
   if (M == 0 || N == 0) return FMM_OK;
   if (K > 0 && (!good(dA, 16) || !good(dW, 16))) return FMM_ERR_ARG;
   if (!good(dSa, 4) || !good(dSw, 4) || !fine(dBias, 4) || !good(dC, type_bytes(desc->type))) return FMM_ERR_ARG;
-  const int ncu = fmm::compute_units();
-  const int ws = check_scratch(dScratch, scratch_bytes, matmul_scratch(M, N, K, ncu), 256);
-  if (ws != FMM_OK) return ws;
   GemmProblem p = {};
   p.A = reinterpret_cast<const uint8_t *>(dA);
   p.B = reinterpret_cast<const uint8_t *>(dW);
@@ -154,14 +143,14 @@ int fmm_q8_matmul(const fmm_q8_desc *desc, const int8_t *dA, const float *dSa, c
   p.N = (int)N;
   p.steps = (int)(pitch_of(K) / kGroup);
   p.parts = 1;
-  return fmm::hip_status(launch_matmul(desc->type, p, ncu, stream));
+  return fmm::hip_status(launch_matmul(desc->type, p, fmm::compute_units(), stream));
 }
 
 int fmm_q8_linear_backward_scratch_size(const fmm_q8_desc *desc, size_t *bytes) {
   if (!bytes) return FMM_ERR_ARG;
   const int st = check_grad(desc);
   if (st != FMM_OK) return st;
-  *bytes = grad_scratch(desc->type, desc->M, desc->N, desc->K, fmm::compute_units());
+  *bytes = grad_scratch(desc->type, desc->M, desc->N, desc->K);
   return FMM_OK;
 }
 
@@ -183,11 +172,10 @@ int fmm_q8_linear_backward(const fmm_q8_desc *desc, const void *dDy, const int8_
     if (dDx && (!good(dW, 16) || !good(dSw, 4))) return FMM_ERR_ARG;
     if (dDw && (!good(dA, 16) || !good(dSa, 4))) return FMM_ERR_ARG;
   }
-  const int ncu = fmm::compute_units();
-  const int ws = check_scratch(dScratch, scratch_bytes, grad_scratch(desc->type, M, N, K, ncu), 256);
+  const int ws = check_scratch(dScratch, scratch_bytes, grad_scratch(desc->type, M, N, K), 256);
   if (ws != FMM_OK) return ws;
   GradArgs a = {dDy, dA, dW, dSa, dSw, dDx, dDw, dDbias, static_cast<uint8_t *>(dScratch), M, N, K};
-  return fmm::hip_status(launch_linear_grad(desc->type, a, ncu, stream));
+  return fmm::hip_status(launch_linear_grad(desc->type, a, fmm::compute_units(), stream));
 }
 
 }  // extern "C"

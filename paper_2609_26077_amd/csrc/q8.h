@@ -73,7 +73,6 @@ struct GemmProblem {
 };
 
 int launch_matmul(int type, const GemmProblem &p, int ncu, void *stream);
-size_t matmul_scratch(int64_t M, int64_t N, int64_t K, int ncu);
 
 struct GradArgs {
   const void *dy;
@@ -84,7 +83,7 @@ struct GradArgs {
   uint8_t *ws;
   int64_t M, N, K;
 };
-size_t grad_scratch(int type, int64_t M, int64_t N, int64_t K, int ncu);
+size_t grad_scratch(int type, int64_t M, int64_t N, int64_t K);
 int launch_linear_grad(int type, const GradArgs &a, int ncu, void *stream);
 
 }  // namespace q8

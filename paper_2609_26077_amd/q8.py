@@ -15,19 +15,24 @@ object's workspace is used by one call at a time.
 """
 from __future__ import annotations
 
-from contextlib import nullcontext
+from contextlib import contextmanager
 from typing import NamedTuple, Optional
 
 import torch
 
-from . import (FMM_BF16, FMM_F16, FMM_F32, fmm_norm_desc, fmm_q8_desc, fmm_q8_dequantize,
-               fmm_q8_linear_backward, fmm_q8_linear_backward_scratch_size, fmm_q8_matmul,
-               fmm_q8_matmul_scratch_size, fmm_q8_pitch, fmm_q8_quantize, fmm_rmsnorm_q8, fmm_rmsnorm_q8_backward,
-               fmm_rmsnorm_q8_backward_scratch_size)
+from . import (FMM_BF16, FMM_F16, FMM_F32, _check, _lib, fmm_norm_desc, fmm_q8_desc,
+               fmm_q8_linear_backward_scratch_size, fmm_rmsnorm_q8_backward_scratch_size)
 from .runner import _require
 
 GROUP = 128
 TYPES = {torch.float32: FMM_F32, torch.bfloat16: FMM_BF16, torch.float16: FMM_F16}
+
+# A call's host time is a small product's whole time, so what follows avoids the
+# 3 us of torch.cuda.current_stream() and the device context where it can.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+if _raw_stream is None:
+    def _raw_stream(index):
+        return torch.cuda.current_stream(index).cuda_stream
 
 
 def pitch(cols: int) -> int:
@@ -49,20 +54,49 @@ def _device(device):
     return d
 
 
-def _aligned(x, name, nbytes=16):
-    """The kernels read these by 16-byte vectors."""
-    if x.data_ptr() % nbytes:
-        raise ValueError(f"{name}: not {nbytes}-byte aligned")
+def _tensor(x, name, shape, dtype, device):
+    """_require, with the usual case decided without building what a message needs."""
+    try:
+        if x.dtype is dtype and x.shape == shape and x.device == device and x.is_contiguous():
+            return
+    except AttributeError:
+        pass
+    _require(x, name, shape, dtype, device)
 
 
-def _on(stream):
-    """Outputs are allocated on the stream that writes them, so that torch's
-    allocator reuses their memory in that stream's order."""
-    if stream is None:
-        return nullcontext()
-    if isinstance(stream, int):
-        stream = torch.cuda.ExternalStream(stream)
-    return torch.cuda.stream(stream)
+def _codes(x, name, shape, device):
+    """Codes are read by 16-byte vectors."""
+    _tensor(x, name, shape, torch.int8, device)
+    if x.data_ptr() % 16:
+        raise ValueError(f"{name}: not 16-byte aligned")
+
+
+def _ptr(x):
+    return None if x is None else x.data_ptr()
+
+
+@contextmanager
+def _switched(index, stream):
+    """The device, and the stream where one is given, made current: outputs are
+    allocated on the stream that writes them, so that torch's allocator reuses
+    their memory in that stream's order."""
+    with torch.cuda.device(index):
+        if stream is None:
+            yield _raw_stream(index)
+        else:
+            if isinstance(stream, int):
+                stream = torch.cuda.ExternalStream(stream)
+            with torch.cuda.stream(stream):
+                yield stream.cuda_stream
+
+
+def _run(device, stream, call):
+    """call(stream handle), on the device and the stream."""
+    index = device.index
+    if stream is None and torch.cuda.current_device() == index:
+        return call(_raw_stream(index))
+    with _switched(index, stream) as handle:
+        return call(handle)
 
 
 def _matrix(x, name):
@@ -75,21 +109,23 @@ def _matrix(x, name):
 def quantize(x, codes=None, scales=None, stream=None):
     """(codes, scales) of the rows of x (float32, bfloat16 or float16)."""
     _matrix(x, "x")
-    rows, cols = x.shape
     t = _type(x.dtype)
-    _require(x, "x", (rows, cols), x.dtype, x.device)
-    with torch.cuda.device(x.device), _on(stream):
-        if codes is None:
-            codes = torch.empty((rows, pitch(cols)), dtype=torch.int8, device=x.device)
-        else:
-            _require(codes, "codes", (rows, pitch(cols)), torch.int8, x.device)
-            _aligned(codes, "codes")
-        if scales is None:
-            scales = torch.empty(rows, dtype=torch.float32, device=x.device)
-        else:
-            _require(scales, "scales", (rows,), torch.float32, x.device)
-        fmm_q8_quantize(t, rows, cols, x, codes, scales, stream)
-    return codes, scales
+    rows, cols = x.shape
+    dev, shape = x.device, (rows, pitch(cols))
+    if not x.is_contiguous():
+        raise ValueError("x: not contiguous")
+    if codes is not None:
+        _codes(codes, "codes", shape, dev)
+    if scales is not None:
+        _tensor(scales, "scales", (rows,), torch.float32, dev)
+
+    def call(handle):
+        q = torch.empty(shape, dtype=torch.int8, device=dev) if codes is None else codes
+        s = torch.empty(rows, dtype=torch.float32, device=dev) if scales is None else scales
+        _check(_lib.fmm_q8_quantize(t, rows, cols, x.data_ptr(), q.data_ptr(), s.data_ptr(), handle), "fmm_q8_quantize")
+        return q, s
+
+    return _run(dev, stream, call)
 
 
 def dequantize(codes, scales, cols, dtype=torch.float32, out=None, stream=None):
@@ -97,20 +133,23 @@ def dequantize(codes, scales, cols, dtype=torch.float32, out=None, stream=None):
     the [rows][pitch / 128] of a checkpoint."""
     _matrix(codes, "codes")
     t = _type(dtype)
-    rows, cols = codes.shape[0], int(cols)
-    _require(codes, "codes", (rows, pitch(cols)), torch.int8, codes.device)
-    _aligned(codes, "codes")
+    rows, cols, dev = codes.shape[0], int(cols), codes.device
+    p = pitch(cols)
+    _codes(codes, "codes", (rows, p), dev)
     if not isinstance(scales, torch.Tensor):
         raise ValueError(f"scales: expected a torch.Tensor, got {type(scales).__name__}")
     group = GROUP if scales.dim() == 2 else 0
-    _require(scales, "scales", (rows, pitch(cols) // GROUP) if group else (rows,), torch.float32, codes.device)
-    with torch.cuda.device(codes.device), _on(stream):
-        if out is None:
-            out = torch.empty((rows, cols), dtype=dtype, device=codes.device)
-        else:
-            _require(out, "out", (rows, cols), dtype, codes.device)
-        fmm_q8_dequantize(t, rows, cols, group, codes, scales, out, stream)
-    return out
+    _tensor(scales, "scales", (rows, p // GROUP) if group else (rows,), torch.float32, dev)
+    if out is not None:
+        _tensor(out, "out", (rows, cols), dtype, dev)
+
+    def call(handle):
+        o = torch.empty((rows, cols), dtype=dtype, device=dev) if out is None else out
+        _check(_lib.fmm_q8_dequantize(t, rows, cols, group, codes.data_ptr(), scales.data_ptr(), o.data_ptr(), handle),
+               "fmm_q8_dequantize")
+        return o
+
+    return _run(dev, stream, call)
 
 
 class NormOutput(NamedTuple):
@@ -130,72 +169,76 @@ class RMSNormQ8:
         self.rows, self.cols, self.dtype = int(rows), int(cols), dtype
         self.device = _device(device)
         self.desc = fmm_norm_desc(self.rows, self.cols, _type(dtype), float(eps))
+        P = pitch(self.cols)
+        self._x, self._q, self._s = (self.rows, self.cols), (self.rows, P), (self.rows, P // GROUP)   # shapes
         self.scratch_bytes = fmm_rmsnorm_q8_backward_scratch_size(self.desc)
         self.scratch = None     # the backward pass's workspace, from its first call on
-
-    def _rows(self, x, name):
-        _require(x, name, (self.rows, self.cols), self.dtype, self.device)
-
-    def _floats(self, x, name, n):
-        _require(x, name, (n,), torch.float32, self.device)
 
     def forward(self, x, residual=None, gain=None, checkpoint=False, inplace=False, stream=None) -> NormOutput:
         """h = x + residual; codes and scales of h / rms(h) * gain.  checkpoint:
         also the 8-bit checkpoint of h that `backward` takes.  inplace: h
         replaces the residual."""
-        self._rows(x, "x")
+        dev, dtype, R = self.device, self.dtype, self.rows
+        _tensor(x, "x", self._x, dtype, dev)
         if residual is not None:
-            self._rows(residual, "residual")
+            _tensor(residual, "residual", self._x, dtype, dev)
         elif inplace:
             raise ValueError("inplace: there is no residual to replace")
         if gain is not None:
-            _require(gain, "gain", (self.cols,), self.dtype, self.device)
-        R, P, dev = self.rows, pitch(self.cols), self.device
-        with torch.cuda.device(dev), _on(stream):
+            _tensor(gain, "gain", (self.cols,), dtype, dev)
+
+        def call(handle):
             h = x if residual is None else residual if inplace else torch.empty_like(x)
-            codes = torch.empty((R, P), dtype=torch.int8, device=dev)
+            codes = torch.empty(self._q, dtype=torch.int8, device=dev)
             scales = torch.empty(R, dtype=torch.float32, device=dev)
             rstd = torch.empty(R, dtype=torch.float32, device=dev)
             saved = saved_scales = None
             if checkpoint:
-                saved = torch.empty((R, P), dtype=torch.int8, device=dev)
-                saved_scales = torch.empty((R, P // GROUP), dtype=torch.float32, device=dev)
-            fmm_rmsnorm_q8(self.desc, x, residual, gain, None if residual is None else h, codes, scales, saved,
-                           saved_scales, rstd, stream)
-        return NormOutput(h, codes, scales, rstd, saved, saved_scales)
+                saved = torch.empty(self._q, dtype=torch.int8, device=dev)
+                saved_scales = torch.empty(self._s, dtype=torch.float32, device=dev)
+            _check(_lib.fmm_rmsnorm_q8(self.desc, x.data_ptr(), _ptr(residual), _ptr(gain),
+                                       None if residual is None else h.data_ptr(), codes.data_ptr(), scales.data_ptr(),
+                                       _ptr(saved), _ptr(saved_scales), rstd.data_ptr(), handle), "fmm_rmsnorm_q8")
+            return NormOutput(h, codes, scales, rstd, saved, saved_scales)
+
+        return _run(dev, stream, call)
 
     def backward(self, dy, rstd, gain=None, h=None, saved=None, dh=None, need_gain=True, stream=None):
         """(gradient of x and of the residual, gradient of the gain or None) from
         dy, the gradient of the normalized rows, and dh, that of h from its other
         uses.  The forward pass's h comes as it was stored (h) or as its 8-bit
         checkpoint (saved = (saved_codes, saved_scales))."""
-        R, P, dev = self.rows, pitch(self.cols), self.device
-        self._rows(dy, "dy")
-        self._floats(rstd, "rstd", R)
+        dev, dtype = self.device, self.dtype
+        _tensor(dy, "dy", self._x, dtype, dev)
+        _tensor(rstd, "rstd", (self.rows,), torch.float32, dev)
         if gain is not None:
-            _require(gain, "gain", (self.cols,), self.dtype, dev)
+            _tensor(gain, "gain", (self.cols,), dtype, dev)
         if dh is not None:
-            self._rows(dh, "dh")
+            _tensor(dh, "dh", self._x, dtype, dev)
         if (h is None) == (saved is None):
             raise ValueError("h or saved: exactly one of them")
         codes = scales = None
         if h is not None:
-            self._rows(h, "h")
+            _tensor(h, "h", self._x, dtype, dev)
         else:
             codes, scales = saved
-            _require(codes, "saved codes", (R, P), torch.int8, dev)
-            _aligned(codes, "saved codes")
-            _require(scales, "saved scales", (R, P // GROUP), torch.float32, dev)
-        with torch.cuda.device(dev), _on(stream):
+            _codes(codes, "saved codes", self._q, dev)
+            _tensor(scales, "saved scales", self._s, torch.float32, dev)
+
+        def call(handle):
             dx = torch.empty_like(dy)
             dgain = None
             if need_gain:
                 dgain = torch.empty(self.cols, dtype=torch.float32, device=dev)
                 if self.scratch is None:
                     self.scratch = torch.empty(max(self.scratch_bytes, 16), dtype=torch.uint8, device=dev)
-            fmm_rmsnorm_q8_backward(self.desc, dy, dh, h, codes, scales, rstd, gain, dx, dgain, self.scratch,
-                                    self.scratch_bytes, stream)
-        return dx, dgain
+            _check(_lib.fmm_rmsnorm_q8_backward(self.desc, dy.data_ptr(), _ptr(dh), _ptr(h), _ptr(codes), _ptr(scales),
+                                                rstd.data_ptr(), _ptr(gain), dx.data_ptr(), _ptr(dgain),
+                                                _ptr(self.scratch), self.scratch_bytes, handle),
+                   "fmm_rmsnorm_q8_backward")
+            return dx, dgain
+
+        return _run(dev, stream, call)
 
 
 class LinearQ8:
@@ -206,48 +249,53 @@ class LinearQ8:
         self.M, self.N, self.K, self.dtype = int(M), int(N), int(K), dtype
         self.device = _device(device)
         self.desc = fmm_q8_desc(self.M, self.N, self.K, _type(dtype))
-        with torch.cuda.device(self.device):
-            self.scratch_bytes = fmm_q8_matmul_scratch_size(self.desc)
-        # the forward workspace, and the backward one from its first call on
-        self.scratch = (torch.empty(self.scratch_bytes, dtype=torch.uint8, device=self.device)
-                        if self.scratch_bytes else None)
-        self.grad_scratch_bytes, self.grad_scratch = 0, None
+        self._a, self._w = (self.M, pitch(self.K)), (self.N, pitch(self.K))   # shapes
+        self.grad_scratch_bytes, self.grad_scratch = 0, None     # the backward pass's, from its first call on
 
-    def _operand(self, codes, scales, name, rows):
-        _require(codes, name, (rows, pitch(self.K)), torch.int8, self.device)
-        _aligned(codes, name)
-        _require(scales, name + " scales", (rows,), torch.float32, self.device)
+    def _operands(self, a, sa, w, sw):
+        dev = self.device
+        _codes(a, "a", self._a, dev)
+        _tensor(sa, "a scales", (self.M,), torch.float32, dev)
+        _codes(w, "w", self._w, dev)
+        _tensor(sw, "w scales", (self.N,), torch.float32, dev)
 
     def matmul(self, a, sa, w, sw, bias=None, C=None, stream=None):
         """C = (codes a x scales sa) (codes w x scales sw)^T + bias."""
-        self._operand(a, sa, "a", self.M)
-        self._operand(w, sw, "w", self.N)
+        dev = self.device
+        self._operands(a, sa, w, sw)
         if bias is not None:
-            _require(bias, "bias", (self.N,), torch.float32, self.device)
+            _tensor(bias, "bias", (self.N,), torch.float32, dev)
         if C is not None:
-            _require(C, "C", (self.M, self.N), self.dtype, self.device)
-        with torch.cuda.device(self.device), _on(stream):
-            if C is None:
-                C = torch.empty((self.M, self.N), dtype=self.dtype, device=self.device)
-            fmm_q8_matmul(self.desc, a, sa, w, sw, bias, C, self.scratch, self.scratch_bytes, stream)
-        return C
+            _tensor(C, "C", (self.M, self.N), self.dtype, dev)
+
+        def call(handle):
+            out = torch.empty((self.M, self.N), dtype=self.dtype, device=dev) if C is None else C
+            _check(_lib.fmm_q8_matmul(self.desc, a.data_ptr(), sa.data_ptr(), w.data_ptr(), sw.data_ptr(), _ptr(bias),
+                                      out.data_ptr(), handle), "fmm_q8_matmul")
+            return out
+
+        return _run(dev, stream, call)
 
     def backward(self, dy, a, sa, w, sw, need_x=True, need_w=True, bias=False, stream=None):
         """(dX, dW, dbias) from dy (M x N) and the 8-bit operands; None for what
         is not wanted (bias: whether its gradient is)."""
-        _require(dy, "dy", (self.M, self.N), self.dtype, self.device)
-        _aligned(dy, "dy")
-        self._operand(a, sa, "a", self.M)
-        self._operand(w, sw, "w", self.N)
-        with torch.cuda.device(self.device), _on(stream):
+        dev = self.device
+        _tensor(dy, "dy", (self.M, self.N), self.dtype, dev)
+        if dy.data_ptr() % 16:
+            raise ValueError("dy: not 16-byte aligned")
+        self._operands(a, sa, w, sw)
+
+        def call(handle):
             if self.grad_scratch is None:
                 self.grad_scratch_bytes = fmm_q8_linear_backward_scratch_size(self.desc)
-                self.grad_scratch = torch.empty(max(self.grad_scratch_bytes, 256), dtype=torch.uint8,
-                                                device=self.device)
-            dev = self.device
+                self.grad_scratch = torch.empty(max(self.grad_scratch_bytes, 256), dtype=torch.uint8, device=dev)
             dx = torch.empty((self.M, self.K), dtype=self.dtype, device=dev) if need_x else None
             dw = torch.empty((self.N, self.K), dtype=self.dtype, device=dev) if need_w else None
             dbias = torch.empty(self.N, dtype=torch.float32, device=dev) if bias else None
-            fmm_q8_linear_backward(self.desc, dy, a, sa, w, sw, dx, dw, dbias, self.grad_scratch,
-                                   self.grad_scratch_bytes, stream)
-        return dx, dw, dbias
+            _check(_lib.fmm_q8_linear_backward(self.desc, dy.data_ptr(), a.data_ptr(), sa.data_ptr(), w.data_ptr(),
+                                               sw.data_ptr(), _ptr(dx), _ptr(dw), _ptr(dbias),
+                                               self.grad_scratch.data_ptr(), self.grad_scratch_bytes, handle),
+                   "fmm_q8_linear_backward")
+            return dx, dw, dbias
+
+        return _run(dev, stream, call)

@@ -40,7 +40,7 @@ def test_quantize_refuses(fm):
     for bad in (dict(type=3), dict(type=-1), dict(rows=-1), dict(cols=-1), dict(x=None), dict(codes=None),
                 dict(scales=None), dict(x=P + 2), dict(type=1, x=P + 1), dict(codes=P + 8), dict(scales=P + 2)):
         assert call(**bad) == fm.FMM_ERR_ARG, bad
-    assert call(rows=1 << 31) == fm.FMM_ERR_UNSUPPORTED
+    assert call(rows=(1 << 30) + 1) == call(cols=(1 << 24) + 1) == fm.FMM_ERR_UNSUPPORTED
     assert call(rows=0, x=None, codes=None, scales=None) == fm.FMM_OK
 
 
@@ -93,19 +93,16 @@ def test_norm_backward_refuses(fm):
 
 
 def test_matmul_refuses(fm):
-    def call(M=4, N=5, K=6, type=0, a=P, sa=P, w=P, sw=P, bias=P, c=P, scratch=P, nbytes=1 << 40, desc=True):
+    def call(M=4, N=5, K=6, type=0, a=P, sa=P, w=P, sw=P, bias=P, c=P, desc=True):
         d = fm.fmm_q8_desc(M, N, K, type)
-        return status(fm, "fmm_q8_matmul", d if desc else None, a, sa, w, sw, bias, c, scratch, nbytes, None)
+        return status(fm, "fmm_q8_matmul", d if desc else None, a, sa, w, sw, bias, c, None)
 
     for bad in (dict(desc=False), dict(M=-1), dict(N=-1), dict(K=-1), dict(type=9), dict(a=None), dict(w=None), dict(a=P + 8),
                 dict(w=P + 4), dict(sa=None), dict(sw=None), dict(sa=P + 2), dict(bias=P + 1), dict(c=None), dict(c=P + 2)):
         assert call(**bad) == fm.FMM_ERR_ARG, bad
-    for bad in (dict(K=131072), dict(M=1 << 31), dict(N=1 << 31)):
+    for bad in (dict(K=131072), dict(M=(1 << 30) + 1), dict(N=1 << 31), dict(M=1 << 20, N=(1 << 17) + 1)):
         assert call(**bad) == fm.FMM_ERR_UNSUPPORTED, bad
     assert call(M=0, a=None, c=None) == call(N=0, w=None) == fm.FMM_OK
-    n = ctypes.c_size_t()
-    assert status(fm, "fmm_q8_matmul_scratch_size", None, n) == fm.FMM_ERR_ARG
-    assert status(fm, "fmm_q8_matmul_scratch_size", fm.fmm_q8_desc(1, 1, 131072, 0), n) == fm.FMM_ERR_UNSUPPORTED
 
 
 def test_linear_backward_refuses(fm):
@@ -121,7 +118,8 @@ def test_linear_backward_refuses(fm):
         assert call(**bad) == fm.FMM_ERR_ARG, bad
     for bad in (dict(scratch=None), dict(nbytes=need - 1), dict(scratch=P + 128)):
         assert call(**bad) == fm.FMM_ERR_WORKSPACE, bad
-    for bad in (dict(M=(1 << 22) + 1), dict(N=(1 << 22) + 1), dict(K=131072)):
+    for bad in (dict(M=(1 << 22) + 1), dict(N=(1 << 22) + 1), dict(K=131072), dict(M=1 << 22, K=(1 << 12) + 1),
+                dict(N=1 << 22, K=(1 << 12) + 1), dict(M=1 << 20, N=(1 << 14) + 1)):
         assert call(**bad) == fm.FMM_ERR_UNSUPPORTED, bad
     assert call(dx=None, dw=None, db=None, dy=None) == fm.FMM_OK
 
@@ -131,9 +129,7 @@ def _objects(device="cpu"):
     import torch
     from paper_2609_26077_amd import q8
     n = q8.RMSNormQ8(4, 200, torch.bfloat16, device=device)
-    lin = q8.LinearQ8.__new__(q8.LinearQ8)
-    lin.M, lin.N, lin.K, lin.dtype, lin.device = 4, 6, 200, torch.bfloat16, torch.device(device)
-    return torch, q8, n, lin
+    return torch, q8, n, q8.LinearQ8(4, 6, 200, torch.bfloat16, device=device)
 
 
 def test_wrappers_refuse_types_and_shapes():
