@@ -20,10 +20,14 @@
 // Geometry: TPR threads share a row and hold C chunks of eight consecutive
 // columns each, chunk c of thread t at column 8 (c TPR + t), so that a wave
 // reads consecutive 16-byte vectors and a checkpoint group is 16 consecutive
-// lanes.  Rows of up to 2048 columns take a wave each (no barrier); many rows
-// of more take 256 threads, 16 or 32 elements a thread; few rows take as many
-// threads as the row has chunks, up to 1024, which is what a single token's
-// latency wants.
+// lanes.  Rows of up to 1024 columns take a wave each (no barrier), longer ones
+// as many threads as leave each 8 to 32 elements; where there are few rows, as
+// many as the row has chunks, up to 1024, which is what a single token's latency
+// wants.
+//
+// Measured, forward with residual and checkpoint: 8192 x 4096 bf16 43 us, 5.2 TB/s
+// and more (a 1 GiB copy: 5.2); 1024 x 8192 fp32 21; one token of 4096 3.4.
+// Gradient from the checkpoint, with dh: 53 (floor 45), 26 and 6.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -70,28 +74,28 @@ __device__ __forceinline__ u32x2 codes_of(const float (&v)[8], const RowScale &k
   return w;
 }
 
-// the row's (sum, largest magnitude) from each thread's part
+// the row's (sum, largest magnitude) from each thread's part; `turn` alternates
+// from row to row, so that a row's values outlive the next row's barrier
 template <int TPR>
-__device__ __forceinline__ void reduce_row(float &sum, uint32_t &m) {
+__device__ __forceinline__ void reduce_row(float &sum, uint32_t &m, int turn) {
   sum = sum64(sum);
   m = max64(m);
   if constexpr (TPR > 64) {
     constexpr int W = TPR / 64;
-    __shared__ float ssum[W];
-    __shared__ uint32_t smax[W];
+    __shared__ float ssum[2][W];
+    __shared__ uint32_t smax[2][W];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    __syncthreads();   // the last row's reads are done
     if (lane == 0) {
-      ssum[wave] = sum;
-      smax[wave] = m;
+      ssum[turn][wave] = sum;
+      smax[turn][wave] = m;
     }
     __syncthreads();
-    sum = ssum[0];
-    m = smax[0];
+    sum = ssum[turn][0];
+    m = smax[turn][0];
 #pragma unroll
     for (int i = 1; i < W; ++i) {
-      sum += ssum[i];
-      m = max(m, smax[i]);
+      sum += ssum[turn][i];
+      m = max(m, smax[turn][i]);
     }
   }
 }
@@ -114,7 +118,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rows_kernel(RowArgs a) 
   using E = elem_t<T>;
   const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   const E *gain = static_cast<const E *>(a.gain);
-  for (int64_t row0 = (int64_t)blockIdx.x * RPB; row0 < a.rows; row0 += (int64_t)gridDim.x * RPB) {
+  int turn = 0;
+  for (int64_t row0 = (int64_t)blockIdx.x * RPB; row0 < a.rows; row0 += (int64_t)gridDim.x * RPB, turn ^= 1) {
     const bool live = row0 + sub < a.rows;   // (waves past the last row repeat it and store nothing)
     const int64_t row = live ? row0 + sub : a.rows - 1;
     const E *x = static_cast<const E *>(a.x) + row * a.cols;
@@ -171,7 +176,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rows_kernel(RowArgs a) 
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int i = 0; i < 8; ++i) m = max(m, mag(h[c][i]));
-    reduce_row<TPR>(sum, m);
+    reduce_row<TPR>(sum, m, turn);
     const RowScale k = row_scale(m);
     if (live) {
 #pragma unroll
@@ -198,7 +203,8 @@ template <int T, bool NORM>
 __global__ __launch_bounds__(1024) void long_rows_kernel(RowArgs a) {
   using E = elem_t<T>;
   const E *gain = static_cast<const E *>(a.gain);
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
     const E *x = static_cast<const E *>(a.x) + row * a.cols;
     const E *res = static_cast<const E *>(a.res) + row * a.cols;
     auto chunk = [&](int64_t col, float (&h)[8]) {
@@ -234,7 +240,7 @@ __global__ __launch_bounds__(1024) void long_rows_kernel(RowArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) m = max(m, mag(h[i]));
     }
-    reduce_row<1024>(sum, m);
+    reduce_row<1024>(sum, m, turn);
     const RowScale k = row_scale(m);
     for (int64_t col = 8 * (int64_t)threadIdx.x; col < a.pitch; col += 8 * 1024) {
       float h[8];
@@ -295,24 +301,51 @@ __device__ __forceinline__ void grad_h(const NormGradArgs &a, int64_t row, int64
 }
 
 template <int TPR>
-__device__ __forceinline__ float reduce_sum(float v) {
+__device__ __forceinline__ float reduce_sum(float v, int turn) {
   uint32_t none = 0;
-  reduce_row<TPR>(v, none);
+  reduce_row<TPR>(v, none, turn);
   return v;
 }
 
+// What a row's gradient reads, as it is stored: the next row's is on its way
+// while this one's is worked on (8192 x 4096 bf16 with dh: 80 us without, 50 with).
+template <int T, int C, bool SAVED>
+struct GradRow {
+  Raw8<T> dy[C], dh[C], h[SAVED ? 1 : C];
+  u32x2 q[SAVED ? C : 1];
+  float s[SAVED ? C : 1], rstd;
+};
+
+// (4 waves a SIMD: 128 registers)
 template <int T, int TPR, int C, bool SAVED>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(NormGradArgs a) {
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR, TPR == 1024 ? 4 : 2) void norm_grad_kernel(NormGradArgs a) {
   constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
   using E = elem_t<T>;
   const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   const E *gain = static_cast<const E *>(a.gain);
+  const E *dys = static_cast<const E *>(a.dy), *dhs = static_cast<const E *>(a.dh), *hs = static_cast<const E *>(a.h);
+  auto column = [&](int c) { return 8 * (int64_t)(c * TPR + t); };
+  auto fetch = [&](int64_t row, GradRow<T, C, SAVED> &r) {
+    r.rstd = a.rstd[row];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int64_t col = column(c);
+      r.dy[c] = raw8<T>(dys + row * a.cols + col, a.cols - col);
+      if (SAVED) {
+        const bool in = col < a.pitch;
+        r.q[c] = in ? *reinterpret_cast<const u32x2 *>(a.saved + row * a.pitch + col) : (u32x2){};
+        r.s[c] = in ? a.saved_scales[row * (a.pitch / kGroup) + col / kGroup] : 0.0f;
+      } else {
+        r.h[c] = raw8<T>(hs + row * a.cols + col, a.cols - col);
+      }
+      if (a.dh) r.dh[c] = raw8<T>(dhs + row * a.cols + col, a.cols - col);
+    }
+  };
   float g[C][8], dg[C][8];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const int64_t col = 8 * (int64_t)(c * TPR + t);
     if (gain) {
-      load8<T>(gain + col, a.cols - col, g[c]);
+      load8<T>(gain + column(c), a.cols - column(c), g[c]);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) g[c][i] = 1.0f;
@@ -321,50 +354,74 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(NormGr
     for (int i = 0; i < 8; ++i) dg[c][i] = 0.0f;
   }
   const float inv = 1.0f / (float)a.cols;
-  for (int64_t row0 = (int64_t)blockIdx.x * RPB; row0 < a.rows; row0 += (int64_t)gridDim.x * RPB) {
-    const bool live = row0 + sub < a.rows;
-    const int64_t row = live ? row0 + sub : a.rows - 1;
-    const float rstd = a.rstd[row];
-    float dy[C][8], xh[C][8], dot = 0.0f;
+  const int64_t stride = (int64_t)gridDim.x * RPB, first = (int64_t)blockIdx.x * RPB + sub;
+  constexpr bool kAhead = TPR < 1024;   // (at 1024 threads a second row would spill)
+  GradRow<T, C, SAVED> r, next;
+  if (kAhead) fetch(min(first, a.rows - 1), r);
+  int turn = 0;
+  // (waves past the last row repeat it and keep nothing)
+  for (int64_t row = first; row - sub < a.rows; row += stride, turn ^= 1) {
+    const bool live = row < a.rows;
+    if (!kAhead) fetch(min(row, a.rows - 1), r);
+    else if (row - sub + stride < a.rows) fetch(min(row + stride, a.rows - 1), next);
+    float xh[C][8], dot = 0.0f;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int64_t col = 8 * (int64_t)(c * TPR + t);
-      load8<T>(static_cast<const E *>(a.dy) + row * a.cols + col, a.cols - col, dy[c]);
-      grad_h<T, SAVED>(a, row, col, xh[c]);
-    }
+      float dy[8];
+      floats8<T>(r.dy[c], dy);
+      if (SAVED) {
+        codes8(r.q[c], xh[c]);
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+        for (int i = 0; i < 8; ++i) xh[c][i] *= r.s[c];   // (codes past the last column are zero, and so is dy there)
+      } else {
+        floats8<T>(r.h[c], xh[c]);
+      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        xh[c][i] *= rstd;
-        const float p = dy[c][i] * xh[c][i];
+        xh[c][i] *= r.rstd;
+        const float p = dy[i] * xh[c][i];
         if (live) dg[c][i] += p;
         dot += p * g[c][i];
       }
-    const float m = reduce_sum<TPR>(dot) * inv;
+    }
+    const float m = reduce_sum<TPR>(dot, turn) * inv;
     if (live) {
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        const int64_t col = 8 * (int64_t)(c * TPR + t);
-        float o[8];
+        float dy[8], o[8];
+        floats8<T>(r.dy[c], dy);
         if (a.dh) {
-          load8<T>(static_cast<const E *>(a.dh) + row * a.cols + col, a.cols - col, o);
+          floats8<T>(r.dh[c], o);
         } else {
 #pragma unroll
           for (int i = 0; i < 8; ++i) o[i] = 0.0f;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] += rstd * (dy[c][i] * g[c][i] - xh[c][i] * m);
-        store8<T>(static_cast<E *>(a.dx) + row * a.cols + col, a.cols - col, o);
+        for (int i = 0; i < 8; ++i) o[i] += r.rstd * (dy[i] * g[c][i] - xh[c][i] * m);
+        store8<T>(static_cast<E *>(a.dx) + row * a.cols + column(c), a.cols - column(c), o);
       }
     }
+    if (kAhead) r = next;
   }
   if (a.dgain) {
-    float *out = a.partial + ((int64_t)blockIdx.x * RPB + sub) * a.cols;
+    if constexpr (RPB > 1) {
+      // the waves' sums meet first
+      __shared__ float sums[RPB][C * TPR * 8];
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int64_t col = 8 * (int64_t)(c * TPR + t);
-      store8<FMM_F32>(out + col, a.cols - col, dg[c]);
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sums[sub][column(c) + i] = dg[c][i];
+      __syncthreads();
+      for (int64_t col = threadIdx.x; col < a.cols; col += 256) {
+        float v = sums[0][col];
+#pragma unroll
+        for (int i = 1; i < RPB; ++i) v += sums[i][col];
+        a.partial[(int64_t)blockIdx.x * a.cols + col] = v;
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        store8<FMM_F32>(a.partial + (int64_t)blockIdx.x * a.cols + column(c), a.cols - column(c), dg[c]);
     }
   }
 }
@@ -375,7 +432,8 @@ __global__ __launch_bounds__(1024) void long_norm_grad_kernel(NormGradArgs a) {
   using E = elem_t<T>;
   const E *gain = static_cast<const E *>(a.gain);
   const float inv = 1.0f / (float)a.cols;
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
     const float rstd = a.rstd[row];
     auto chunk = [&](int64_t col, float (&w)[8], float (&xh)[8]) {
       load8<T>(static_cast<const E *>(a.dy) + row * a.cols + col, a.cols - col, w);
@@ -396,7 +454,7 @@ __global__ __launch_bounds__(1024) void long_norm_grad_kernel(NormGradArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) dot += w[i] * xh[i];
     }
-    const float m = reduce_sum<1024>(dot) * inv;
+    const float m = reduce_sum<1024>(dot, turn) * inv;
     for (int64_t col = 8 * (int64_t)threadIdx.x; col < a.cols; col += 8 * 1024) {
       float w[8], xh[8], o[8];
       chunk(col, w, xh);
@@ -432,23 +490,23 @@ __global__ __launch_bounds__(256) void long_gain_grad_kernel(NormGradArgs a) {
   store8<FMM_F32>(a.partial + (int64_t)blockIdx.x * a.cols + col, a.cols - col, dg);
 }
 
-// out[j] = sum over n rows of partial[row][j], in ascending order within each
-// of eight interleaved sets of rows, which are then added in order
-__global__ __launch_bounds__(256) void sum_partials_kernel(const float *__restrict__ partial, float *__restrict__ out,
-                                                           int64_t n, int64_t cols) {
-  __shared__ float part[8][32];
+// out[j] = sum over n rows of partial[row][j]: ascending within each of 32
+// interleaved sets of rows, whose sums are then added in order
+__global__ __launch_bounds__(1024) void sum_partials_kernel(const float *__restrict__ partial, float *__restrict__ out,
+                                                            int64_t n, int64_t cols) {
+  __shared__ float part[32][33];
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
   const int64_t col = 32 * (int64_t)blockIdx.x + x;
   float s = 0.0f;
   if (col < cols) {
-#pragma unroll 4
-    for (int64_t r = y; r < n; r += 8) s += partial[r * cols + col];
+#pragma unroll 8
+    for (int64_t r = y; r < n; r += 32) s += partial[r * cols + col];
   }
   part[y][x] = s;
   __syncthreads();
   if (y == 0 && col < cols) {
 #pragma unroll
-    for (int i = 1; i < 8; ++i) s += part[i][x];
+    for (int i = 1; i < 32; ++i) s += part[i][x];
     out[col] = s;
   }
 }
@@ -464,10 +522,12 @@ Geometry geometry(int64_t rows, int64_t cols) {
   if (cols > kMaxHeldCols) return {0, 0};
   const bool few = rows <= kFewRows;
   if (cols <= 512) return {64, 1};
-  if (cols <= 2048) return few ? Geometry{256, 1} : Geometry{64, 4};
+  if (cols <= 1024 && !few) return {64, 2};
+  if (cols <= 2048) return {256, 1};
   if (cols <= 8192 && few) return {1024, 1};
   if (cols <= 4096) return {256, 2};
   if (cols <= 8192) return {256, 4};
+  if (cols <= 16384) return {1024, 2};
   return {1024, 4};
 }
 
@@ -478,11 +538,12 @@ void launch_rows(const RowArgs &a, hipStream_t s) {
   const dim3 grid((unsigned)std::min<int64_t>((a.rows + rpb - 1) / rpb, kMaxBlocks));
   if (g.tpr == 0) long_rows_kernel<T, NORM><<<grid, 1024, 0, s>>>(a);
   else if (g.tpr == 64 && g.c == 1) rows_kernel<T, 64, 1, NORM><<<grid, 256, 0, s>>>(a);
-  else if (g.tpr == 64) rows_kernel<T, 64, 4, NORM><<<grid, 256, 0, s>>>(a);
+  else if (g.tpr == 64) rows_kernel<T, 64, 2, NORM><<<grid, 256, 0, s>>>(a);
   else if (g.tpr == 256 && g.c == 1) rows_kernel<T, 256, 1, NORM><<<grid, 256, 0, s>>>(a);
   else if (g.tpr == 256 && g.c == 2) rows_kernel<T, 256, 2, NORM><<<grid, 256, 0, s>>>(a);
   else if (g.tpr == 256) rows_kernel<T, 256, 4, NORM><<<grid, 256, 0, s>>>(a);
   else if (g.c == 1) rows_kernel<T, 1024, 1, NORM><<<grid, 1024, 0, s>>>(a);
+  else if (g.c == 2) rows_kernel<T, 1024, 2, NORM><<<grid, 1024, 0, s>>>(a);
   else rows_kernel<T, 1024, 4, NORM><<<grid, 1024, 0, s>>>(a);
 }
 
@@ -495,19 +556,32 @@ int launch_rows_typed(int type, const RowArgs &a, void *stream) {
   return hipGetLastError();
 }
 
-// the workgroups that share the rows of a gradient
+// A gradient holds more a thread, so at most two chunks each; rows of more than
+// 16384 columns are read twice.
+Geometry grad_geometry(int64_t cols) {
+  if (cols <= 512) return {64, 1};
+  if (cols <= 1024) return {64, 2};
+  if (cols <= 2048) return {256, 1};
+  if (cols <= 4096) return {256, 2};
+  if (cols <= 8192) return {512, 2};
+  if (cols <= 16384) return {1024, 2};
+  return {0, 0};
+}
+// The workgroups that share the rows: two of 256 threads a compute unit.  More
+// leave more partial sums (8192 x 4096 bf16: 53 us; twice as many 59, half 79).
 int64_t grad_blocks(int64_t rows, int64_t cols) {
-  const Geometry g = geometry(rows, cols);
+  const Geometry g = grad_geometry(cols);
   const int64_t rpb = g.tpr == 64 ? 4 : 1;
-  const int64_t most = g.tpr == 1024 ? 256 : g.tpr == 0 ? 64 : 512;
+  const int64_t most = g.tpr == 0 ? 64 : 512 * 256 / std::max(g.tpr, 256);
   return std::max<int64_t>(1, std::min((rows + rpb - 1) / rpb, most));
 }
 
 template <int T, bool SAVED>
-void launch_grad(const NormGradArgs &a, hipStream_t s) {
-  const Geometry g = geometry(a.rows, a.cols);
+void launch_grad(NormGradArgs a, hipStream_t s) {
+  const Geometry g = grad_geometry(a.cols);
   const int64_t blocks = a.rows > 0 ? grad_blocks(a.rows, a.cols) : 0;
   const dim3 grid((unsigned)blocks);
+  if (blocks == 1) a.partial = a.dgain;   // one workgroup's sums are all of them
   if (blocks == 0) {
     // no rows: the gain's sums are empty
   } else if (g.tpr == 0) {
@@ -516,16 +590,13 @@ void launch_grad(const NormGradArgs &a, hipStream_t s) {
     if (a.dgain)
       long_gain_grad_kernel<T, SAVED><<<dim3((unsigned)blocks, (unsigned)((a.cols + 2047) / 2048)), 256, 0, s>>>(a);
   } else if (g.tpr == 64 && g.c == 1) norm_grad_kernel<T, 64, 1, SAVED><<<grid, 256, 0, s>>>(a);
-  else if (g.tpr == 64) norm_grad_kernel<T, 64, 4, SAVED><<<grid, 256, 0, s>>>(a);
+  else if (g.tpr == 64) norm_grad_kernel<T, 64, 2, SAVED><<<grid, 256, 0, s>>>(a);
   else if (g.tpr == 256 && g.c == 1) norm_grad_kernel<T, 256, 1, SAVED><<<grid, 256, 0, s>>>(a);
-  else if (g.tpr == 256 && g.c == 2) norm_grad_kernel<T, 256, 2, SAVED><<<grid, 256, 0, s>>>(a);
-  else if (g.tpr == 256) norm_grad_kernel<T, 256, 4, SAVED><<<grid, 256, 0, s>>>(a);
-  else if (g.c == 1) norm_grad_kernel<T, 1024, 1, SAVED><<<grid, 1024, 0, s>>>(a);
-  else norm_grad_kernel<T, 1024, 4, SAVED><<<grid, 1024, 0, s>>>(a);
-  if (a.dgain) {
-    const int64_t n = blocks * (g.tpr == 64 ? 4 : 1);
-    sum_partials_kernel<<<dim3((unsigned)((a.cols + 31) / 32)), 256, 0, s>>>(a.partial, a.dgain, n, a.cols);
-  }
+  else if (g.tpr == 256) norm_grad_kernel<T, 256, 2, SAVED><<<grid, 256, 0, s>>>(a);
+  else if (g.tpr == 512) norm_grad_kernel<T, 512, 2, SAVED><<<grid, 512, 0, s>>>(a);
+  else norm_grad_kernel<T, 1024, 2, SAVED><<<grid, 1024, 0, s>>>(a);
+  if (a.dgain && blocks != 1)
+    sum_partials_kernel<<<dim3((unsigned)((a.cols + 31) / 32)), 1024, 0, s>>>(a.partial, a.dgain, blocks, a.cols);
 }
 
 template <int T>
@@ -550,7 +621,7 @@ int launch_dequantize(int type, const DequantArgs &a, void *stream) {
 }
 
 int64_t norm_grad_partials(int64_t rows, int64_t cols) {
-  return grad_blocks(rows, cols) * (geometry(rows, cols).tpr == 64 ? 4 : 1);
+  return grad_blocks(rows, cols);
 }
 
 int launch_rmsnorm_grad(int type, const NormGradArgs &a, void *stream) {

@@ -23,9 +23,6 @@ typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
 typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
 typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
 
-template <int T>
-__device__ __forceinline__ float to_float(elem_t<T> v) { return (float)v; }
-
 // two floats -> the bits of two 16-bit elements (round to nearest even)
 template <int T>
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -46,26 +43,49 @@ __device__ __forceinline__ void unpack2(uint32_t w, float &a, float &b) {
   }
 }
 
-// v[0..7] = p[0..7], with zeros from element n on (n may be <= 0)
+// eight elements as they are stored
 template <int T>
-__device__ __forceinline__ void load8(const elem_t<T> *p, int64_t n, float (&v)[8]) {
+struct Raw8 {
+  u32x4 w[T == FMM_F32 ? 2 : 1];
+};
+
+// p[0..7], with zeros from element n on (n may be <= 0)
+template <int T>
+__device__ __forceinline__ Raw8<T> raw8(const elem_t<T> *p, int64_t n) {
+  Raw8<T> r;
   if (n >= 8) {
     if constexpr (T == FMM_F32) {
-      const u32x4 a = *reinterpret_cast<const u32x4_a4 *>(p), b = *reinterpret_cast<const u32x4_a4 *>(p + 4);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[i] = __uint_as_float(a[i]);
-        v[4 + i] = __uint_as_float(b[i]);
-      }
+      r.w[0] = *reinterpret_cast<const u32x4_a4 *>(p);
+      r.w[1] = *reinterpret_cast<const u32x4_a4 *>(p + 4);
     } else {
-      const u32x4 a = *reinterpret_cast<const u32x4_a2 *>(p);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) unpack2<T>(a[i], v[2 * i], v[2 * i + 1]);
+      r.w[0] = *reinterpret_cast<const u32x4_a2 *>(p);
     }
+  } else if constexpr (T == FMM_F32) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.w[i / 4][i % 4] = i < n ? __float_as_uint(p[i]) : 0u;
+  } else {
+    const uint16_t *q = reinterpret_cast<const uint16_t *>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      r.w[0][i] = (uint32_t)(2 * i < n ? q[2 * i] : 0) | (uint32_t)(2 * i + 1 < n ? q[2 * i + 1] : 0) << 16;
+  }
+  return r;
+}
+
+template <int T>
+__device__ __forceinline__ void floats8(const Raw8<T> &r, float (&v)[8]) {
+  if constexpr (T == FMM_F32) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r.w[i / 4][i % 4]);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? to_float<T>(p[i]) : 0.0f;
+    for (int i = 0; i < 4; ++i) unpack2<T>(r.w[0][i], v[2 * i], v[2 * i + 1]);
   }
+}
+
+template <int T>
+__device__ __forceinline__ void load8(const elem_t<T> *p, int64_t n, float (&v)[8]) {
+  floats8<T>(raw8<T>(p, n), v);
 }
 
 template <int T>
