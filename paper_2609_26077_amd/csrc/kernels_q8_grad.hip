@@ -11,12 +11,13 @@
 //     or three bfloat16 parts (16 and 24 significant bits) along a longer
 //     contracted axis, the codes staying exact.
 //
-// Two launches.  The first lays the operands out along the contracted axes
+// Two launches, or three.  The first lays the operands out along the contracted axes
 // (transposes through LDS, converted on the way, padded with zeros to the
 // product's 64-position step) and leaves dY's column sums by 64-row tiles; it
 // moves about 14 bytes for each element of dY and the codes, a tenth of the
 // products' time.  The second runs both products' tiles and adds up the column
-// sums.
+// sums.  Where a product has few tiles and a long axis, its tiles' axis is split
+// into runs, and the third adds the runs' sums.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -182,6 +183,26 @@ __global__ __launch_bounds__(T::kThreads, 2) void grad_kernel(GradGemms g) {
   g.dbias[n] = s;
 }
 
+// The sums of a split product's runs, added in order, eight elements a thread.
+template <int OUT>
+__device__ __forceinline__ void add_runs(const GemmProblem &p, int64_t at) {
+  const int64_t n = (int64_t)p.M * p.N;
+  float v[8], w[8];
+  load8<FMM_F32>(p.partial + at, n - at, v);
+  for (int s = 1; s < p.splits; ++s) {
+    load8<FMM_F32>(p.partial + s * n + at, n - at, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += w[i];
+  }
+  store8<OUT>(static_cast<elem_t<OUT> *>(p.C) + at, n - at, v);
+}
+template <int OUT>
+__global__ __launch_bounds__(256) void add_runs_kernel(GradGemms g, int64_t chunks0, int64_t chunks) {
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (e < chunks0) add_runs<OUT>(g.p[0], 8 * e);
+  else if (e < chunks) add_runs<OUT>(g.p[1], 8 * (e - chunks0));
+}
+
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 struct Layout {
@@ -208,45 +229,68 @@ Layout layout_of(int type, int64_t M, int64_t N, int64_t K) {
   return l;
 }
 
+// How the products are cut: the tile that both take, and the runs that each
+// one's contracted axis is split into.
+struct Cut {
+  int tile;        // 0: 64, 1: 128, 2: 256
+  int splits[2];
+};
+
+// t = start + max(chain steps of a run, work steps tiles / CUs) us, as for the
+// int8 product, whose fits of these three tiles these are (a step moves and
+// multiplies as much); runs cost a launch and the traffic of their sums besides.
+// Without them few tiles with a long axis leave most of the chip idle: 8192 tokens
+// of 512 x 512 channels 42 -> 32 us, of 1024 x 1024 87 -> 65.
+Cut cut_of(const int64_t (&m)[2], const int64_t (&n)[2], const int64_t (&steps)[2], int ncu) {
+  constexpr int kEdge[3] = {64, 128, 256};
+  constexpr double kStart[3] = {3.2, 4.5, 7.5}, kChain[3] = {0.20, 0.47, 1.05}, kWork[3] = {0.29, 0.76, 2.45};
+  constexpr double kMostSums = 1 << 24;   // floats of sums: 64 MB
+  Cut best = {};
+  double least = 1e300;
+  for (int i = 0; i < 3; ++i) {
+    double tiles[2];
+    for (int k = 0; k < 2; ++k)
+      tiles[k] = (double)((m[k] + kEdge[i] - 1) / kEdge[i]) * (double)((n[k] + kEdge[i] - 1) / kEdge[i]);
+    const double work = kWork[i] * (steps[0] * tiles[0] + steps[1] * tiles[1]) / ncu;
+    for (int s0 = 1; s0 <= 16; s0 *= 2)
+      for (int s1 = 1; s1 <= 16; s1 *= 2) {
+        if ((s0 > 1 && s0 * 4 > steps[0]) || (s1 > 1 && s1 * 4 > steps[1])) continue;
+        const double sums = (s0 > 1 ? (double)m[0] * n[0] * s0 : 0) + (s1 > 1 ? (double)m[1] * n[1] * s1 : 0);
+        if (sums > kMostSums) continue;
+        const double chain = kChain[i] * std::max((steps[0] + s0 - 1) / s0, (steps[1] + s1 - 1) / s1);
+        const double t = kStart[i] + std::max(chain, work) + (sums > 0 ? 3.0 + sums * 8 / 4e6 : 0);
+        if (t < least) {
+          least = t;
+          best = {i, {s0, s1}};
+        }
+      }
+  }
+  return best;
+}
+
+// (nothing is wanted of a product with m = 0)
+Cut cut_of(int type, int64_t M, int64_t N, int64_t K, bool dx, bool dw, int ncu) {
+  const int64_t parts = type == FMM_BF16 ? 1 : type == FMM_F16 ? 2 : 3;
+  return cut_of({dx ? M : 0, dw ? N : 0}, {K, K}, {parts * ((N + kPos - 1) / kPos), parts * ((M + kPos - 1) / kPos)}, ncu);
+}
+
 template <int T, class TL>
 void launch_gemms(GradGemms g, const GradArgs &a, hipStream_t s) {
   for (int i = 0; i < 2; ++i) {
     g.p[i].tiles_m = (g.p[i].M + TL::TM - 1) / TL::TM;
     g.p[i].tiles_n = (g.p[i].N + TL::TN - 1) / TL::TN;
   }
-  const int64_t dx = a.dx ? (int64_t)g.p[0].tiles_m * g.p[0].tiles_n : 0;
-  const int64_t dw = a.dw ? (int64_t)g.p[1].tiles_m * g.p[1].tiles_n : 0;
+  const int64_t dx = a.dx ? (int64_t)g.p[0].tiles_m * g.p[0].tiles_n * g.p[0].splits : 0;
+  const int64_t dw = a.dw ? (int64_t)g.p[1].tiles_m * g.p[1].tiles_n * g.p[1].splits : 0;
   const int64_t db = a.dbias ? (a.N + TL::kThreads - 1) / TL::kThreads : 0;
   g.items0 = (int)dx;
   g.items = (int)(dx + dw);
   if (dx + dw + db > 0) grad_kernel<TL, T><<<dim3((unsigned)(dx + dw + db)), TL::kThreads, 0, s>>>(g);
-}
-
-// The tile that both products take: t = start + max(chain steps, work steps
-// tiles / CUs) us, as for the int8 product, whose fits of these three these are
-// (a step moves and multiplies as much).
-int pick(const GradGemms &q, const GradArgs &a, int ncu) {
-  constexpr int kEdge[3] = {64, 128, 256};
-  constexpr double kStart[3] = {3.2, 4.5, 7.5}, kChain[3] = {0.20, 0.47, 1.05}, kWork[3] = {0.29, 0.76, 2.45};
-  int best = 0;
-  double least = 1e300;
-  for (int i = 0; i < 3; ++i) {
-    double chain = 0, work = 0;
-    for (int k = 0; k < 2; ++k) {
-      const GemmProblem &p = q.p[k];
-      if (!(k == 0 ? a.dx : a.dw)) continue;
-      const double steps = (double)p.steps * p.parts;
-      const double tiles = (double)((p.M + kEdge[i] - 1) / kEdge[i]) * ((p.N + kEdge[i] - 1) / kEdge[i]);
-      chain = std::max(chain, steps);
-      work += steps * tiles;
-    }
-    const double t = kStart[i] + std::max(kChain[i] * chain, kWork[i] * work / ncu);
-    if (t < least) {
-      best = i;
-      least = t;
-    }
-  }
-  return best;
+  int64_t chunks[2];
+  for (int i = 0; i < 2; ++i)
+    chunks[i] = (i ? dw : dx) > 0 && g.p[i].splits > 1 ? ((int64_t)g.p[i].M * g.p[i].N + 7) / 8 : 0;
+  const int64_t all = chunks[0] + chunks[1];
+  if (all > 0) add_runs_kernel<T><<<dim3((unsigned)((all + 255) / 256)), 256, 0, s>>>(g, chunks[0], all);
 }
 
 template <int T>
@@ -281,7 +325,12 @@ int launch(const GradArgs &a, int ncu, hipStream_t s) {
   w.B = reinterpret_cast<const uint8_t *>(g.at); w.pitch_b = 2 * g.Mp;
   w.C = a.dw; w.M = (int)a.N; w.N = (int)a.K; w.steps = g.bm; w.parts = P;
   q.colsum = g.colsum; q.dbias = a.dbias; q.N = a.N; q.tiles = g.bm;
-  switch (pick(q, a, ncu)) {
+  const Cut cut = cut_of(T, a.M, a.N, a.K, a.dx, a.dw, ncu);
+  x.splits = cut.splits[0];
+  w.splits = cut.splits[1];
+  x.partial = reinterpret_cast<float *>(a.ws + l.total);
+  w.partial = x.partial + (x.splits > 1 ? (int64_t)x.splits * a.M * a.K : 0);
+  switch (cut.tile) {
     case 0: launch_gemms<T, Tile64>(q, a, s); break;
     case 1: launch_gemms<T, Tile128>(q, a, s); break;
     default: launch_gemms<T, Tile256>(q, a, s);
@@ -291,7 +340,18 @@ int launch(const GradArgs &a, int ncu, hipStream_t s) {
 
 }  // namespace
 
-size_t grad_scratch(int type, int64_t M, int64_t N, int64_t K) { return layout_of(type, M, N, K).total; }
+// (what is wanted is not known here: the most that any choice of it takes)
+size_t grad_scratch(int type, int64_t M, int64_t N, int64_t K, int ncu) {
+  size_t sums = 0;
+  for (int want = 1; want < 4; ++want) {
+    const Cut c = cut_of(type, M, N, K, want & 1, want & 2, ncu);
+    size_t n = 0;
+    if ((want & 1) && c.splits[0] > 1) n += sizeof(float) * c.splits[0] * M * K;
+    if ((want & 2) && c.splits[1] > 1) n += sizeof(float) * c.splits[1] * N * K;
+    sums = std::max(sums, n);
+  }
+  return layout_of(type, M, N, K).total + align256(sums);
+}
 
 int launch_linear_grad(int type, const GradArgs &a, int ncu, void *stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);

@@ -176,6 +176,7 @@ template <class T, int OUT>
 void launch_tiles(GemmProblem g, hipStream_t s) {
   g.tiles_m = (g.M + T::TM - 1) / T::TM;
   g.tiles_n = (g.N + T::TN - 1) / T::TN;
+  g.splits = 1;
   matmul_kernel<T, OUT><<<dim3((unsigned)(g.tiles_m * g.tiles_n)), T::kThreads, 0, s>>>(g);
 }
 

@@ -150,7 +150,7 @@ int fmm_q8_linear_backward_scratch_size(const fmm_q8_desc *desc, size_t *bytes) 
   if (!bytes) return FMM_ERR_ARG;
   const int st = check_grad(desc);
   if (st != FMM_OK) return st;
-  *bytes = grad_scratch(desc->type, desc->M, desc->N, desc->K);
+  *bytes = grad_scratch(desc->type, desc->M, desc->N, desc->K, fmm::compute_units());
   return FMM_OK;
 }
 
@@ -172,10 +172,11 @@ int fmm_q8_linear_backward(const fmm_q8_desc *desc, const void *dDy, const int8_
     if (dDx && (!good(dW, 16) || !good(dSw, 4))) return FMM_ERR_ARG;
     if (dDw && (!good(dA, 16) || !good(dSa, 4))) return FMM_ERR_ARG;
   }
-  const int ws = check_scratch(dScratch, scratch_bytes, grad_scratch(desc->type, M, N, K), 256);
+  const int ncu = fmm::compute_units();
+  const int ws = check_scratch(dScratch, scratch_bytes, grad_scratch(desc->type, M, N, K, ncu), 256);
   if (ws != FMM_OK) return ws;
   GradArgs a = {dDy, dA, dW, dSa, dSw, dDx, dDw, dDbias, static_cast<uint8_t *>(dScratch), M, N, K};
-  return fmm::hip_status(launch_linear_grad(desc->type, a, fmm::compute_units(), stream));
+  return fmm::hip_status(launch_linear_grad(desc->type, a, ncu, stream));
 }
 
 }  // extern "C"

@@ -70,6 +70,8 @@ struct GemmProblem {
   int M, N;
   int steps, parts;                 // 128-byte steps of a plane, planes
   int tiles_m, tiles_n;
+  int splits;                       // the contracted axis in this many runs of steps;
+  float *partial;                   // if more than one, their sums go here: [splits][M][N] (bf16 only)
 };
 
 int launch_matmul(int type, const GemmProblem &p, int ncu, void *stream);
@@ -83,7 +85,7 @@ struct GradArgs {
   uint8_t *ws;
   int64_t M, N, K;
 };
-size_t grad_scratch(int type, int64_t M, int64_t N, int64_t K);
+size_t grad_scratch(int type, int64_t M, int64_t N, int64_t K, int ncu);
 int launch_linear_grad(int type, const GradArgs &a, int ncu, void *stream);
 
 }  // namespace q8

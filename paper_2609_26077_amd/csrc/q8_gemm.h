@@ -79,17 +79,20 @@ typedef Tile<64, 64, 2, 2, 4> Tile64;      // two
 
 __device__ __forceinline__ int swz128(int row) { return (row & 7) ^ ((row >> 3) & 1); }
 
-// Which tile item `id` of a problem is.  Workgroups are dispatched
+// Which tile, and which run of steps, item `id` of a problem is.  Workgroups are dispatched
 // round-robin over the eight XCDs, each with an L2 of its own: the ids of one
 // XCD get a contiguous range of items, and tiles run in groups of GM tile rows,
 // so that the workgroups that share an L2 share rows of A and B.
 template <int GM>
-__device__ __forceinline__ void item_of(int id, int items, int tiles_m, int tiles_n, int &tm, int &tn) {
+__device__ __forceinline__ void item_of(int id, int items, int tiles_m, int tiles_n, int &tm, int &tn,
+                                        int &split) {
   if (items >= 8) {
     // XCD x takes items base(x) .. : the first `extra` XCDs one more than the others
     const int per = items / 8, extra = items - 8 * per, x = id & 7;
     id = x * per + min(x, extra) + (id >> 3);
   }
+  split = id / (tiles_m * tiles_n);
+  id -= split * tiles_m * tiles_n;
   const int per_group = GM * tiles_n;
   const int group = id / per_group;
   const int first = group * GM;
@@ -119,8 +122,8 @@ __device__ __forceinline__ void load4(const float *p, int n, float (&v)[4]) {
 // lane (5 us).  16-byte chunk c of a row sits at chunk c ^ (row mod the row's
 // chunks).  FULL: the whole wave tile lies inside C.
 template <class E, class T, int OUT, bool FULL>
-__device__ __forceinline__ void store_tile(const GemmProblem &g, typename E::acc (&acc)[T::MI][T::NI], int m0, int n0,
-                                           uint8_t *lds) {
+__device__ __forceinline__ void store_tile(const GemmProblem &g, void *C, typename E::acc (&acc)[T::MI][T::NI], int m0,
+                                           int n0, uint8_t *lds) {
   constexpr int B = OUT == FMM_F32 ? 4 : 2, EPC = 16 / B;          // bytes of an element, elements of a chunk
   constexpr int CH = T::NI * 32 / EPC;                             // chunks of a row
   constexpr int kRow = CH * 16;
@@ -167,7 +170,7 @@ __device__ __forceinline__ void store_tile(const GemmProblem &g, typename E::acc
       }
     const int lrow = lane / CH, c = lane % CH;
     const int n = n0 + c * EPC;
-    elem_t<OUT> *out = static_cast<elem_t<OUT> *>(g.C) + (int64_t)(m0 + 32 * pass * MP + lrow) * g.N + n;
+    elem_t<OUT> *out = static_cast<elem_t<OUT> *>(C) + (int64_t)(m0 + 32 * pass * MP + lrow) * g.N + n;
 #pragma unroll
     for (int e = 0; e < MP * 32 * CH / 64; ++e) {
       const int row = (64 / CH) * e + lrow;
@@ -199,8 +202,8 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem &g, int id, uint4 *l
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = wave / T::WN, wn = wave % T::WN;
   const int r32 = lane & 31, h = lane >> 5;
-  int tm, tn;
-  item_of<T::TM == 256 ? 4 : 8>(id, g.tiles_m * g.tiles_n, g.tiles_m, g.tiles_n, tm, tn);
+  int tm, tn, split;
+  item_of<T::TM == 256 ? 4 : 8>(id, g.tiles_m * g.tiles_n * g.splits, g.tiles_m, g.tiles_n, tm, tn, split);
   const int m0 = tm * T::TM, n0 = tn * T::TN;
 
   // what this wave transfers of each side: rows 8 (wave J + j) + lane / 8, j < J;
@@ -217,7 +220,17 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem &g, int id, uint4 *l
   const uint8_t *pa = g.A + (int64_t)m0 * g.pitch_a, *pb = g.B + (int64_t)n0 * g.pitch_b;   // the next step's
   const uint8_t *const pb0 = pb;
   const int64_t next_part = g.part_a - (int64_t)g.steps * kStep;
-  int ka = 0, kb = 0;                                 // its place in its plane
+  // this run of steps, and the place of its first in its plane
+  int ns = g.steps * g.parts, ka = 0;
+  if (g.splits > 1) {
+    const int first = (int)((int64_t)ns * split / g.splits);
+    ns = (int)((int64_t)ns * (split + 1) / g.splits) - first;
+    const int part = first / g.steps;
+    ka = first - part * g.steps;
+    pa += part * g.part_a + (int64_t)ka * kStep;
+    pb += (int64_t)ka * kStep;
+  }
+  int kb = ka;
   const uint32_t base = dma::lds_addr(lds_raw) + wave * J * 1024;
   uint32_t wa = 0, wb = T::kHalf, ra = 0, rb = T::kHalf;   // half-slots to fill and to read next, in bytes
   auto turn = [](uint32_t &x) {
@@ -295,7 +308,6 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem &g, int id, uint4 *l
     asm volatile("" ::: "memory");
   };
 
-  const int ns = g.steps * g.parts;
   if (ns > 0) {
 #pragma unroll
     for (int s = 0; s < T::H - 1; ++s)
@@ -393,8 +405,17 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem &g, int id, uint4 *l
   __syncthreads();
   const int mw = m0 + wm * T::MI * 32, nw = n0 + wn * T::NI * 32;
   uint8_t *share = reinterpret_cast<uint8_t *>(lds_raw) + wave * (T::kLds / T::kWaves);
-  if (mw + T::MI * 32 <= g.M && nw + T::NI * 32 <= g.N) store_tile<E, T, OUT, true>(g, acc, mw, nw, share);
-  else store_tile<E, T, OUT, false>(g, acc, mw, nw, share);
+  const bool full = mw + T::MI * 32 <= g.M && nw + T::NI * 32 <= g.N;
+  if constexpr (!E::kScaled) {
+    if (g.splits > 1) {
+      float *sums = g.partial + (int64_t)split * g.M * g.N;
+      if (full) store_tile<E, T, FMM_F32, true>(g, sums, acc, mw, nw, share);
+      else store_tile<E, T, FMM_F32, false>(g, sums, acc, mw, nw, share);
+      return;
+    }
+  }
+  if (full) store_tile<E, T, OUT, true>(g, g.C, acc, mw, nw, share);
+  else store_tile<E, T, OUT, false>(g, g.C, acc, mw, nw, share);
 }
 
 }  // namespace q8
