@@ -11,7 +11,8 @@ Codes are int8 [rows][pitch(cols)], zero past cols; scales are float32 [rows],
 or [rows][pitch / 128] for a checkpoint.  Allocation, checks and marshalling
 only: the arithmetic happens in the library's HIP kernels.  Every call runs on
 `stream` (default: torch's current one) and allocates its outputs there; an
-object's workspace is used by one call at a time.
+object's workspace, which its first backward call allocates, belongs to the
+calls of one stream.
 """
 from __future__ import annotations
 
@@ -90,13 +91,21 @@ def _switched(index, stream):
                 yield stream.cuda_stream
 
 
-def _run(device, stream, call):
-    """call(stream handle), on the device and the stream."""
+def _run(device, stream, call, *tensors):
+    """call(stream handle), on the device and the stream.  A stream that the
+    caller names may not be the one the inputs were allocated on: the allocator
+    is told, so that it does not hand out their memory before the call is done."""
     index = device.index
     if stream is None and torch.cuda.current_device() == index:
         return call(_raw_stream(index))
     with _switched(index, stream) as handle:
-        return call(handle)
+        out = call(handle)
+        if stream is not None:
+            used = torch.cuda.current_stream(index)
+            for x in tensors:
+                if x is not None:
+                    x.record_stream(used)
+    return out
 
 
 def _matrix(x, name):
@@ -125,7 +134,7 @@ def quantize(x, codes=None, scales=None, stream=None):
         _check(_lib.fmm_q8_quantize(t, rows, cols, x.data_ptr(), q.data_ptr(), s.data_ptr(), handle), "fmm_q8_quantize")
         return q, s
 
-    return _run(dev, stream, call)
+    return _run(dev, stream, call, x, codes, scales)
 
 
 def dequantize(codes, scales, cols, dtype=torch.float32, out=None, stream=None):
@@ -149,7 +158,7 @@ def dequantize(codes, scales, cols, dtype=torch.float32, out=None, stream=None):
                "fmm_q8_dequantize")
         return o
 
-    return _run(dev, stream, call)
+    return _run(dev, stream, call, codes, scales, out)
 
 
 class NormOutput(NamedTuple):
@@ -201,7 +210,7 @@ class RMSNormQ8:
                                        _ptr(saved), _ptr(saved_scales), rstd.data_ptr(), handle), "fmm_rmsnorm_q8")
             return NormOutput(h, codes, scales, rstd, saved, saved_scales)
 
-        return _run(dev, stream, call)
+        return _run(dev, stream, call, x, residual, gain)
 
     def backward(self, dy, rstd, gain=None, h=None, saved=None, dh=None, need_gain=True, stream=None):
         """(gradient of x and of the residual, gradient of the gain or None) from
@@ -238,7 +247,7 @@ class RMSNormQ8:
                    "fmm_rmsnorm_q8_backward")
             return dx, dgain
 
-        return _run(dev, stream, call)
+        return _run(dev, stream, call, dy, rstd, gain, h, codes, scales, dh)
 
 
 class LinearQ8:
@@ -274,7 +283,7 @@ class LinearQ8:
                                       out.data_ptr(), handle), "fmm_q8_matmul")
             return out
 
-        return _run(dev, stream, call)
+        return _run(dev, stream, call, a, sa, w, sw, bias, C)
 
     def backward(self, dy, a, sa, w, sw, need_x=True, need_w=True, bias=False, stream=None):
         """(dX, dW, dbias) from dy (M x N) and the 8-bit operands; None for what
@@ -298,4 +307,4 @@ class LinearQ8:
                    "fmm_q8_linear_backward")
             return dx, dw, dbias
 
-        return _run(dev, stream, call)
+        return _run(dev, stream, call, dy, a, sa, w, sw)

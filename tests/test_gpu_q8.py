@@ -483,3 +483,66 @@ def test_graph_replays(torch, q8, M, N, K):
         want = step(*args)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want)), k
+
+
+# ---- offsets beyond 32 bits ----------------------------------------------------------------
+def test_rows_beyond_32_bit_offsets(torch, q8):
+    """More than 2^31 elements, and more than 2^32 bytes: the last rows are as if they were alone."""
+    rows, cols = 70000, 32768
+    x = torch.zeros((rows, cols), dtype=torch.bfloat16, device="cuda")
+    tail = randn(torch, 4, 3, cols, t="bf16")
+    x[-3:] = tail
+    q, s = q8.quantize(x)
+    want_q, want_s = q8.quantize(tail)
+    assert torch.equal(q[-3:], want_q) and torch.equal(s[-3:], want_s)
+    assert not q[:-3].any() and (s[:-3] == s[0]).all()
+    del q, s
+    n, alone = q8.RMSNormQ8(rows, cols, x.dtype), q8.RMSNormQ8(3, cols, x.dtype)
+    o, w = n.forward(x, checkpoint=True), alone.forward(tail, checkpoint=True)
+    for got, want in zip(o[1:], w[1:]):
+        assert torch.equal(got[-3:], want)
+    dx, dgain = n.backward(x, o.rstd, saved=(o.saved_codes, o.saved_scales))
+    want_dx, want_g = alone.backward(tail, w.rstd, saved=(w.saved_codes, w.saved_scales))
+    assert torch.equal(dx[-3:], want_dx) and not dx[:-3].any()
+    within(f64(dgain), f64(want_g), 8 * U * np.abs(f64(want_g)) + 1e-6, "dgain")
+    v = q8.dequantize(o.codes, o.scales, cols, torch.bfloat16)
+    assert torch.equal(v[-3:], q8.dequantize(w.codes, w.scales, cols, torch.bfloat16))
+
+
+@pytest.mark.parametrize("M,N,K", [(300000, 8192, 130), (8193, 270000, 64)])
+def test_matmul_beyond_32_bit_offsets(torch, q8, M, N, K):
+    a, sa = torch.zeros((M, ref.pitch(K)), dtype=torch.int8, device="cuda"), torch.ones(M, device="cuda")
+    w, sw = torch.zeros((N, ref.pitch(K)), dtype=torch.int8, device="cuda"), torch.ones(N, device="cuda")
+    ta, _ = codes(torch, 1, 300, K)
+    tw, _ = codes(torch, 2, 300, K)
+    a[-300:], w[-300:] = ta, tw
+    C = q8.LinearQ8(M, N, K, torch.bfloat16).matmul(a, sa, w, sw)
+    want = q8.LinearQ8(300, 300, K, torch.bfloat16).matmul(ta, sa[:300].clone(), tw, sw[:300].clone())
+    assert torch.equal(C[-300:, -300:], want)
+    assert not C[:-300].any() and not C[:, :-300].any()
+
+
+# ---- the example -----------------------------------------------------------------------------
+def test_feedforward_example(torch, q8):
+    """It learns, and a token's output is that of the same layer evaluated in
+    binary64 on the values its codes stand for, but for the roundings of u and
+    silu(u): silu's slope is at most 1.1 and a code's half step 1/254 of its row's
+    largest magnitude."""
+    from examples.q8_feedforward import FeedForward, train
+    width, hidden = 256, 520
+    layer = FeedForward(width, hidden)
+    losses, x = train(layer, 300, 25)
+    assert losses[-1] < 0.5 * losses[0] and np.isfinite(losses).all()
+    token = x[:1]
+    out, h, kept = layer.forward(token, torch.zeros_like(token))
+    assert kept is None and torch.equal(h, token)
+    o = q8.RMSNormQ8(1, width).forward(token, None, layer.gain_in)
+    y = ref.values(o.codes.cpu().numpy(), o.scales.cpu().numpy(), width)
+    W1 = ref.values(layer.q1[0].cpu().numpy(), layer.q1[1].cpu().numpy(), width)
+    W2 = ref.values(layer.q2[0].cpu().numpy(), layer.q2[1].cpu().numpy(), hidden)
+    u = y @ W1.T + f64(layer.b1)
+    s = u / (1 + np.exp(-u))
+    du = 2.0 ** -8 * np.abs(u) * 1.1 + 2.0 ** -8 * np.abs(s)          # u and silu(u) in bf16
+    ds = du + np.abs(s).max() * (1 + 2.0 ** -8) / 254 + 2.0 ** -8 * np.abs(s)
+    want = s @ W2.T + f64(layer.b2)
+    within(f64(out), want, ds @ np.abs(W2).T + 2.0 ** -8 * np.abs(want) + 1e-6, "out")
