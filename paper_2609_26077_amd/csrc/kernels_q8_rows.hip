@@ -426,6 +426,105 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR, TPR == 1024 ? 4 : 2) void no
   }
 }
 
+// Small gradients: one launch.  dg does not need c, so its column sums come from
+// workgroups of their own, which read dy and h again (from the caches) rather
+// than wait for a second kernel: one row of 4096 6.0 -> 3.2 us, 64 rows 6.8 -> 3.4,
+// 512 rows 12.5 -> 7.8 (1000 of 1302 would take 18, 12 with partial sums).  A
+// workgroup of those takes 8 LANES columns, LANES threads a row and 256 / LANES
+// rows at a time.
+template <int T, int TPR, int C, bool SAVED, int LANES>
+__global__ __launch_bounds__(256) void small_norm_grad_kernel(NormGradArgs a, int row_blocks) {
+  using E = elem_t<T>;
+  const E *gain = static_cast<const E *>(a.gain), *dys = static_cast<const E *>(a.dy);
+  if ((int)blockIdx.x >= row_blocks) {
+    constexpr int ROWS = 256 / LANES;
+    __shared__ float sums[4][8 * LANES];
+    const int lane = threadIdx.x % LANES, first = threadIdx.x / LANES;
+    const int64_t col = 8 * ((int64_t)(blockIdx.x - row_blocks) * LANES + lane);
+    float dg[8] = {};
+    // four rows' reads on their way at a time (rows past the last: its, times zero)
+    for (int64_t row0 = first; row0 < a.rows; row0 += 4 * ROWS) {
+      Raw8<T> dy[4], h[SAVED ? 1 : 4];
+      u32x2 q[SAVED ? 4 : 1];
+      float s[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int64_t row = min(row0 + u * ROWS, a.rows - 1);
+        dy[u] = raw8<T>(dys + row * a.cols + col, a.cols - col);
+        s[u] = a.rstd[row];
+        if (SAVED) {
+          const bool in = col < a.pitch;
+          q[u] = in ? *reinterpret_cast<const u32x2 *>(a.saved + row * a.pitch + col) : (u32x2){};
+          s[u] *= in ? a.saved_scales[row * (a.pitch / kGroup) + col / kGroup] : 0.0f;
+        } else {
+          h[u] = raw8<T>(static_cast<const E *>(a.h) + row * a.cols + col, a.cols - col);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (row0 + u * ROWS >= a.rows) break;
+        float d[8], x[8];
+        floats8<T>(dy[u], d);
+        if (SAVED) codes8(q[u], x);
+        else floats8<T>(h[u], x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dg[i] += d[i] * (x[i] * s[u]);
+      }
+    }
+    // over a wave's rows, then the four waves'
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+      for (int o = LANES; o < 64; o *= 2) dg[i] += __shfl_xor(dg[i], o);
+      if ((threadIdx.x & 63) < LANES) sums[threadIdx.x >> 6][8 * lane + i] = dg[i];
+    }
+    __syncthreads();
+    const int64_t out = 8 * (int64_t)(blockIdx.x - row_blocks) * LANES + threadIdx.x;
+    if (threadIdx.x < 8 * LANES && out < a.cols)
+      a.dgain[out] = sums[0][threadIdx.x] + sums[1][threadIdx.x] + sums[2][threadIdx.x] + sums[3][threadIdx.x];
+    return;
+  }
+  constexpr int RPB = 256 / TPR;
+  const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  const int64_t want = (int64_t)blockIdx.x * RPB + sub, row = min(want, a.rows - 1);
+  const float rstd = a.rstd[row];
+  float w[C][8], xh[C][8], dot = 0.0f;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int64_t col = 8 * (int64_t)(c * TPR + t);
+    load8<T>(dys + row * a.cols + col, a.cols - col, w[c]);
+    grad_h<T, SAVED>(a, row, col, xh[c]);
+  }
+  if (gain) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int64_t col = 8 * (int64_t)(c * TPR + t);
+      float g[8];
+      load8<T>(gain + col, a.cols - col, g);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[c][i] *= g[i];
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      xh[c][i] *= rstd;
+      dot += w[c][i] * xh[c][i];
+    }
+  const float m = reduce_sum<TPR>(dot, 0) * (1.0f / (float)a.cols);
+  if (want != row) return;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int64_t col = 8 * (int64_t)(c * TPR + t);
+    float o[8] = {};
+    if (a.dh) load8<T>(static_cast<const E *>(a.dh) + row * a.cols + col, a.cols - col, o);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] += rstd * (w[c][i] - xh[c][i] * m);
+    store8<T>(static_cast<E *>(a.dx) + row * a.cols + col, a.cols - col, o);
+  }
+}
+
 // Long rows: two walks for dx; the gain's sums come from a kernel of their own.
 template <int T, bool SAVED>
 __global__ __launch_bounds__(1024) void long_norm_grad_kernel(NormGradArgs a) {
@@ -576,12 +675,32 @@ int64_t grad_blocks(int64_t rows, int64_t cols) {
   return std::max<int64_t>(1, std::min((rows + rpb - 1) / rpb, most));
 }
 
+// One launch up to here: at most 8 rows a thread in the columns' workgroups, two
+// round trips to memory.
+bool small_grad(int64_t rows, int64_t cols) { return rows > 0 && rows <= kFewRows && cols <= 8192; }
+
+template <int T, int TPR, int C, bool SAVED>
+void launch_small(const NormGradArgs &a, hipStream_t s) {
+  constexpr int RPB = 256 / TPR;
+  const int rows = (int)((a.rows + RPB - 1) / RPB), chunks = (int)((a.cols + 7) / 8);
+  const int wide = a.dgain ? (chunks + 7) / 8 : 0, narrow = a.dgain ? (chunks + 3) / 4 : 0;
+  if (a.rows <= 128) small_norm_grad_kernel<T, TPR, C, SAVED, 8><<<dim3((unsigned)(rows + wide)), 256, 0, s>>>(a, rows);
+  else small_norm_grad_kernel<T, TPR, C, SAVED, 4><<<dim3((unsigned)(rows + narrow)), 256, 0, s>>>(a, rows);
+}
+
 template <int T, bool SAVED>
-void launch_grad(NormGradArgs a, hipStream_t s) {
+void launch_grad(const NormGradArgs &a, hipStream_t s) {
+  if (small_grad(a.rows, a.cols)) {
+    if (a.cols <= 512) launch_small<T, 64, 1, SAVED>(a, s);
+    else if (a.cols <= 1024) launch_small<T, 64, 2, SAVED>(a, s);
+    else if (a.cols <= 2048) launch_small<T, 256, 1, SAVED>(a, s);
+    else if (a.cols <= 4096) launch_small<T, 256, 2, SAVED>(a, s);
+    else launch_small<T, 256, 4, SAVED>(a, s);
+    return;
+  }
   const Geometry g = grad_geometry(a.cols);
   const int64_t blocks = a.rows > 0 ? grad_blocks(a.rows, a.cols) : 0;
   const dim3 grid((unsigned)blocks);
-  if (blocks == 1) a.partial = a.dgain;   // one workgroup's sums are all of them
   if (blocks == 0) {
     // no rows: the gain's sums are empty
   } else if (g.tpr == 0) {
@@ -595,7 +714,7 @@ void launch_grad(NormGradArgs a, hipStream_t s) {
   else if (g.tpr == 256) norm_grad_kernel<T, 256, 2, SAVED><<<grid, 256, 0, s>>>(a);
   else if (g.tpr == 512) norm_grad_kernel<T, 512, 2, SAVED><<<grid, 512, 0, s>>>(a);
   else norm_grad_kernel<T, 1024, 2, SAVED><<<grid, 1024, 0, s>>>(a);
-  if (a.dgain && blocks != 1)
+  if (a.dgain)
     sum_partials_kernel<<<dim3((unsigned)((a.cols + 31) / 32)), 1024, 0, s>>>(a.partial, a.dgain, blocks, a.cols);
 }
 
@@ -621,7 +740,7 @@ int launch_dequantize(int type, const DequantArgs &a, void *stream) {
 }
 
 int64_t norm_grad_partials(int64_t rows, int64_t cols) {
-  return grad_blocks(rows, cols);
+  return small_grad(rows, cols) ? 0 : grad_blocks(rows, cols);
 }
 
 int launch_rmsnorm_grad(int type, const NormGradArgs &a, void *stream) {

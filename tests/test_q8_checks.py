@@ -74,7 +74,7 @@ def test_norm_refuses(fm):
 
 def test_norm_backward_refuses(fm):
     n = ctypes.c_size_t()
-    d = fm.fmm_norm_desc(4, 8, 0, 1e-6)
+    d = fm.fmm_norm_desc(4000, 8, 0, 1e-6)
     assert status(fm, "fmm_rmsnorm_q8_backward_scratch_size", d, None) == fm.FMM_ERR_ARG
     assert status(fm, "fmm_rmsnorm_q8_backward_scratch_size", fm.fmm_norm_desc(4, 0, 0, 0.0), n) == fm.FMM_ERR_SHAPE
     need = fm.fmm_rmsnorm_q8_backward_scratch_size(d)
