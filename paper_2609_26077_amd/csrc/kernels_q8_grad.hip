@@ -268,10 +268,11 @@ Cut cut_of(const int64_t (&m)[2], const int64_t (&n)[2], const int64_t (&steps)[
   return best;
 }
 
-// (nothing is wanted of a product with m = 0)
+// (a product that is not wanted has no rows and no steps: it is left in one run)
 Cut cut_of(int type, int64_t M, int64_t N, int64_t K, bool dx, bool dw, int ncu) {
   const int64_t parts = type == FMM_BF16 ? 1 : type == FMM_F16 ? 2 : 3;
-  return cut_of({dx ? M : 0, dw ? N : 0}, {K, K}, {parts * ((N + kPos - 1) / kPos), parts * ((M + kPos - 1) / kPos)}, ncu);
+  return cut_of({dx ? M : 0, dw ? N : 0}, {K, K},
+                {dx ? parts * ((N + kPos - 1) / kPos) : 0, dw ? parts * ((M + kPos - 1) / kPos) : 0}, ncu);
 }
 
 template <int T, class TL>

@@ -666,13 +666,17 @@ Geometry grad_geometry(int64_t cols) {
   if (cols <= 16384) return {1024, 2};
   return {0, 0};
 }
-// The workgroups that share the rows: two of 256 threads a compute unit.  More
-// leave more partial sums (8192 x 4096 bf16: 53 us; twice as many 59, half 79).
-int64_t grad_blocks(int64_t rows, int64_t cols) {
+// The workgroups that share the rows: two of 256 threads a compute unit, or three
+// where that leaves each eight rows or more and their registers fit (16-bit rows).
+// More of them leave more partial sums.  bf16 8192 x 4096: 52 us with 512, 47 with
+// 768, 59 with 1024; 700 x 4096 13.8 with 512, 16.2 with 700; fp32 4096 x 4096 39
+// with 512, 43 with 768.
+int64_t grad_blocks(int type, int64_t rows, int64_t cols) {
   const Geometry g = grad_geometry(cols);
-  const int64_t rpb = g.tpr == 64 ? 4 : 1;
-  const int64_t most = g.tpr == 0 ? 64 : 512 * 256 / std::max(g.tpr, 256);
-  return std::max<int64_t>(1, std::min((rows + rpb - 1) / rpb, most));
+  const int64_t units = g.tpr == 64 ? (rows + 3) / 4 : rows;
+  const bool three = g.tpr != 0 && g.tpr <= 256 && type != FMM_F32 && units >= 8 * 768;
+  const int64_t most = g.tpr == 0 ? 64 : three ? 768 : 512 * 256 / std::max(g.tpr, 256);
+  return std::max<int64_t>(1, std::min(units, most));
 }
 
 // One launch up to here: at most 8 rows a thread in the columns' workgroups, two
@@ -699,7 +703,7 @@ void launch_grad(const NormGradArgs &a, hipStream_t s) {
     return;
   }
   const Geometry g = grad_geometry(a.cols);
-  const int64_t blocks = a.rows > 0 ? grad_blocks(a.rows, a.cols) : 0;
+  const int64_t blocks = a.rows > 0 ? grad_blocks(T, a.rows, a.cols) : 0;
   const dim3 grid((unsigned)blocks);
   if (blocks == 0) {
     // no rows: the gain's sums are empty
@@ -739,8 +743,8 @@ int launch_dequantize(int type, const DequantArgs &a, void *stream) {
   return hipGetLastError();
 }
 
-int64_t norm_grad_partials(int64_t rows, int64_t cols) {
-  return small_grad(rows, cols) ? 0 : grad_blocks(rows, cols);
+int64_t norm_grad_partials(int type, int64_t rows, int64_t cols) {
+  return small_grad(rows, cols) ? 0 : grad_blocks(type, rows, cols);
 }
 
 int launch_rmsnorm_grad(int type, const NormGradArgs &a, void *stream) {

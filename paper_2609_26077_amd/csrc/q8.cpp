@@ -45,7 +45,7 @@ int check_grad(const fmm_q8_desc *d) {
 }
 
 size_t norm_grad_scratch(const fmm_norm_desc &d) {
-  return d.rows == 0 ? 0 : sizeof(float) * (size_t)norm_grad_partials(d.rows, d.cols) * (size_t)d.cols;
+  return d.rows == 0 ? 0 : sizeof(float) * (size_t)norm_grad_partials(d.type, d.rows, d.cols) * (size_t)d.cols;
 }
 
 }  // namespace

@@ -56,7 +56,7 @@ struct NormGradArgs {
   int64_t rows, cols, pitch;
 };
 // rows of partial sums that the gradient of the gain goes through
-int64_t norm_grad_partials(int64_t rows, int64_t cols);
+int64_t norm_grad_partials(int type, int64_t rows, int64_t cols);
 int launch_rmsnorm_grad(int type, const NormGradArgs &a, void *stream);
 
 // ---- products (q8_gemm.h, kernels_q8_matmul.hip, kernels_q8_grad.hip) -------

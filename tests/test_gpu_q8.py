@@ -383,6 +383,14 @@ def test_linear_gradient_of_what_is_wanted(torch, q8, t, x, w, b):
     check_grad(torch, q8, t, 70, 130, 200, need_x=x, need_w=w, bias=b)
 
 
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("x,w", [(True, True), (True, False), (False, True)])
+@pytest.mark.parametrize("M,N,K", [(4096, 4100, 17), (4100, 130, 70), (70, 4100, 130)])
+def test_linear_gradient_in_runs(torch, q8, t, x, w, M, N, K):
+    """Few outputs and long sums, whose contracted axes are split: of both products, and of each where only it is wanted."""
+    check_grad(torch, q8, t, M, N, K, need_x=x, need_w=w)
+
+
 @pytest.mark.parametrize("M,N,K", [(0, 5, 7), (5, 0, 7), (4, 6, 0)])
 def test_linear_gradient_of_nothing(torch, q8, M, N, K):
     check_grad(torch, q8, "bf16", M, N, K)
