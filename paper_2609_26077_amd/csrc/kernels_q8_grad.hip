@@ -166,16 +166,18 @@ struct GradGemms {
   int tiles;                 // rows of colsum
 };
 
-template <class T, int OUT>
-__global__ __launch_bounds__(T::kThreads, 2) void grad_kernel(GradGemms g) {
-  __shared__ uint4 lds[T::kLds / 16];
+// Tiles TX of dX and TW of dW (equal workgroups).
+template <class TX, class TW, int OUT>
+__global__ __launch_bounds__(TX::kThreads, 2) void grad_kernel(GradGemms g) {
+  static_assert(TX::kThreads == TW::kThreads, "one launch");
+  __shared__ uint4 lds[(TX::kLds > TW::kLds ? TX::kLds : TW::kLds) / 16];
   const int id = blockIdx.x;
   if (id < g.items) {
-    if (id < g.items0) gemm_tile<Bf16, T, OUT>(g.p[0], id, lds);
-    else gemm_tile<Bf16, T, OUT>(g.p[1], id - g.items0, lds);
+    if (id < g.items0) gemm_tile<Bf16, TX, OUT>(g.p[0], id, lds);
+    else gemm_tile<Bf16, TW, OUT>(g.p[1], id - g.items0, lds);
     return;
   }
-  const int64_t n = (int64_t)(id - g.items) * T::kThreads + threadIdx.x;
+  const int64_t n = (int64_t)(id - g.items) * TX::kThreads + threadIdx.x;
   if (n >= g.N) return;
   float s = 0.0f;
 #pragma unroll 4
@@ -229,42 +231,49 @@ Layout layout_of(int type, int64_t M, int64_t N, int64_t K) {
   return l;
 }
 
-// How the products are cut: the tile that both take, and the runs that each
-// one's contracted axis is split into.
+// How the products are cut: the tile of each, and the runs that its contracted
+// axis is split into.
 struct Cut {
-  int tile;        // 0: 64, 1: 128, 2: 256
+  int tile[2];     // 0: 64, 1: 128, 2: 256 (of both, or neither: its workgroups are larger)
   int splits[2];
 };
 
-// t = start + max(chain steps of a run, work steps tiles / CUs) us, as for the
-// int8 product, whose fits of these three tiles these are (a step moves and
-// multiplies as much); runs cost a launch and the traffic of their sums besides.
-// Without them few tiles with a long axis leave most of the chip idle: 8192 tokens
-// of 512 x 512 channels 42 -> 32 us, of 1024 x 1024 87 -> 65.
+// t = max(start + chain steps of a run, of either; start + work of both / CUs) us,
+// a product's work being its tile's `work` times steps and tiles, as for the int8
+// product, whose fits of these three tiles these are (a step moves and multiplies
+// as much); runs cost a launch and the traffic of their sums besides.  Without
+// them few tiles with a long axis leave most of the chip idle: 8192 tokens of 512 x
+// 512 channels 42 -> 32 us, of 1024 x 1024 87 -> 65.  A tile for each, not one for
+// both: 2000 tokens of 300 x 2000 in fp16 37.6 -> 32.1, 6000 x 6000 x 1000 205 -> 198.
 Cut cut_of(const int64_t (&m)[2], const int64_t (&n)[2], const int64_t (&steps)[2], int ncu) {
   constexpr int kEdge[3] = {64, 128, 256};
   constexpr double kStart[3] = {3.2, 4.5, 7.5}, kChain[3] = {0.20, 0.47, 1.05}, kWork[3] = {0.29, 0.76, 2.45};
   constexpr double kMostSums = 1 << 24;   // floats of sums: 64 MB
+  double work[2][3];
+  for (int k = 0; k < 2; ++k)
+    for (int i = 0; i < 3; ++i)
+      work[k][i] = kWork[i] * steps[k] * (double)((m[k] + kEdge[i] - 1) / kEdge[i]) *
+                   (double)((n[k] + kEdge[i] - 1) / kEdge[i]) / ncu;
   Cut best = {};
   double least = 1e300;
-  for (int i = 0; i < 3; ++i) {
-    double tiles[2];
-    for (int k = 0; k < 2; ++k)
-      tiles[k] = (double)((m[k] + kEdge[i] - 1) / kEdge[i]) * (double)((n[k] + kEdge[i] - 1) / kEdge[i]);
-    const double work = kWork[i] * (steps[0] * tiles[0] + steps[1] * tiles[1]) / ncu;
-    for (int s0 = 1; s0 <= 16; s0 *= 2)
-      for (int s1 = 1; s1 <= 16; s1 *= 2) {
-        if ((s0 > 1 && s0 * 4 > steps[0]) || (s1 > 1 && s1 * 4 > steps[1])) continue;
-        const double sums = (s0 > 1 ? (double)m[0] * n[0] * s0 : 0) + (s1 > 1 ? (double)m[1] * n[1] * s1 : 0);
-        if (sums > kMostSums) continue;
-        const double chain = kChain[i] * std::max((steps[0] + s0 - 1) / s0, (steps[1] + s1 - 1) / s1);
-        const double t = kStart[i] + std::max(chain, work) + (sums > 0 ? 3.0 + sums * 8 / 4e6 : 0);
-        if (t < least) {
-          least = t;
-          best = {i, {s0, s1}};
+  for (int t0 = 0; t0 < 3; ++t0)
+    for (int t1 = 0; t1 < 3; ++t1) {
+      if ((t0 == 2) != (t1 == 2)) continue;
+      const double busy = std::max(m[0] ? kStart[t0] : 0, m[1] ? kStart[t1] : 0) + work[0][t0] + work[1][t1];
+      for (int s0 = 1; s0 <= 16; s0 *= 2)
+        for (int s1 = 1; s1 <= 16; s1 *= 2) {
+          if ((s0 > 1 && s0 * 4 > steps[0]) || (s1 > 1 && s1 * 4 > steps[1])) continue;
+          const double sums = (s0 > 1 ? (double)m[0] * n[0] * s0 : 0) + (s1 > 1 ? (double)m[1] * n[1] * s1 : 0);
+          if (sums > kMostSums) continue;
+          const double chain = std::max(kStart[t0] + kChain[t0] * ((steps[0] + s0 - 1) / s0),
+                                        kStart[t1] + kChain[t1] * ((steps[1] + s1 - 1) / s1));
+          const double t = std::max(chain, busy) + (sums > 0 ? 3.0 + sums * 8 / 4e6 : 0);
+          if (t < least) {
+            least = t;
+            best = {{t0, t1}, {s0, s1}};
+          }
         }
-      }
-  }
+    }
   return best;
 }
 
@@ -275,18 +284,19 @@ Cut cut_of(int type, int64_t M, int64_t N, int64_t K, bool dx, bool dw, int ncu)
                 {dx ? parts * ((N + kPos - 1) / kPos) : 0, dw ? parts * ((M + kPos - 1) / kPos) : 0}, ncu);
 }
 
-template <int T, class TL>
+template <int T, class TX, class TW>
 void launch_gemms(GradGemms g, const GradArgs &a, hipStream_t s) {
+  constexpr int kEdge[2] = {TX::TM, TW::TM};
   for (int i = 0; i < 2; ++i) {
-    g.p[i].tiles_m = (g.p[i].M + TL::TM - 1) / TL::TM;
-    g.p[i].tiles_n = (g.p[i].N + TL::TN - 1) / TL::TN;
+    g.p[i].tiles_m = (g.p[i].M + kEdge[i] - 1) / kEdge[i];
+    g.p[i].tiles_n = (g.p[i].N + kEdge[i] - 1) / kEdge[i];
   }
   const int64_t dx = a.dx ? (int64_t)g.p[0].tiles_m * g.p[0].tiles_n * g.p[0].splits : 0;
   const int64_t dw = a.dw ? (int64_t)g.p[1].tiles_m * g.p[1].tiles_n * g.p[1].splits : 0;
-  const int64_t db = a.dbias ? (a.N + TL::kThreads - 1) / TL::kThreads : 0;
+  const int64_t db = a.dbias ? (a.N + TX::kThreads - 1) / TX::kThreads : 0;
   g.items0 = (int)dx;
   g.items = (int)(dx + dw);
-  if (dx + dw + db > 0) grad_kernel<TL, T><<<dim3((unsigned)(dx + dw + db)), TL::kThreads, 0, s>>>(g);
+  if (dx + dw + db > 0) grad_kernel<TX, TW, T><<<dim3((unsigned)(dx + dw + db)), TX::kThreads, 0, s>>>(g);
   int64_t chunks[2];
   for (int i = 0; i < 2; ++i)
     chunks[i] = (i ? dw : dx) > 0 && g.p[i].splits > 1 ? ((int64_t)g.p[i].M * g.p[i].N + 7) / 8 : 0;
@@ -331,11 +341,11 @@ int launch(const GradArgs &a, int ncu, hipStream_t s) {
   w.splits = cut.splits[1];
   x.partial = reinterpret_cast<float *>(a.ws + l.total);
   w.partial = x.partial + (x.splits > 1 ? (int64_t)x.splits * a.M * a.K : 0);
-  switch (cut.tile) {
-    case 0: launch_gemms<T, Tile64>(q, a, s); break;
-    case 1: launch_gemms<T, Tile128>(q, a, s); break;
-    default: launch_gemms<T, Tile256>(q, a, s);
-  }
+  if (cut.tile[0] == 2) launch_gemms<T, Tile256, Tile256>(q, a, s);
+  else if (cut.tile[0] == 1 && cut.tile[1] == 1) launch_gemms<T, Tile128, Tile128>(q, a, s);
+  else if (cut.tile[0] == 1) launch_gemms<T, Tile128, Tile64>(q, a, s);
+  else if (cut.tile[1] == 1) launch_gemms<T, Tile64, Tile128>(q, a, s);
+  else launch_gemms<T, Tile64, Tile64>(q, a, s);
   return hipGetLastError();
 }
 
