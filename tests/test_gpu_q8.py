@@ -554,3 +554,52 @@ def test_feedforward_example(torch, q8):
     ds = du + np.abs(s).max() * (1 + 2.0 ** -8) / 254 + 2.0 ** -8 * np.abs(s)
     want = s @ W2.T + f64(layer.b2)
     within(f64(out), want, ds @ np.abs(W2).T + 2.0 ** -8 * np.abs(want) + 1e-6, "out")
+
+
+# ---- the binding under the wrappers ------------------------------------------------------------
+@pytest.mark.parametrize("t", TYPES)
+def test_binding_calls_are_what_the_wrappers_call(torch, q8, t):
+    """The functions named after the C entry points, on tensors, and outputs that the caller provides."""
+    import paper_2609_26077_amd as fm
+    M, N, K = 9, 70, 200
+    dt, P = dtype_of(torch, t), ref.pitch(K)
+    ty = q8.TYPES[dt]
+    x, res, dy = randn(torch, 1, M, K, t=t), randn(torch, 2, M, K, t=t), randn(torch, 3, M, N, t=t)
+    gain = 1 + randn(torch, 4, K, t=t, scale=0.1)
+    new = lambda *s, d=dt: torch.empty(s, dtype=d, device="cuda")
+    i8, f4 = torch.int8, torch.float32
+
+    want_q, want_s = q8.quantize(x)
+    q, s = new(M, P, d=i8), new(M, d=f4)
+    a, b = q8.quantize(x, codes=q, scales=s)
+    assert a is q and b is s and torch.equal(q, want_q) and torch.equal(s, want_s)
+    q2, s2 = new(M, P, d=i8), new(M, d=f4)
+    fm.fmm_q8_quantize(ty, M, K, x, q2, s2)
+    assert torch.equal(q2, want_q) and torch.equal(s2, want_s)
+    v = new(M, K)
+    fm.fmm_q8_dequantize(ty, M, K, 0, q2, s2, v)
+    assert torch.equal(v, q8.dequantize(want_q, want_s, K, dt))
+
+    norm = q8.RMSNormQ8(M, K, dt)
+    o = norm.forward(x, res, gain, checkpoint=True)
+    h, rstd, saved, saved_s = new(M, K), new(M, d=f4), new(M, P, d=i8), new(M, P // 128, d=f4)
+    fm.fmm_rmsnorm_q8(norm.desc, x, res, gain, h, q2, s2, saved, saved_s, rstd)
+    for got, want in zip((h, q2, s2, rstd, saved, saved_s), o):
+        assert torch.equal(got, want)
+    dx, dg = new(M, K), new(K, d=f4)
+    n = fm.fmm_rmsnorm_q8_backward_scratch_size(norm.desc)
+    fm.fmm_rmsnorm_q8_backward(norm.desc, x, res, None, saved, saved_s, rstd, gain, dx, dg, new(max(n, 16), d=torch.uint8), n)
+    for got, want in zip((dx, dg), norm.backward(x, o.rstd, gain, saved=(o.saved_codes, o.saved_scales), dh=res)):
+        assert torch.equal(got, want)
+
+    lin = q8.LinearQ8(M, N, K, dt)
+    w, sw = codes(torch, 5, N, K)
+    bias = randn(torch, 6, N)
+    C = new(M, N)
+    fm.fmm_q8_matmul(lin.desc, q2, s2, w, sw, bias, C)
+    assert torch.equal(C, lin.matmul(q2, s2, w, sw, bias))
+    n = fm.fmm_q8_linear_backward_scratch_size(lin.desc)
+    gx, gw, gb = new(M, K), new(N, K), new(N, d=f4)
+    fm.fmm_q8_linear_backward(lin.desc, dy, q2, s2, w, sw, gx, gw, gb, new(n, d=torch.uint8), n)
+    for got, want in zip((gx, gw, gb), lin.backward(dy, q2, s2, w, sw, bias=True)):
+        assert torch.equal(got, want)
