@@ -135,13 +135,14 @@ void launch_few(const GemmProblem &g, hipStream_t s) {
 // where it is.  Fitted to all seven on 210 shapes (1 to 8192 tokens, 64 to 8192
 // channels; 13 to 20% standard deviation each); the one it picks is 2% slower than the
 // fastest on average, 32% at worst.  Each is the fastest somewhere, us:
-//   tokens x channels x channels   16x16  32x32  48x32  64x32  64x64  128   256
-//   1 x 8192 x 8192                 14.1   16.0   16.8   17.4   24    43    74
-//   64 x 4096 x 4096                12.1    6.2    8.9    7.7    8.7  17    38
-//   256 x 1024 x 8192               22.0   10.9    8.6   10.3   15    33    73
-//   1000 x 1302 x 1472              27     11.8   12.5   13.2    7.6  10.2  22
-//   2048 x 4096 x 4096             370    103     92     99     55    36    47
-//   8192 x 8192 x 8192               -      -      -   1640    800   493   419
+//   tokens x channels x channels   16x16  32x32  48x32  64x32  64x64    128    256
+//   1 x 8192 x 8192                 13.8   15.9   16.1   16.6   20.6   53.5   89.8
+//   64 x 4096 x 4096                10.3    6.2    7.0    7.7    9.0   19.7   39.5
+//   64 x 8192 x 8192                42.6   26.8   28.8   20.7   25.5   53.7   92.7
+//   256 x 1024 x 8192               13.3    8.9    8.6   10.3   14.1   32.9   71.0
+//   256 x 4096 x 4096               31.3   16.8   15.3   14.3    9.7   19.5   39.2
+//   2048 x 4096 x 4096             196    106     89     99     63     37.6   46.6
+//   2048 x 8192 x 8192            1140    622    450    458    239    149    124
 struct Shape {
   int tm, tn, waves;            // tile, and the waves that share its contracted axis
   float start, chain, work;

@@ -25,9 +25,9 @@
 // many as the row has chunks, up to 1024, which is what a single token's latency
 // wants.
 //
-// Measured, forward with residual and checkpoint: 8192 x 4096 bf16 43 us, 5.2 TB/s
-// and more (a 1 GiB copy: 5.2); 1024 x 8192 fp32 21; one token of 4096 3.4.
-// Gradient from the checkpoint, with dh: 53 (floor 45), 26 and 6.
+// Measured: forward with residual and checkpoint, 8192 x 4096 bf16 51 us, 5.2 TB/s
+// (the rate of a 1 GiB copy), 1024 x 8192 fp32 21, one token of 4096 3.4; gradient
+// from the checkpoint with dh 51 (4.6 TB/s), 26 and 3.2.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
