@@ -316,7 +316,7 @@ struct GradRow {
   float s[SAVED ? C : 1], rstd;
 };
 
-// (4 waves a SIMD: 128 registers)
+// 1024 threads a row are 4 waves a SIMD, 128 registers each; the others may have 256.
 template <int T, int TPR, int C, bool SAVED>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR, TPR == 1024 ? 4 : 2) void norm_grad_kernel(NormGradArgs a) {
   constexpr int RPB = TPR < 256 ? 256 / TPR : 1;

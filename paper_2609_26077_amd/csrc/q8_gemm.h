@@ -29,8 +29,8 @@
 // What bounds the 256 x 256 tile is power: at 8192^3 int8 the matrix cores are
 // busy 73% of the cycles, at 1.6 to 1.7 GHz; 420 us with operands that the caches
 // keep from call to call (2.6 POP/s; the runtime's own int8 product 434 and 71%),
-// 450 to 460 with others.  bf16, 8192 x 4096 x 8192: 400 us, 1.38 PFLOP/s.  The
-// smaller tiles are bound by their transfers from L2 (24 to 26 TB/s).
+// 450 to 460 with others.  bf16, 8192 x 4096 x 8192: 392 to 400 us, 1.37 to
+// 1.40 PFLOP/s.  The smaller tiles are bound by their transfers from L2 (24 to 26 TB/s).
 #pragma once
 
 #include <hip/hip_runtime.h>
