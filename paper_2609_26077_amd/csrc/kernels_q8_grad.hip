@@ -234,35 +234,42 @@ Layout layout_of(int type, int64_t M, int64_t N, int64_t K) {
 // How the products are cut: the tile of each, and the runs that its contracted
 // axis is split into.
 struct Cut {
-  int tile[2];     // 0: 64, 1: 128, 2: 256 (of both, or neither: its workgroups are larger)
+  int tile[2];     // 0: 64, 1: 128, 2: 256, 3: 128 with the longer ring (2 and 3 of both, or
+                   // neither: their workgroups are larger)
   int splits[2];
 };
 
 // t = max(start + chain steps of a run, of either; start + work of both / CUs) us,
-// a product's work being its tile's `work` times steps and tiles, as for the int8
-// product, whose fits of these three tiles these are (a step moves and multiplies
-// as much); runs cost a launch and the traffic of their sums besides.  Without
-// them few tiles with a long axis leave most of the chip idle: 8192 tokens of 512 x
-// 512 channels 42 -> 32 us, of 1024 x 1024 87 -> 65.  A tile for each, not one for
-// both: 2000 tokens of 300 x 2000 in fp16 37.6 -> 32.1, 6000 x 6000 x 1000 205 -> 198.
+// a product's work being its tile's `work` times steps and tiles; runs cost a launch
+// and the traffic of their sums besides.  The form is the int8 product's (a step moves
+// and multiplies as much), the constants the best of six sets on 80 shapes, each with
+// either product and with both: 1.3% over the best of the six on average, 20% at worst.
+// Without runs few tiles with a long axis leave most of the chip idle: 8192 tokens of
+// 512 x 512 channels 42 -> 32 us, of 1024 x 1024 87 -> 65 to 69.  A tile for each, not
+// one for both: 2000 tokens of 300 x 2000 in fp16 37.6 -> 32.1.  The longer ring where
+// each CU has a workgroup at most: 1000 x 1302 x 1472 fp32 49 -> 43, 2048^3 bf16 54 ->
+// 47; 13436 tokens of 2023 x 124, the worst of the 80, 69 -> 74.
 Cut cut_of(const int64_t (&m)[2], const int64_t (&n)[2], const int64_t (&steps)[2], int ncu) {
-  constexpr int kEdge[3] = {64, 128, 256};
-  constexpr double kStart[3] = {3.2, 4.5, 7.5}, kChain[3] = {0.20, 0.47, 1.05}, kWork[3] = {0.29, 0.76, 2.45};
+  constexpr int kEdge[4] = {64, 128, 256, 128};
+  constexpr double kStart[4] = {3.2, 4.5, 7.5, 4.0}, kChain[4] = {0.20, 0.47, 1.2, 0.36},
+                   kWork[4] = {0.29, 0.60, 2.0, 0.36};
   constexpr double kMostSums = 1 << 24;   // floats of sums: 64 MB
-  double work[2][3];
+  double tiles[2][4], work[2][4];
   for (int k = 0; k < 2; ++k)
-    for (int i = 0; i < 3; ++i)
-      work[k][i] = kWork[i] * steps[k] * (double)((m[k] + kEdge[i] - 1) / kEdge[i]) *
-                   (double)((n[k] + kEdge[i] - 1) / kEdge[i]) / ncu;
+    for (int i = 0; i < 4; ++i) {
+      tiles[k][i] = (double)((m[k] + kEdge[i] - 1) / kEdge[i]) * (double)((n[k] + kEdge[i] - 1) / kEdge[i]);
+      work[k][i] = kWork[i] * steps[k] * tiles[k][i] / ncu;
+    }
   Cut best = {};
   double least = 1e300;
-  for (int t0 = 0; t0 < 3; ++t0)
-    for (int t1 = 0; t1 < 3; ++t1) {
-      if ((t0 == 2) != (t1 == 2)) continue;
+  for (int t0 = 0; t0 < 4; ++t0)
+    for (int t1 = 0; t1 < 4; ++t1) {
+      if (t0 != t1 && (t0 > 1 || t1 > 1)) continue;
       const double busy = std::max(m[0] ? kStart[t0] : 0, m[1] ? kStart[t1] : 0) + work[0][t0] + work[1][t1];
       for (int s0 = 1; s0 <= 16; s0 *= 2)
         for (int s1 = 1; s1 <= 16; s1 *= 2) {
           if ((s0 > 1 && s0 * 4 > steps[0]) || (s1 > 1 && s1 * 4 > steps[1])) continue;
+          if (t0 == 3 && s0 * tiles[0][3] + s1 * tiles[1][3] > ncu) continue;
           const double sums = (s0 > 1 ? (double)m[0] * n[0] * s0 : 0) + (s1 > 1 ? (double)m[1] * n[1] * s1 : 0);
           if (sums > kMostSums) continue;
           const double chain = std::max(kStart[t0] + kChain[t0] * ((steps[0] + s0 - 1) / s0),
@@ -342,6 +349,7 @@ int launch(const GradArgs &a, int ncu, hipStream_t s) {
   x.partial = reinterpret_cast<float *>(a.ws + l.total);
   w.partial = x.partial + (x.splits > 1 ? (int64_t)x.splits * a.M * a.K : 0);
   if (cut.tile[0] == 2) launch_gemms<T, Tile256, Tile256>(q, a, s);
+  else if (cut.tile[0] == 3) launch_gemms<T, Tile128Ahead, Tile128Ahead>(q, a, s);
   else if (cut.tile[0] == 1 && cut.tile[1] == 1) launch_gemms<T, Tile128, Tile128>(q, a, s);
   else if (cut.tile[0] == 1) launch_gemms<T, Tile128, Tile64>(q, a, s);
   else if (cut.tile[1] == 1) launch_gemms<T, Tile64, Tile128>(q, a, s);

@@ -132,37 +132,42 @@ void launch_few(const GemmProblem &g, hipStream_t s) {
 // The shapes of workgroup the product comes in, and what each takes: t = start +
 // max(chain pieces, work pieces groups / CUs) us, pieces being the 128-byte steps
 // that a wave walks.  `chain` is a piece's time where the chip is not full, `work`
-// where it is.  Fitted to all seven on 210 shapes (1 to 8192 tokens, 64 to 8192
-// channels; 13 to 20% standard deviation each); the one it picks is 2% slower than the
-// fastest on average, 32% at worst.  Each is the fastest somewhere, us:
-//   tokens x channels x channels   16x16  32x32  48x32  64x32  64x64    128    256
-//   1 x 8192 x 8192                 13.8   15.9   16.1   16.6   20.6   53.5   89.8
-//   64 x 4096 x 4096                10.3    6.2    7.0    7.7    9.0   19.7   39.5
-//   64 x 8192 x 8192                42.6   26.8   28.8   20.7   25.5   53.7   92.7
-//   256 x 1024 x 8192               13.3    8.9    8.6   10.3   14.1   32.9   71.0
-//   256 x 4096 x 4096               31.3   16.8   15.3   14.3    9.7   19.5   39.2
-//   2048 x 4096 x 4096             196    106     89     99     63     37.6   46.6
-//   2048 x 8192 x 8192            1140    622    450    458    239    149    124
+// where it is.  Fitted on 390 shapes (1 to 32768 tokens, 1 to 65536 channels) by what
+// the choice then costs: the one it picks is 1.2% slower than the fastest on average,
+// 28% at worst (fitted on half of them, 2.2% and 30% on the others).  Each is the
+// fastest somewhere, us (128+: where there are no more tiles than CUs, the 128 tile with
+// a longer ring):
+//   tokens x channels x channels   16x16  32x32  48x32  64x32  64x64   128+    128    256
+//   1 x 8192 x 8192                13.8   15.9   16.1   16.6   20.6   32.3   53.6   89.8
+//   64 x 4096 x 4096               10.3    6.2    7.0    7.7    9.0   14.9   19.7   39.5
+//   64 x 8192 x 8192               42.6   26.8   28.8   20.7   25.5   35.2   53.8   92.7
+//   256 x 1024 x 8192              13.3    8.9    8.6   10.3   14.1   24.3   33.0   71.0
+//   256 x 4096 x 4096              31.3   16.8   15.3   14.3    9.7   15.3   19.4   39.2
+//   2048 x 1024 x 8192             86.4   48.3   46.6   43.5   29.1   28.2   35.4   71.5
+//   2048 x 4096 x 4096              196    106   89.1   98.8   62.9      -   37.4   46.6
+//   2048 x 8192 x 8192             1140    622    450    458    239      -    148    124
 struct Shape {
   int tm, tn, waves;            // tile, and the waves that share its contracted axis
   float start, chain, work;
+  bool one;                     // only where each CU has one group at most
 };
 constexpr Shape kShapes[] = {
-    {16, 16, 8, 2.0f, 0.30f, 0.55f}, {32, 32, 4, 2.2f, 0.28f, 0.60f}, {48, 32, 4, 2.4f, 0.34f, 0.76f},
-    {64, 32, 4, 2.6f, 0.41f, 1.09f}, {64, 64, 1, 3.2f, 0.20f, 0.29f}, {128, 128, 1, 4.5f, 0.47f, 0.76f},
-    {256, 256, 1, 7.5f, 1.05f, 2.45f},
+    {16, 16, 8, 1.7f, 0.30f, 0.57f, false}, {32, 32, 4, 2.2f, 0.37f, 0.61f, false},
+    {48, 32, 4, 2.4f, 0.58f, 0.76f, false}, {64, 32, 4, 2.6f, 0.41f, 1.2f, false},
+    {64, 64, 1, 3.2f, 0.19f, 0.28f, false}, {128, 128, 1, 3.3f, 0.45f, 0.60f, true},
+    {128, 128, 1, 3.6f, 0.47f, 0.62f, false}, {256, 256, 1, 8.7f, 1.2f, 1.8f, false},
 };
 
 // (a launch takes fewer than 2^32 threads; the largest tile stays below that by the limit on M N)
 constexpr double kMaxGroups = 1 << 22;
 
 int pick(const GemmProblem &g, int ncu) {
-  int best = 6;
+  int best = 7;
   double least = 1e300;
-  for (int i = 0; i < 7; ++i) {
+  for (int i = 0; i < 8; ++i) {
     const Shape &p = kShapes[i];
     const double groups = (double)((g.M + p.tm - 1) / p.tm) * ((g.N + p.tn - 1) / p.tn);
-    if (groups > kMaxGroups) continue;
+    if (groups > kMaxGroups || (p.one && groups > ncu)) continue;
     const double pieces = (g.steps + p.waves - 1) / p.waves;
     const double t = p.start + std::max(p.chain * pieces, p.work * pieces * groups / ncu);
     if (t < least) {
@@ -189,7 +194,8 @@ void launch(const GemmProblem &g, int ncu, hipStream_t s) {
     case 2: return launch_few<3, 2, 4, 2, OUT>(g, s);
     case 3: return launch_few<4, 2, 4, 2, OUT>(g, s);
     case 4: return launch_tiles<Tile64, OUT>(g, s);
-    case 5: return launch_tiles<Tile128, OUT>(g, s);
+    case 5: return launch_tiles<Tile128Ahead, OUT>(g, s);
+    case 6: return launch_tiles<Tile128, OUT>(g, s);
     default: return launch_tiles<Tile256, OUT>(g, s);
   }
 }

@@ -603,3 +603,18 @@ def test_binding_calls_are_what_the_wrappers_call(torch, q8, t):
     fm.fmm_q8_linear_backward(lin.desc, dy, q2, s2, w, sw, gx, gw, gb, new(n, d=torch.uint8), n)
     for got, want in zip((gx, gw, gb), lin.backward(dy, q2, s2, w, sw, bias=True)):
         assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("t,M,N,K", [("fp32", 1500, 1700, 100), ("bf16", 2047, 1999, 128), ("fp16", 2040, 1900, 129),
+                                     ("bf16", 1900, 2000, 300), ("fp32", 1800, 2010, 500), ("fp16", 1283, 1411, 1030),
+                                     ("bf16", 127, 30001, 520)])
+def test_matmul_of_about_a_tile_a_unit(torch, q8, t, M, N, K):
+    """Tiles enough for most compute units and no more, one step of the contracted axis to nine."""
+    check_matmul(torch, q8, t, M, N, K, bias=K > 300)
+
+
+@pytest.mark.parametrize("t,M,N,K", [("bf16", 1030, 1100, 1300), ("fp16", 900, 700, 1500), ("fp32", 300, 2000, 900),
+                                     ("fp32", 1283, 200, 1411), ("bf16", 1900, 33, 2000), ("bf16", 33, 1900, 2000)])
+@pytest.mark.parametrize("x,w", [(True, True), (True, False), (False, True)])
+def test_linear_gradient_of_about_a_tile_a_unit(torch, q8, t, x, w, M, N, K):
+    check_grad(torch, q8, t, M, N, K, need_x=x, need_w=w)
