@@ -87,7 +87,8 @@ def _switched(index, stream):
             yield _raw_stream(index)
         else:
             if isinstance(stream, int):
-                stream = torch.cuda.ExternalStream(stream)
+                # (torch takes a null handle for "any stream of its pool", not for the default stream)
+                stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream(index)
             with torch.cuda.stream(stream):
                 yield stream.cuda_stream
 

@@ -618,3 +618,20 @@ def test_matmul_of_about_a_tile_a_unit(torch, q8, t, M, N, K):
 @pytest.mark.parametrize("x,w", [(True, True), (True, False), (False, True)])
 def test_linear_gradient_of_about_a_tile_a_unit(torch, q8, t, x, w, M, N, K):
     check_grad(torch, q8, t, M, N, K, need_x=x, need_w=w)
+
+
+# ---- the default stream by its handle -------------------------------------------------------------
+def test_default_stream_by_handle(torch, q8):
+    """Handle 0 is torch's default stream: calls on it come after what writes their
+    inputs there, and before what reads their outputs."""
+    M, N, K = 64, 96, 1024
+    assert torch.cuda.current_stream().cuda_stream == 0
+    lin = q8.LinearQ8(M, N, K, torch.float32)
+    w, sw = q8.quantize(randn(torch, 2, N, K))
+    x, late = torch.zeros((M, K), device="cuda"), randn(torch, 1, M, K)
+    want = lin.matmul(*q8.quantize(late), w, sw)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)                 # some ms: the write of x is still to come when the calls are made
+    x.copy_(late)
+    got = lin.matmul(*q8.quantize(x, stream=0), w, sw, stream=0).clone()
+    assert torch.equal(got, want)

@@ -182,6 +182,28 @@ def test_wrappers_refuse_other_devices():
                    torch.zeros(6))
 
 
+def test_handle_zero_is_the_default_stream(monkeypatch):
+    """torch's own default stream has the handle 0, which a caller may pass on; torch
+    makes of ExternalStream(0) a stream of its pool."""
+    import contextlib
+    import types
+
+    import torch
+    from paper_2609_26077_amd import q8
+    made = []
+
+    def stream(handle):
+        return types.SimpleNamespace(cuda_stream=handle, device_index=0, device=torch.device("cuda:0"))
+
+    monkeypatch.setattr(torch.cuda, "device", lambda index: contextlib.nullcontext())
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: (made.append(s), contextlib.nullcontext())[1])
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, *a, **k: stream(handle or 0x7700))
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda index: stream(0))
+    for handle in (0, 0x1230):
+        with q8._switched(0, handle) as used:
+            assert used == handle and made[-1].cuda_stream == handle
+
+
 # ---- the reference itself ------------------------------------------------------------------
 def test_reference_gradient_is_the_losses_derivative():
     """The norm's gradient formula against central differences, binary64."""
