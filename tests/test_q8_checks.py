@@ -182,6 +182,36 @@ def test_wrappers_refuse_other_devices():
                    torch.zeros(6))
 
 
+@pytest.mark.parametrize("stream", [None, 0, 0x1230])
+def test_wrappers_refuse_host_memory(monkeypatch, stream):
+    """Tensors and objects that are all on the CPU: nothing reaches the library, whatever stream is named."""
+    import contextlib
+    import types
+    torch, q8, n, lin = _objects("cpu")
+
+    class NoLibrary:
+        def __getattr__(self, name):
+            raise AssertionError(f"{name} called")
+
+    monkeypatch.setattr(q8, "_lib", NoLibrary())
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "device", lambda index: contextlib.nullcontext())
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: contextlib.nullcontext())
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle: types.SimpleNamespace(cuda_stream=handle))
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda index: types.SimpleNamespace(cuda_stream=0))
+    x, r = torch.zeros((4, 200), dtype=torch.bfloat16), torch.zeros(4)
+    q, s = torch.zeros((4, 256), dtype=torch.int8), torch.zeros((4, 2))
+    w, sw, dy = torch.zeros((6, 256), dtype=torch.int8), torch.zeros(6), torch.zeros((4, 6), dtype=torch.bfloat16)
+    for call in (lambda: q8.quantize(x, stream=stream), lambda: q8.quantize(x, codes=q, scales=r, stream=stream),
+                 lambda: q8.dequantize(q, r, 200, stream=stream),
+                 lambda: q8.dequantize(q, s, 200, torch.bfloat16, out=x, stream=stream),
+                 lambda: n.forward(x, x, checkpoint=True, stream=stream), lambda: n.backward(x, r, h=x, stream=stream),
+                 lambda: n.backward(x, r, saved=(q, s), stream=stream), lambda: lin.matmul(q, r, w, sw, stream=stream),
+                 lambda: lin.backward(dy, q, r, w, sw, bias=True, stream=stream)):
+        with pytest.raises(ValueError, match="device cpu"):
+            call()
+
+
 def test_handle_zero_is_the_default_stream(monkeypatch):
     """torch's own default stream has the handle 0, which a caller may pass on; torch
     makes of ExternalStream(0) a stream of its pool."""
