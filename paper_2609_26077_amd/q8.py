@@ -89,6 +89,8 @@ def _switched(index, stream):
             if isinstance(stream, int):
                 # (torch takes a null handle for "any stream of its pool", not for the default stream)
                 stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream(index)
+            if stream.device_index != index:
+                raise ValueError(f"stream: of device {stream.device_index}, expected {index}")
             with torch.cuda.stream(stream):
                 yield stream.cuda_stream
 

@@ -234,6 +234,23 @@ def test_handle_zero_is_the_default_stream(monkeypatch):
             assert used == handle and made[-1].cuda_stream == handle
 
 
+def test_stream_of_another_device_is_refused(monkeypatch):
+    """Its handle would be used with this device current, and its order is not that of the tensors."""
+    import contextlib
+    import types
+
+    import torch
+    from paper_2609_26077_amd import q8
+    monkeypatch.setattr(torch.cuda, "device", lambda index: contextlib.nullcontext())
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: contextlib.nullcontext())
+    other = types.SimpleNamespace(cuda_stream=0x1230, device_index=1, device=torch.device("cuda:1"))
+    with pytest.raises(ValueError, match="stream: of device 1, expected 0"):
+        with q8._switched(0, other):
+            pass
+    with q8._switched(1, other) as used:
+        assert used == 0x1230
+
+
 # ---- the reference itself ------------------------------------------------------------------
 def test_reference_gradient_is_the_losses_derivative():
     """The norm's gradient formula against central differences, binary64."""
