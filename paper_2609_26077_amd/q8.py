@@ -10,9 +10,9 @@ they stand for.
 Codes are int8 [rows][pitch(cols)], zero past cols; scales are float32 [rows],
 or [rows][pitch / 128] for a checkpoint.  Allocation, checks and marshalling
 only: the arithmetic happens in the library's HIP kernels.  Every call runs on
-`stream` (default: torch's current one) and allocates its outputs there; an
-object's workspace, which its first backward call allocates, belongs to the
-calls of one stream.
+`stream` (default: torch's current one) and allocates its outputs and its
+workspace there; an object holds sizes only, so any streams and threads may use
+it at once.
 """
 from __future__ import annotations
 
@@ -188,7 +188,6 @@ class RMSNormQ8:
         P = pitch(self.cols)
         self._x, self._q, self._s = (self.rows, self.cols), (self.rows, P), (self.rows, P // GROUP)   # shapes
         self.scratch_bytes = fmm_rmsnorm_q8_backward_scratch_size(self.desc)
-        self.scratch = None     # the backward pass's workspace, from its first call on
 
     def forward(self, x, residual=None, gain=None, checkpoint=False, inplace=False, stream=None) -> NormOutput:
         """h = x + residual; codes and scales of h / rms(h) * gain.  checkpoint:
@@ -243,14 +242,14 @@ class RMSNormQ8:
 
         def call(handle):
             dx = torch.empty_like(dy)
-            dgain = None
+            dgain = scratch = None
             if need_gain:
                 dgain = torch.empty(self.cols, dtype=torch.float32, device=dev)
-                if self.scratch is None:
-                    self.scratch = torch.empty(max(self.scratch_bytes, 16), dtype=torch.uint8, device=dev)
+                if self.scratch_bytes:
+                    scratch = torch.empty(self.scratch_bytes, dtype=torch.uint8, device=dev)
             _check(_lib.fmm_rmsnorm_q8_backward(self.desc, dy.data_ptr(), _ptr(dh), _ptr(h), _ptr(codes), _ptr(scales),
                                                 rstd.data_ptr(), _ptr(gain), dx.data_ptr(), _ptr(dgain),
-                                                _ptr(self.scratch), self.scratch_bytes, handle),
+                                                _ptr(scratch), self.scratch_bytes, handle),
                    "fmm_rmsnorm_q8_backward")
             return dx, dgain
 
@@ -266,7 +265,7 @@ class LinearQ8:
         self.device = _device(device)
         self.desc = fmm_q8_desc(self.M, self.N, self.K, _type(dtype))
         self._a, self._w = (self.M, pitch(self.K)), (self.N, pitch(self.K))   # shapes
-        self.grad_scratch_bytes, self.grad_scratch = 0, None     # the backward pass's, from its first call on
+        self.grad_scratch_bytes = None     # the backward pass's workspace: from its first call on
 
     def _operands(self, a, sa, w, sw):
         dev = self.device
@@ -302,15 +301,15 @@ class LinearQ8:
         self._operands(a, sa, w, sw)
 
         def call(handle):
-            if self.grad_scratch is None:
+            if self.grad_scratch_bytes is None:
                 self.grad_scratch_bytes = fmm_q8_linear_backward_scratch_size(self.desc)
-                self.grad_scratch = torch.empty(max(self.grad_scratch_bytes, 256), dtype=torch.uint8, device=dev)
+            scratch = torch.empty(self.grad_scratch_bytes, dtype=torch.uint8, device=dev)
             dx = torch.empty(self.M, self.K, dtype=self.dtype, device=dev) if need_x else None
             dw = torch.empty(self.N, self.K, dtype=self.dtype, device=dev) if need_w else None
             dbias = torch.empty(self.N, dtype=torch.float32, device=dev) if bias else None
             _check(_lib.fmm_q8_linear_backward(self.desc, dy.data_ptr(), a.data_ptr(), sa.data_ptr(), w.data_ptr(),
                                                sw.data_ptr(), _ptr(dx), _ptr(dw), _ptr(dbias),
-                                               self.grad_scratch.data_ptr(), self.grad_scratch_bytes, handle),
+                                               scratch.data_ptr(), self.grad_scratch_bytes, handle),
                    "fmm_q8_linear_backward")
             return dx, dw, dbias
 

@@ -635,3 +635,30 @@ def test_default_stream_by_handle(torch, q8):
     x.copy_(late)
     got = lin.matmul(*q8.quantize(x, stream=0), w, sw, stream=0).clone()
     assert torch.equal(got, want)
+
+
+def test_one_object_on_two_streams(torch, q8):
+    """Gradients of the same objects, under way on two streams at once."""
+    M, N, K = 4100, 130, 520
+    norm, lin = q8.RMSNormQ8(M, K, torch.bfloat16), q8.LinearQ8(M, N, K, torch.bfloat16)
+    w, sw = codes(torch, 5, N, K)
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    inputs = []
+    for s in (10, 20):
+        a, sa = codes(torch, s, M, K)
+        h, dh = randn(torch, s + 1, M, K, t="bf16"), randn(torch, s + 2, M, K, t="bf16")
+        inputs.append((randn(torch, s + 3, M, N, t="bf16", scale=0.1), a, sa, h, dh, randn(torch, s + 4, M).abs() + 0.5))
+
+    def both(dy, a, sa, h, dh, rstd, stream=None):
+        return (*norm.backward(dh, rstd, h=h, stream=stream), *lin.backward(dy, a, sa, w, sw, bias=True, stream=stream))
+
+    want = [both(*i) for i in inputs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(8):
+        for k in (0, 1):
+            got[k].append(both(*inputs[k], stream=sides[k]))
+    torch.cuda.synchronize()
+    for k in (0, 1):
+        for out in got[k]:
+            assert all(torch.equal(a, b) for a, b in zip(out, want[k]))

@@ -251,6 +251,40 @@ def test_stream_of_another_device_is_refused(monkeypatch):
         assert used == 0x1230
 
 
+def test_every_backward_call_has_a_workspace_of_its_own(monkeypatch):
+    """Calls of one object on two streams may run at once: what one adds up must not
+    pass through the other's memory.  (Outputs are held here, so that memory that is
+    the same was handed out once.)"""
+    import torch
+    from paper_2609_26077_amd import q8
+    seen, held = [], []
+    fresh = torch.empty
+
+    class Library:
+        def fmm_rmsnorm_q8_backward(self, *a):
+            seen.append((a[-3], a[-2]))
+            return 0
+        fmm_q8_linear_backward = fmm_rmsnorm_q8_backward
+
+    def empty(*shape, **kw):
+        held.append(fresh(*shape, **kw))
+        return held[-1]
+
+    monkeypatch.setattr(q8, "_lib", Library())
+    monkeypatch.setattr(q8, "_run", lambda device, stream, call, *tensors: call(stream))
+    monkeypatch.setattr(torch, "empty", empty)
+    n, lin = (q8.RMSNormQ8(2000, 300, torch.float32, device="cpu"), q8.LinearQ8(2000, 6, 300, torch.float32, device="cpu"))
+    x, r = torch.zeros((2000, 300)), torch.zeros(2000)
+    q, w, sw, dy = (torch.zeros((2000, 384), dtype=torch.int8), torch.zeros((6, 384), dtype=torch.int8), torch.zeros(6),
+                    torch.zeros((2000, 6)))
+    for call in (lambda s: n.backward(x, r, h=x, stream=s), lambda s: lin.backward(dy, q, r, w, sw, stream=s)):
+        del seen[:]
+        call(1)
+        call(2)
+        (one, bytes1), (two, bytes2) = seen
+        assert bytes1 == bytes2 > 0 and one and two and one != two
+
+
 # ---- the reference itself ------------------------------------------------------------------
 def test_reference_gradient_is_the_losses_derivative():
     """The norm's gradient formula against central differences, binary64."""
