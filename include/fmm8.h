@@ -524,7 +524,9 @@ int fmm_q8_matmul(const fmm_q8_desc *desc, const int8_t *dA, const float *dSa, c
  * (dW, dSw; dA, dSa) with it.  The products run on the bf16 matrix cores with
  * fp32 sums.  FMM_BF16 rounds the values q s to bf16, its dY being exact; FMM_F16
  * carries dY s to 16 bits and FMM_F32 to 24, the codes being exact, at two and
- * three times the matrix work.  M and N at most 2^22, and M N, M K and N K at
+ * three times the matrix work.  Where bf16 would round a finite value to infinity,
+ * it is bf16's largest number (FMM_BF16), or parts of one sign that add up to it (the
+ * others).  M and N at most 2^22, and M N, M K and N K at
  * most 2^34 (FMM_ERR_UNSUPPORTED).  dScratch: 256-byte aligned, at least the
  * size below (FMM_ERR_WORKSPACE). */
 int fmm_q8_linear_backward_scratch_size(const fmm_q8_desc *desc, size_t *bytes);

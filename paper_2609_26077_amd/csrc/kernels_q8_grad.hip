@@ -50,15 +50,26 @@ struct LayoutArgs {
 __device__ __forceinline__ uint16_t bf16_bits(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
 __device__ __forceinline__ float bf16_value(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
 
-// part p of v: bf16 of what the parts before leave
+// part p of v: bf16 of what the parts before leave.  A finite v that bf16 rounds to
+// infinity is cut towards zero instead, and what is left of it too: the parts' sum
+// then never exceeds v on its way.
 template <int P>
 __device__ __forceinline__ void split_parts(float v, uint16_t (&out)[P]) {
+  const uint32_t mag = __float_as_uint(v) & 0x7fffffffu;
+  const bool cut = mag >= 0x7f7f8000u && mag < 0x7f800000u;
 #pragma unroll
   for (int p = 0; p < P; ++p) {
-    out[p] = bf16_bits(v);
+    out[p] = cut ? (uint16_t)(__float_as_uint(v) >> 16) : bf16_bits(v);
     const float r = v - bf16_value(out[p]);
     v = (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u ? 0.0f : r;   // (nothing is left of NaN and infinity)
   }
+}
+
+// q s.  A row quantized from the largest float has codes whose q s lies between it and
+// 2^128 and is rounded to infinity: that is the largest float here.
+__device__ __forceinline__ float code_value(float q, float s) {
+  const float v = q * s;
+  return fabsf(q * (0.5f * s)) <= 0x1p127f ? fminf(fmaxf(v, -0x1.fffffep127f), 0x1.fffffep127f) : v;
 }
 
 // 16 consecutive values of each part to dst + part * plane
@@ -143,7 +154,7 @@ __global__ __launch_bounds__(256) void layout_kernel(LayoutArgs g) {
     const u32x4 w = *reinterpret_cast<const u32x4 *>(q + (r0 + r) * g.pitch + k0 + c);
     const float s = P == 1 ? sc[r0 + r] : 1.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = (float)(int8_t)(w[i / 4] >> (8 * (i % 4))) * s;
+    for (int i = 0; i < 16; ++i) v[i] = code_value((float)(int8_t)(w[i / 4] >> (8 * (i % 4))), s);
   } else {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = 0.0f;

@@ -662,3 +662,37 @@ def test_one_object_on_two_streams(torch, q8):
     for k in (0, 1):
         for out in got[k]:
             assert all(torch.equal(a, b) for a, b in zip(out, want[k]))
+
+
+@pytest.mark.parametrize("t", TYPES)
+def test_linear_gradient_near_the_largest_float(torch, q8, t):
+    """Finite products with a scale, past what bfloat16 rounds to infinity: a sum with
+    one term of 1 or -1 times such a value is that value, and one of zeros is zero."""
+    M, N, K = 70, 66, 100
+    big = float(np.finfo(np.float32).max)
+    a, sa = codes(torch, 1, M, K)
+    w, sw = codes(torch, 2, N, K)
+    a[:, :K] = torch.sign(a[:, :K])
+    w[:, :K] = torch.sign(w[:, :K])
+    sa[:], sw[:] = 1, 1
+    dy = torch.zeros((M, N), dtype=dtype_of(torch, t), device="cuda")
+    if t == "fp32":
+        dy[5, 9], dy[64, 65], dy[6, 10] = big, -big, 3.397e38
+    elif t == "fp16":
+        dy[5, 9], dy[64, 65], dy[6, 10] = 65504.0, -65504.0, 65504.0
+        sa[[5, 64, 6]] = sw[[9, 65, 10]] = 5.19e33          # (times 65504: 3.39966e38)
+    else:
+        dy[5, 9], dy[64, 65], dy[6, 10] = 1.0, -1.0, 1.0
+        a[5, :K] = w[9, :K] = 127
+        a[64, :K] = w[65, :K] = -127
+        sa[[5, 64, 6]] = sw[[9, 65, 10]] = big / 127
+    lin = q8.LinearQ8(M, N, K, dy.dtype)
+    dx, dw, _ = lin.backward(dy, a, sa, w, sw)
+    for got, P, Q, name in ((dx, f64(dy) * f64(sw), f64(w)[:, :K], "dX"), (dw, (f64(dy) * f64(sa)[:, None]).T, f64(a)[:, :K], "dW")):
+        want = P @ Q
+        r = ROUNDING[t] + 2.0 ** -19 + 2.0 ** -7 * (t == "bf16")       # (bfloat16's largest number is 2^-8 below its power of two)
+        if t == "fp16":                                                # what fp16 holds of it
+            want = np.where(np.abs(want) > 65520, np.copysign(np.inf, want), want)
+            assert np.array_equal(f64(got), want), name
+        else:
+            within(f64(got), want, r * np.abs(want) + ref.HALF_ULP[t] * np.abs(want), name)
