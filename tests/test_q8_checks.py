@@ -251,12 +251,14 @@ def test_stream_of_another_device_is_refused(monkeypatch):
         assert used == 0x1230
 
 
-def test_every_backward_call_has_a_workspace_of_its_own(monkeypatch):
-    """Calls of one object on two streams may run at once: what one adds up must not
-    pass through the other's memory.  (Outputs are held here, so that memory that is
-    the same was handed out once.)"""
+def test_backward_calls_that_may_overlap_share_no_workspace(monkeypatch):
+    """Calls of one object on two streams may run at once, and a captured call beside
+    later ones on its stream: what one adds up must not pass through the other's
+    memory.  (What is allocated is held here, so that memory that is the same was handed
+    out once.)"""
     import torch
     from paper_2609_26077_amd import q8
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     seen, held = [], []
     fresh = torch.empty
 
@@ -279,10 +281,12 @@ def test_every_backward_call_has_a_workspace_of_its_own(monkeypatch):
                     torch.zeros((2000, 6)))
     for call in (lambda s: n.backward(x, r, h=x, stream=s), lambda s: lin.backward(dy, q, r, w, sw, stream=s)):
         del seen[:]
-        call(1)
-        call(2)
-        (one, bytes1), (two, bytes2) = seen
-        assert bytes1 == bytes2 > 0 and one and two and one != two
+        for stream, capturing in ((1, False), (2, False), (1, True), (2, True), (1, False)):
+            monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing)
+            call(stream)
+        blocks, sizes = zip(*seen)
+        assert all(blocks) and len(set(blocks[:4])) == 4 and len(set(sizes)) == 1 and sizes[0] > 0
+        assert blocks[4] == blocks[0]                   # (a stream's calls are in its order: they may share)
 
 
 # ---- the reference itself ------------------------------------------------------------------
