@@ -50,22 +50,23 @@ struct LayoutArgs {
 __device__ __forceinline__ uint16_t bf16_bits(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
 __device__ __forceinline__ float bf16_value(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
 
-// part p of v: bf16 of what the parts before leave.  A finite v that bf16 rounds to
-// infinity is cut towards zero instead, and what is left of it too: the parts' sum
-// then never exceeds v on its way.
-template <int P>
+// part p of v: bf16 of what the parts before leave.  EVERY: any v, else finite ones
+// that bf16 does not round to infinity.  A finite v that it would is cut towards zero
+// instead, and what is left of it too: the parts' sum then never exceeds v on its way.
+constexpr uint32_t kFirstCut = 0x7f7f8000u;
+template <int P, bool EVERY>
 __device__ __forceinline__ void split_parts(float v, uint16_t (&out)[P]) {
   const uint32_t mag = __float_as_uint(v) & 0x7fffffffu;
-  const bool cut = mag >= 0x7f7f8000u && mag < 0x7f800000u;
+  const bool finite = mag < 0x7f800000u, cut = finite && mag >= kFirstCut;
 #pragma unroll
   for (int p = 0; p < P; ++p) {
-    out[p] = cut ? (uint16_t)(__float_as_uint(v) >> 16) : bf16_bits(v);
+    out[p] = EVERY && cut ? (uint16_t)(__float_as_uint(v) >> 16) : bf16_bits(v);
     const float r = v - bf16_value(out[p]);
-    v = (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u ? 0.0f : r;   // (nothing is left of NaN and infinity)
+    v = EVERY && !finite ? 0.0f : r;   // (nothing is left of NaN and infinity)
   }
 }
 
-// q s.  A row quantized from the largest float has codes whose q s lies between it and
+// q s of large scales.  A row quantized from the largest float has codes whose q s lies between it and
 // 2^128 and is rounded to infinity: that is the largest float here.
 __device__ __forceinline__ float code_value(float q, float s) {
   const float v = q * s;
@@ -76,8 +77,16 @@ __device__ __forceinline__ float code_value(float q, float s) {
 template <int P>
 __device__ __forceinline__ void store_parts(const float (&v)[16], uint16_t *dst, int64_t plane) {
   uint16_t b[16][P];
+  uint32_t most = 0;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) split_parts<P>(v[i], b[i]);
+  for (int i = 0; i < 16; ++i) most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
+  if (most < kFirstCut) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) split_parts<P, false>(v[i], b[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) split_parts<P, true>(v[i], b[i]);
+  }
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     u32x4 o[2];
@@ -152,9 +161,16 @@ __global__ __launch_bounds__(256) void layout_kernel(LayoutArgs g) {
   float v[16];
   if (r0 + r < rows) {
     const u32x4 w = *reinterpret_cast<const u32x4 *>(q + (r0 + r) * g.pitch + k0 + c);
-    const float s = P == 1 ? sc[r0 + r] : 1.0f;
+    const float s = P == 1 ? sc[r0 + r] : 1.0f;   // (else it goes to dY)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = code_value((float)(int8_t)(w[i / 4] >> (8 * (i % 4))), s);
+    for (int i = 0; i < 16; ++i) v[i] = (float)(int8_t)(w[i / 4] >> (8 * (i % 4)));
+    if (P == 1 && fabsf(s) > 0x1p119f) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] = code_value(v[i], s);
+    } else if (P == 1) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] *= s;
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = 0.0f;
