@@ -22,8 +22,7 @@ __global__ __launch_bounds__(T::kThreads, 2) void matmul_kernel(GemmProblem g) {
 // a time, and waits for nobody until the waves' (exact) sums meet in LDS at the
 // end.  v_mfma_i32_16x16x64_i8 takes 16 bytes a lane of 16 rows; rows in LDS are
 // swizzled as in the tile kernel.  Loading the operands' lanes straight from
-// memory instead touches half lines: 64 tokens of 8192 x 8192 took 43 us (20 here),
-// one token 16.4 (14).
+// memory instead touches half lines: one token of 8192 x 8192 took 16.4 us (14).
 template <int MT, int NT, int W, int D, int OUT>
 __global__ __launch_bounds__(64 * W) void few_tokens_kernel(GemmProblem g) {
   constexpr int kPiece = 16 * (MT + NT) * kStep;
@@ -132,20 +131,26 @@ void launch_few(const GemmProblem &g, hipStream_t s) {
 // The shapes of workgroup the product comes in, and what each takes: t = start +
 // max(chain pieces, work pieces groups / CUs) us, pieces being the 128-byte steps
 // that a wave walks.  `chain` is a piece's time where the chip is not full, `work`
-// where it is.  Fitted on 390 shapes (1 to 32768 tokens, 1 to 65536 channels) by what
-// the choice then costs: the one it picks is 1.2% slower than the fastest on average,
-// 28% at worst (fitted on half of them, 2.2% and 30% on the others).  Each is the
-// fastest somewhere, us (128+: where there are no more tiles than CUs, the 128 tile with
-// a longer ring):
-//   tokens x channels x channels   16x16  32x32  48x32  64x32  64x64   128+    128    256
-//   1 x 8192 x 8192                13.8   15.9   16.1   16.6   20.6   32.3   53.6   89.8
-//   64 x 4096 x 4096               10.3    6.2    7.0    7.7    9.0   14.9   19.7   39.5
-//   64 x 8192 x 8192               42.6   26.8   28.8   20.7   25.5   35.2   53.8   92.7
-//   256 x 1024 x 8192              13.3    8.9    8.6   10.3   14.1   24.3   33.0   71.0
-//   256 x 4096 x 4096              31.3   16.8   15.3   14.3    9.7   15.3   19.4   39.2
-//   2048 x 1024 x 8192             86.4   48.3   46.6   43.5   29.1   28.2   35.4   71.5
-//   2048 x 4096 x 4096              196    106   89.1   98.8   62.9      -   37.4   46.6
-//   2048 x 8192 x 8192             1140    622    450    458    239      -    148    124
+// where it is.  On 1400 shapes (1 to 32768 tokens, 1 to 65536 channels) the one that it
+// picks is 1.1% slower than the fastest on average, with operands that the last-level
+// cache holds or with weights from HBM; 4% of the shapes are off by more than 10%, the
+// worst (8749 x 65 x 447, 7.1 us for 4.8) by 50%.  On decode's shapes, up to 384 tokens,
+// 2% on average.  Each shape is the fastest somewhere, us (operands in the last-level
+// cache / weights from HBM; 128+: where there are no more tiles than CUs, the 128 tile
+// with a longer ring):
+//   tokens x channels x channels   16x16      32x32      48x32      64x64      128+       128        256
+//   1 x 8192 x 8192                13.0/17.8  18.6/22.0  18.9/22.3  14.8/23.4  24.3/35.1  34.5/56.6  70.4/93.8
+//   48 x 7168 x 2048               8.6/9.8    5.9/7.8    5.3/7.2    6.7/8.8    9.7/12.6   12.8/17.8  23.9/29.2
+//   64 x 4096 x 4096               11.0/12.4  6.2/8.6    7.1/8.6    8.8/13.6   14.6/20.4  19.7/29.5  39.9/50.6
+//   64 x 8192 x 8192               43.0/43.4  30.4/30.7  31.2/32.2  14.9/26.1  24.6/38.1  34.7/56.6  71.3/96.6
+//   256 x 4096 x 4096              31.1/32.4  15.9/18.0  14.7/16.9  9.7/13.2   14.7/22.4  19.3/28.8  39.2/52.9
+//   1000 x 1302 x 1472             21.1/21.8  11.9/12.2  11.2/11.6  8.0/9.8    9.2/11.9   11.1/14.4  21.9/24.9
+//   3000 x 1000 x 4000             106/104    36.2/37.6  31.1/32.7  21.8/24.5  17.3/20.3  20.9/28.6  40.0/49.7
+//   2048 x 4096 x 4096             199/202    93.8/98.6  77.5/81.9  52.3/62.0  -          34.9/38.4  42.7/51.1
+//   2048 x 8192 x 8192             1167/1173  634/648    501/513    232/232    -          143/147    113/115
+// (a 64 x 32 shape was the cheapest by this rule on 1 shape in 4000 and is not kept: it
+// is the fastest by up to 30% for about 256 tokens of 2048 channels and a long contracted
+// axis, which start, chain and work do not tell from 64 x 8192 x 8192, where it is not.)
 struct Shape {
   int tm, tn, waves;            // tile, and the waves that share its contracted axis
   float start, chain, work;
@@ -153,18 +158,20 @@ struct Shape {
 };
 constexpr Shape kShapes[] = {
     {16, 16, 8, 1.7f, 0.30f, 0.57f, false}, {32, 32, 4, 2.2f, 0.37f, 0.61f, false},
-    {48, 32, 4, 2.4f, 0.58f, 0.76f, false}, {64, 32, 4, 2.6f, 0.41f, 1.2f, false},
-    {64, 64, 1, 3.2f, 0.19f, 0.28f, false}, {128, 128, 1, 3.3f, 0.45f, 0.60f, true},
-    {128, 128, 1, 3.6f, 0.47f, 0.62f, false}, {256, 256, 1, 8.7f, 1.2f, 1.8f, false},
+    {48, 32, 4, 2.4f, 0.58f, 0.76f, false}, {64, 64, 1, 3.2f, 0.19f, 0.28f, false},
+    {128, 128, 1, 3.3f, 0.45f, 0.60f, true}, {128, 128, 1, 3.6f, 0.47f, 0.62f, false},
+    {256, 256, 1, 8.7f, 1.2f, 1.8f, false},
 };
+
+constexpr int kShapeCount = sizeof(kShapes) / sizeof(kShapes[0]);
 
 // (a launch takes fewer than 2^32 threads; the largest tile stays below that by the limit on M N)
 constexpr double kMaxGroups = 1 << 22;
 
 int pick(const GemmProblem &g, int ncu) {
-  int best = 7;
+  int best = kShapeCount - 1;
   double least = 1e300;
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < kShapeCount; ++i) {
     const Shape &p = kShapes[i];
     const double groups = (double)((g.M + p.tm - 1) / p.tm) * ((g.N + p.tn - 1) / p.tn);
     if (groups > kMaxGroups || (p.one && groups > ncu)) continue;
@@ -192,10 +199,9 @@ void launch(const GemmProblem &g, int ncu, hipStream_t s) {
     case 0: return launch_few<1, 1, 8, 2, OUT>(g, s);
     case 1: return launch_few<2, 2, 4, 2, OUT>(g, s);
     case 2: return launch_few<3, 2, 4, 2, OUT>(g, s);
-    case 3: return launch_few<4, 2, 4, 2, OUT>(g, s);
-    case 4: return launch_tiles<Tile64, OUT>(g, s);
-    case 5: return launch_tiles<Tile128Ahead, OUT>(g, s);
-    case 6: return launch_tiles<Tile128, OUT>(g, s);
+    case 3: return launch_tiles<Tile64, OUT>(g, s);
+    case 4: return launch_tiles<Tile128Ahead, OUT>(g, s);
+    case 5: return launch_tiles<Tile128, OUT>(g, s);
     default: return launch_tiles<Tile256, OUT>(g, s);
   }
 }
