@@ -516,6 +516,11 @@ typedef struct {
 int fmm_q8_matmul(const fmm_q8_desc *desc, const int8_t *dA, const float *dSa, const int8_t *dW, const float *dSw,
                   const float *dBias, void *dC, void *stream);
 
+/* The kernel that fmm_q8_matmul launches for these sizes on the current device, with
+ * its tile, e.g. "matmul_kernel 256x256" ("ahead": the 128 tile with a longer ring).  A
+ * static string; NULL for sizes that the call refuses. */
+const char *fmm_q8_matmul_kernel(const fmm_q8_desc *desc);
+
 /* The gradients of that product from dDy = d loss / d C (M x N, 16-byte aligned)
  * and the layer's 8-bit operands, the checkpoint of its input among them:
  *   dDx (M x K) = (dDy * sw) qw,  dDw (N x K) = (dDy * sa)^T qa,
@@ -533,6 +538,11 @@ int fmm_q8_linear_backward_scratch_size(const fmm_q8_desc *desc, size_t *bytes);
 int fmm_q8_linear_backward(const fmm_q8_desc *desc, const void *dDy, const int8_t *dA, const float *dSa,
                            const int8_t *dW, const float *dSw, void *dDx, void *dDw, float *dDbias, void *dScratch,
                            size_t scratch_bytes, void *stream);
+
+/* The kernel of its products, as above, with the tiles of dDx and dDw, e.g.
+ * "grad_kernel 64x64 128x128"; runs (may be NULL) receives how many runs the
+ * contracted axis of each is split into.  want_dx, want_dw: which of them are wanted. */
+const char *fmm_q8_linear_backward_kernel(const fmm_q8_desc *desc, int want_dx, int want_dw, int32_t runs[2]);
 
 /* ---- misc ---------------------------------------------------------------- */
 

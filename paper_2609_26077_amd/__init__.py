@@ -149,8 +149,11 @@ _SIGS = {
     "fmm_rmsnorm_q8_backward_scratch_size": (ctypes.c_int, [_norm_p, _size_p]),
     "fmm_rmsnorm_q8_backward": (ctypes.c_int, [_norm_p] + [_vp] * 10 + [ctypes.c_size_t, _vp]),
     "fmm_q8_matmul": (ctypes.c_int, [_q8_p] + [_vp] * 7),
+    "fmm_q8_matmul_kernel": (ctypes.c_char_p, [_q8_p]),
     "fmm_q8_linear_backward_scratch_size": (ctypes.c_int, [_q8_p, _size_p]),
     "fmm_q8_linear_backward": (ctypes.c_int, [_q8_p] + [_vp] * 9 + [ctypes.c_size_t, _vp]),
+    "fmm_q8_linear_backward_kernel": (ctypes.c_char_p, [_q8_p, ctypes.c_int, ctypes.c_int,
+                                                        ctypes.POINTER(ctypes.c_int32)]),
     "fmm_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "fmm_last_error_detail": (ctypes.c_char_p, []),
     "fmm_device_check": (ctypes.c_int, [ctypes.c_int]),
@@ -535,6 +538,12 @@ def fmm_q8_matmul(desc: fmm_q8_desc, A, sa, W, sw, bias, C, stream=None) -> None
            "fmm_q8_matmul")
 
 
+def fmm_q8_matmul_kernel(desc: fmm_q8_desc):
+    """The kernel that a product of these sizes launches, with its tile (None if they are refused)."""
+    name = _lib.fmm_q8_matmul_kernel(desc)
+    return name and name.decode()
+
+
 def fmm_q8_linear_backward_scratch_size(desc: fmm_q8_desc) -> int:
     n = ctypes.c_size_t()
     _check(_lib.fmm_q8_linear_backward_scratch_size(desc, ctypes.byref(n)), "fmm_q8_linear_backward_scratch_size")
@@ -546,6 +555,13 @@ def fmm_q8_linear_backward(desc: fmm_q8_desc, dY, A, sa, W, sw, dX, dW, dbias, s
     _check(_lib.fmm_q8_linear_backward(desc, _ptr(dY), _ptr(A), _ptr(sa), _ptr(W), _ptr(sw), _ptr(dX), _ptr(dW),
                                        _ptr(dbias), _ptr(scratch), scratch_bytes, _stream(stream)),
            "fmm_q8_linear_backward")
+
+
+def fmm_q8_linear_backward_kernel(desc: fmm_q8_desc, want_dx=True, want_dw=True):
+    """(kernel of the gradients' products with the tiles of dX and dW, (runs of dX, of dW)), or None if refused."""
+    runs = (ctypes.c_int32 * 2)()
+    name = _lib.fmm_q8_linear_backward_kernel(desc, int(want_dx), int(want_dw), runs)
+    return name and (name.decode(), tuple(runs))
 
 
 def fmm_status_string(status: int) -> str:

@@ -399,6 +399,19 @@ size_t grad_scratch(int type, int64_t M, int64_t N, int64_t K, int ncu) {
   return layout_of(type, M, N, K).total + align256(sums);
 }
 
+const char *linear_grad_kernel_name(int type, int64_t M, int64_t N, int64_t K, bool dx, bool dw, int ncu, int32_t *runs) {
+  static const char *const small[2][2] = {{"grad_kernel 64x64 64x64", "grad_kernel 64x64 128x128"},
+                                          {"grad_kernel 128x128 64x64", "grad_kernel 128x128 128x128"}};
+  const Cut c = cut_of(type, M, N, K, dx, dw, ncu);
+  if (runs) {
+    runs[0] = c.splits[0];
+    runs[1] = c.splits[1];
+  }
+  if (c.tile[0] == 2) return "grad_kernel 256x256 256x256";
+  if (c.tile[0] == 3) return "grad_kernel 128x128 128x128 ahead";
+  return small[c.tile[0]][c.tile[1]];
+}
+
 int launch_linear_grad(int type, const GradArgs &a, int ncu, void *stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (type == FMM_F32) return launch<FMM_F32>(a, ncu, s);

@@ -208,6 +208,13 @@ void launch(const GemmProblem &g, int ncu, hipStream_t s) {
 
 }  // namespace
 
+const char *matmul_kernel_name(const GemmProblem &p, int ncu) {
+  static const char *const names[kShapeCount] = {
+      "few_tokens_kernel 16x16", "few_tokens_kernel 32x32",      "few_tokens_kernel 48x32", "matmul_kernel 64x64",
+      "matmul_kernel 128x128 ahead", "matmul_kernel 128x128", "matmul_kernel 256x256"};
+  return names[pick(p, ncu)];
+}
+
 int launch_matmul(int type, const GemmProblem &p, int ncu, void *stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (type == FMM_F32) launch<FMM_F32>(p, ncu, s);

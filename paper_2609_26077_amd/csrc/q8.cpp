@@ -44,6 +44,17 @@ int check_grad(const fmm_q8_desc *d) {
   return d->M * d->N > most || d->M * d->K > most || d->N * d->K > most ? FMM_ERR_UNSUPPORTED : FMM_OK;
 }
 
+// the int8 product's sizes
+GemmProblem product(const fmm_q8_desc &d) {
+  GemmProblem p = {};
+  p.pitch_a = p.pitch_b = pitch_of(d.K);
+  p.M = (int)d.M;
+  p.N = (int)d.N;
+  p.steps = (int)(pitch_of(d.K) / kGroup);
+  p.parts = 1;
+  return p;
+}
+
 size_t norm_grad_scratch(const fmm_norm_desc &d) {
   return d.rows == 0 ? 0 : sizeof(float) * (size_t)norm_grad_partials(d.type, d.rows, d.cols) * (size_t)d.cols;
 }
@@ -123,6 +134,11 @@ int fmm_rmsnorm_q8_backward(const fmm_norm_desc *desc, const void *dDy, const vo
   return fmm::hip_status(launch_rmsnorm_grad(desc->type, a, stream));
 }
 
+const char *fmm_q8_matmul_kernel(const fmm_q8_desc *desc) {
+  if (check_linear(desc) != FMM_OK) return nullptr;
+  return matmul_kernel_name(product(*desc), fmm::compute_units());
+}
+
 int fmm_q8_matmul(const fmm_q8_desc *desc, const int8_t *dA, const float *dSa, const int8_t *dW, const float *dSw,
                   const float *dBias, void *dC, void *stream) {
   const int st = check_linear(desc);
@@ -131,18 +147,13 @@ int fmm_q8_matmul(const fmm_q8_desc *desc, const int8_t *dA, const float *dSa, c
   if (M == 0 || N == 0) return FMM_OK;
   if (K > 0 && (!good(dA, 16) || !good(dW, 16))) return FMM_ERR_ARG;
   if (!good(dSa, 4) || !good(dSw, 4) || !fine(dBias, 4) || !good(dC, type_bytes(desc->type))) return FMM_ERR_ARG;
-  GemmProblem p = {};
+  GemmProblem p = product(*desc);
   p.A = reinterpret_cast<const uint8_t *>(dA);
   p.B = reinterpret_cast<const uint8_t *>(dW);
-  p.pitch_a = p.pitch_b = pitch_of(K);
   p.sa = dSa;
   p.sw = dSw;
   p.bias = dBias;
   p.C = dC;
-  p.M = (int)M;
-  p.N = (int)N;
-  p.steps = (int)(pitch_of(K) / kGroup);
-  p.parts = 1;
   return fmm::hip_status(launch_matmul(desc->type, p, fmm::compute_units(), stream));
 }
 
@@ -177,6 +188,12 @@ int fmm_q8_linear_backward(const fmm_q8_desc *desc, const void *dDy, const int8_
   if (ws != FMM_OK) return ws;
   GradArgs a = {dDy, dA, dW, dSa, dSw, dDx, dDw, dDbias, static_cast<uint8_t *>(dScratch), M, N, K};
   return fmm::hip_status(launch_linear_grad(desc->type, a, ncu, stream));
+}
+
+const char *fmm_q8_linear_backward_kernel(const fmm_q8_desc *desc, int want_dx, int want_dw, int32_t runs[2]) {
+  if (check_grad(desc) != FMM_OK) return nullptr;
+  const int64_t M = desc->M, N = desc->N, K = desc->K;
+  return linear_grad_kernel_name(desc->type, M, N, K, want_dx && M * K > 0, want_dw && N * K > 0, fmm::compute_units(), runs);
 }
 
 }  // extern "C"

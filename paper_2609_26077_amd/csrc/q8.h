@@ -75,6 +75,7 @@ struct GemmProblem {
 };
 
 int launch_matmul(int type, const GemmProblem &p, int ncu, void *stream);
+const char *matmul_kernel_name(const GemmProblem &p, int ncu);
 
 struct GradArgs {
   const void *dy;
@@ -86,6 +87,7 @@ struct GradArgs {
   int64_t M, N, K;
 };
 size_t grad_scratch(int type, int64_t M, int64_t N, int64_t K, int ncu);
+const char *linear_grad_kernel_name(int type, int64_t M, int64_t N, int64_t K, bool dx, bool dw, int ncu, int32_t *runs);
 int launch_linear_grad(int type, const GradArgs &a, int ncu, void *stream);
 
 }  // namespace q8

@@ -696,3 +696,146 @@ def test_linear_gradient_near_the_largest_float(torch, q8, t):
             assert np.array_equal(f64(got), want), name
         else:
             within(f64(got), want, r * np.abs(want) + ref.HALF_ULP[t] * np.abs(want), name)
+
+
+# ---- every kernel that the rules choose --------------------------------------------------------------
+# The shapes are chosen for a device of 256 compute units; each test first asserts which
+# kernel its sizes take (and a CPU test that the lists hold every kernel).  The references are products in binary64 on the GPU: sums of
+# integers, exact in any order, for the int8 product.
+def check_product(torch, q8, t, kernel, M, N, K):
+    import paper_2609_26077_amd as fm
+    lin = q8.LinearQ8(M, N, K, dtype_of(torch, t))
+    assert fm.fmm_q8_matmul_kernel(lin.desc) == kernel
+    a, sa = codes(torch, M, M, K)
+    w, sw = codes(torch, N + 1, N, K)
+    b = randn(torch, 3, N, scale=5.0)
+    C = lin.matmul(a, sa, w, sw, b)
+    wt, b64 = w[:, :K].double().t().contiguous(), b.double()
+    for m in range(0, M, 2048):
+        rows = slice(m, m + 2048)
+        p = torch.mm(a[rows, :K].double(), wt) * sa[rows, None].double() * sw.double()
+        want = p + b64
+        bound = 4 * U * p.abs() + 2 * U * b64.abs() + ref.HALF_ULP[t] * want.abs() + ref.SMALLEST[t]
+        err = (C[rows].double() - want).abs()
+        assert bool((err <= bound).all()), f"rows from {m}: {float((err / bound).max()):.3g} of the bound"
+
+
+PRODUCTS = (
+    # (pieces of a wave: from none to enough that each slot is filled again)
+    [("few_tokens_kernel 16x16", 13, 333, K) for K in (100, 1100, 2100, 4300)]
+    + [("few_tokens_kernel 32x32", *s) for s in ((2140, 33, 430), (23, 4651, 560), (23, 4651, 1100), (2237, 33, 2700))]
+    + [("few_tokens_kernel 48x32", *s) for s in ((37, 6201, 100), (36, 4651, 560), (48, 7168, 2048), (47, 4651, 1500),
+                                                 (4177, 33, 2700))]
+    + [("matmul_kernel 64x64", *s) for s in ((49, 8200, 100), (49, 9300, 200), (101, 6201, 300), (101, 6201, 430),
+                                             (49, 7203, 560), (49, 7200, 700), (49, 8200, 800), (51, 6203, 2700))]
+    + [("matmul_kernel 128x128 ahead", *s) for s in ((200, 8200, 100), (200, 8200, 200), (199, 7201, 300), (153, 9301, 430),
+                                                     (140, 9300, 560), (141, 9303, 700), (140, 9300, 2700))]
+    + [("matmul_kernel 128x128", *s) for s in ((782, 4651, 100), (394, 8200, 200), (395, 8201, 300), (394, 8203, 430),
+                                               (394, 8200, 560), (391, 8207, 700), (394, 8200, 2700))]
+    + [("matmul_kernel 256x256", *s) for s in ((20001, 9003, 100), (9001, 9003, 200), (9001, 9003, 300), (9001, 8963, 430),
+                                               (5001, 5003, 560), (3498, 6203, 700), (4096, 4096, 1000), (1946, 4651, 2700))])
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("kernel,M,N,K", PRODUCTS)
+def test_each_product_kernel(torch, q8, t, kernel, M, N, K):
+    """Each workgroup shape over one step of the contracted axis and many, with ragged edges."""
+    check_product(torch, q8, t, kernel, M, N, K)
+
+
+# kernel, runs of dX and dW (None: whatever they are), sizes, what is wanted; each for the types named
+GRADIENTS = (
+    [("grad_kernel 64x64 64x64", *r) for r in (
+        ((1, 1), (33, 35, 17), (1, 1), TYPES), ((8, 2), (200, 700, 17), (1, 1), ["fp32"]),
+        ((4, 2), (200, 700, 17), (1, 1), ["fp16"]), ((1, 16), (1700, 33, 17), (0, 1), ["fp32"]),
+        ((1, 8), (1700, 33, 17), (0, 1), ["fp16"]), ((1, 4), (1700, 33, 17), (0, 1), ["bf16"]),
+        ((16, 1), (33, 1700, 17), (1, 0), ["fp32"]), ((8, 1), (33, 1700, 17), (1, 0), ["fp16"]),
+        ((4, 1), (33, 1700, 17), (1, 0), ["bf16"]))]
+    + [("grad_kernel 64x64 128x128", *r) for r in (
+        ((1, 1), (130, 333, 3000), (1, 1), ["fp32"]), ((8, 1), (33, 2600, 1302), (1, 1), ["fp32"]),
+        ((1, 8), (5200, 2050, 130), (0, 1), ["fp32"]), ((1, 1), (70, 1700, 3000), (1, 1), ["bf16"]),
+        ((4, 1), (33, 5200, 2100), (1, 1), ["bf16"]), ((1, 4), (4100, 4100, 130), (0, 1), ["fp16"]),
+        ((2, 1), (33, 1700, 3000), (1, 1), ["fp16"]))]
+    + [("grad_kernel 128x128 64x64", *r) for r in (
+        ((1, 1), (333, 130, 3000), (1, 1), ["fp32"]), ((1, 8), (2600, 33, 1302), (1, 1), ["fp32"]),
+        ((1, 4), (5200, 33, 2100), (1, 1), ["bf16"]), ((1, 2), (1700, 33, 3000), (1, 1), ["fp16"]),
+        ((8, 1), (2050, 5200, 130), (1, 0), ["fp32"]), ((4, 1), (4100, 4100, 130), (1, 0), ["fp16"]))]
+    + [("grad_kernel 128x128 128x128", runs, s, (1, 1), t) for runs, s, t in (
+        ((1, 1), (333, 520, 4160), TYPES), ((1, 8), (2050, 70, 1302), ["fp32"]), ((8, 1), (70, 2050, 1302), ["fp32"]),
+        ((4, 2), (2050, 4100, 130), ["fp32"]), ((4, 4), (4100, 4100, 70), ["fp16"]), ((8, 1), (70, 5200, 1302), ["bf16"]))]
+    + [("grad_kernel 128x128 128x128 ahead", *r) for r in (
+        ((1, 1), (200, 201, 4160), (1, 1), TYPES), ((16, 1), (70, 2050, 520), (1, 1), ["fp32"]),
+        ((8, 8), (1700, 2050, 17), (1, 1), ["fp32"]), ((8, 4), (1700, 4100, 17), (1, 1), ["fp16"]),
+        ((8, 2), (1290, 5200, 70), (1, 1), ["bf16"]), ((1, 16), (4100, 1700, 17), (0, 1), ["fp32"]),
+        ((1, 1), (2050, 33, 1302), (1, 0), ["fp16", "fp32"]))]
+    + [("grad_kernel 256x256 256x256", *r) for r in (
+        ((1, 1), (1000, 1290, 4161), (1, 1), ["fp32"]), ((1, 1), (640, 4096, 4160), (0, 1), TYPES),
+        ((1, 1), (4100, 333, 3001), (1, 0), ["fp16", "fp32"]), ((1, 8), (5200, 130, 3000), (1, 1), ["fp32"]),
+        ((8, 1), (130, 5200, 3000), (1, 1), ["fp32"]), ((1, 1), (4096, 4096, 4096), (1, 1), TYPES),
+        ((1, 1), (4033, 4031, 3903), (1, 1), TYPES))])
+GRADIENTS = [(t, kernel, runs, s, w) for kernel, runs, s, w, types in GRADIENTS for t in types]
+
+
+def gradient_plan(torch, q8, t, kernel, runs, sizes, wanted):
+    import paper_2609_26077_amd as fm
+    lin = q8.LinearQ8(*sizes, dtype_of(torch, t))
+    assert fm.fmm_q8_linear_backward_kernel(lin.desc, *wanted) == (kernel, runs)
+    return lin
+
+
+@pytest.mark.parametrize("t,kernel,runs,sizes,wanted", GRADIENTS)
+def test_each_gradient_kernel(torch, q8, t, kernel, runs, sizes, wanted):
+    """Dense codes, to the bound of the module's head."""
+    lin = gradient_plan(torch, q8, t, kernel, runs, sizes, wanted)
+    M, N, K = sizes
+    a, sa = codes(torch, 1, M, K)
+    w, sw = codes(torch, 2, N, K)
+    dy = randn(torch, 3, M, N, t=t, scale=0.1)
+    dx, dw, db = lin.backward(dy, a, sa, w, sw, need_x=bool(wanted[0]), need_w=bool(wanted[1]), bias=True)
+    D, A, W = dy.double(), a[:, :K].double() * sa[:, None].double(), w[:, :K].double() * sw[:, None].double()
+    r = ROUNDING[t] + 2.0 ** -19
+    for got, P, Q, name in ((dx, D, W, "dX"), (dw, D.t().contiguous(), A, "dW")):
+        if got is None:
+            continue
+        want, S = torch.mm(P, Q), torch.mm(P.abs(), Q.abs())
+        bound = (r + P.shape[1] * U) * S + ref.HALF_ULP[t] * want.abs() + ref.SMALLEST[t]
+        err = (got.double() - want).abs()
+        assert bool((err <= bound).all()), f"{name}: {float((err / bound).max()):.3g} of the bound"
+    within(f64(db), f64(D.sum(dim=0)), (M + 4) * U * f64(D.abs().sum(dim=0)), "dbias")
+
+
+@pytest.mark.parametrize("t,kernel,runs,sizes,wanted", GRADIENTS)
+def test_each_part_of_a_gradient_counts(torch, q8, t, kernel, runs, sizes, wanted):
+    """Codes with one entry a column: an output is one term, dY s q, which every part of
+    dY s has to reach, wherever along the contracted axis it is.  The factors are such
+    that the parts hold all of dY s (24 bits for fp32, 16 for fp16; bf16's q s has 8) and
+    that the term is exact in fp32: outputs are equal to it, rounded once."""
+    lin = gradient_plan(torch, q8, t, kernel, runs, sizes, wanted)
+    M, N, K = sizes
+    g = torch.Generator().manual_seed(7)
+
+    def pick(values, *shape):
+        return torch.tensor(values, dtype=torch.float64)[torch.randint(0, len(values), shape, generator=g)]
+
+    def one_hot(rows):
+        at, q = torch.randint(0, rows, (K,), generator=g), pick([-128, -64, -4, -2, -1, 1, 2, 8, 32, 64], K)
+        full = torch.zeros((rows, ref.pitch(K)), dtype=torch.int8)
+        full[at, torch.arange(K)] = q.to(torch.int8)
+        return full.cuda(), at.cuda(), q.cuda()
+
+    powers = [2.0 ** e for e in range(-3, 4)]
+    scales = powers if t != "fp16" else [m / 32 for m in range(17, 32, 2)]     # (fp16: 11 bits of dY, 5 of s)
+    if t == "fp32":
+        dy = (torch.randint(-2 ** 24 + 1, 2 ** 24, (M, N), generator=g) | 1).double() * 2.0 ** -20
+    else:
+        bits = 11 if t == "fp16" else 8
+        dy = (torch.randint(2 ** (bits - 1), 2 ** bits, (M, N), generator=g) | 1).double() * 2.0 ** -bits * pick([-1, 1], M, N)
+    dy, sa, sw = dy.cuda(), pick(scales, M).cuda(), pick(scales, N).cuda()
+    a, m, qa = one_hot(M)
+    w, n, qw = one_hot(N)
+    dt = dtype_of(torch, t)
+    dx, dw, _ = lin.backward(dy.to(dt), a, sa.float(), w, sw.float(), need_x=bool(wanted[0]), need_w=bool(wanted[1]))
+    if dx is not None:
+        assert torch.equal(dx, ((dy * sw)[:, n] * qw).float().to(dt))
+    if dw is not None:
+        assert torch.equal(dw, ((dy * sa[:, None])[m].t() * qa).float().to(dt))

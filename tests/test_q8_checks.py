@@ -124,6 +124,32 @@ def test_linear_backward_refuses(fm):
     assert call(dx=None, dw=None, db=None, dy=None) == fm.FMM_OK
 
 
+def test_kernels_are_named_and_each_is_tested(fm):
+    """The kernels that sizes take, over a range of sizes, against the GPU tests' lists."""
+    import test_gpu_q8 as gpu
+    sizes = (1, 10, 40, 130, 520, 1030, 2100, 5000, 9000, 20001)
+    types = {"fp32": 0, "bf16": 1, "fp16": 2}
+    products, gradients = set(), set()
+    for M in sizes:
+        for N in sizes:
+            for K in (1, 200, 560, 2100, 8200):
+                products.add(fm.fmm_q8_matmul_kernel(fm.fmm_q8_desc(M, N, K, 1)))
+                for t in range(3):
+                    for want in ((1, 1), (1, 0), (0, 1)):
+                        kernel, runs = fm.fmm_q8_linear_backward_kernel(fm.fmm_q8_desc(M, N, K, t), *want)
+                        gradients.add(kernel)
+                        assert all(1 <= r <= 16 for r in runs)
+    assert products == {c[0] for c in gpu.PRODUCTS} and gradients == {c[1] for c in gpu.GRADIENTS}
+    for kernel, M, N, K in gpu.PRODUCTS:
+        assert fm.fmm_q8_matmul_kernel(fm.fmm_q8_desc(M, N, K, 1)) == kernel, (M, N, K)
+    for t, kernel, runs, s, want in gpu.GRADIENTS:
+        assert fm.fmm_q8_linear_backward_kernel(fm.fmm_q8_desc(*s, types[t]), *want) == (kernel, runs), (t, s)
+    for bad in ((-1, 4, 4, 0), (4, 4, 131072, 0), (4, 4, 4, 3)):
+        assert fm.fmm_q8_matmul_kernel(fm.fmm_q8_desc(*bad)) is None
+        assert fm.fmm_q8_linear_backward_kernel(fm.fmm_q8_desc(*bad)) is None
+    assert fm.fmm_q8_matmul_kernel(None) is None and fm.fmm_q8_linear_backward_kernel(None) is None
+
+
 # ---- the torch wrappers -----------------------------------------------------------------
 def _objects(device="cpu"):
     import torch
