@@ -839,3 +839,52 @@ def test_each_part_of_a_gradient_counts(torch, q8, t, kernel, runs, sizes, wante
         assert torch.equal(dx, ((dy * sw)[:, n] * qw).float().to(dt))
     if dw is not None:
         assert torch.equal(dw, ((dy * sa[:, None])[m].t() * qa).float().to(dt))
+
+
+# ---- the norm over many rows ------------------------------------------------------------------------
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("source", ["h", "saved"])
+@pytest.mark.parametrize("rows,cols", [
+    # 768 workgroups of 256 threads (16-bit types; 512 for fp32), 8 rows and more for each, the last ones fewer
+    (8192, 1300), (6500, 4095), (6144, 2049),
+    # 512 workgroups, three rows for each and more; 512 and 1024 threads a row: 256 and 128 workgroups
+    (1700, 3001), (2011, 1500), (1000, 6001), (700, 12001),
+    # four rows a workgroup at once, 512 and 768 workgroups
+    (9003, 700), (26001, 300), (25001, 520)])
+def test_norm_gradient_of_many_rows(torch, q8, t, source, rows, cols):
+    """Workgroups that walk many rows, to the bounds of the module's head; the reference in binary64 on the GPU."""
+    n, x, g, o, dy, dh = norm_case(torch, q8, t, rows, cols)
+    if source == "h":
+        h, given = x.double(), {"h": x}
+    else:
+        h = (o.saved_codes.view(rows, -1, 128).double() * o.saved_scales[:, :, None].double()).view(rows, -1)[:, :cols]
+        given = {"saved": (o.saved_codes, o.saved_scales)}
+    dx, dgain = n.backward(dy, o.rstd, g, dh=dh, **given)
+    r = o.rstd[:, None].double()
+    xh, d = h * r, dy.double()
+    w = d * g.double()
+    c = (w * xh).mean(dim=1, keepdim=True)
+    want = r * (w - xh * c) + dh.double()
+    terms = r * (w.abs() + xh.abs() * (w * xh).abs().mean(dim=1, keepdim=True)) + dh.double().abs()
+    err, bound = (dx.double() - want).abs(), 80 * U * terms + ref.HALF_ULP[t] * want.abs() + ref.SMALLEST[t]
+    assert bool((err <= bound).all()), f"dx: {float((err / bound).max()):.3g} of the bound"
+    within(f64(dgain), f64((d * xh).sum(dim=0)), (rows + 16) * U * f64((d * xh).abs().sum(dim=0)), "dgain")
+    again, again_g = n.backward(dy, o.rstd, g, dh=dh, **given)
+    assert torch.equal(again, dx) and torch.equal(again_g, dgain)
+
+
+@pytest.mark.parametrize("rows,cols", [((1 << 20) + 5, 1100), ((1 << 22) + 7, 72)])
+def test_rows_beyond_a_launch(torch, q8, rows, cols):
+    """More rows than a launch has places for: workgroups go on to further rows, whose
+    results are those of the same rows in calls of their own."""
+    x = torch.randn((rows, cols), generator=torch.Generator("cuda").manual_seed(1), device="cuda", dtype=torch.bfloat16)
+    gain = 1 + randn(torch, 2, cols, t="bf16", scale=0.1)
+    q, s = q8.quantize(x)
+    o = q8.RMSNormQ8(rows, cols, x.dtype).forward(x, x, gain, checkpoint=True)
+    for r0 in range(0, rows, 1 << 19):
+        part = x[r0:r0 + (1 << 19)]
+        want_q, want_s = q8.quantize(part)
+        assert torch.equal(q[r0:r0 + len(part)], want_q) and torch.equal(s[r0:r0 + len(part)], want_s)
+        want = q8.RMSNormQ8(len(part), cols, x.dtype).forward(part, part, gain, checkpoint=True)
+        for got, v in zip(o, want):
+            assert torch.equal(got[r0:r0 + len(part)], v)
