@@ -481,9 +481,12 @@ typedef struct {
  * dH (may be NULL) receives h rounded to the type, dCodes / dScales the codes of
  * y, dRstd [rows] rstd, and dSaved / dSavedScales (both NULL or neither) the
  * checkpoint of h.  The codes are those of the row h gain (the factor rstd is
- * common to the row, and multiplies the scale only).  dResidual and dGain may be
- * NULL (0 and 1).  dH may be dX or dResidual (FMM_ERR_UNSUPPORTED for rows of
- * more than 32768 columns, which are read twice). */
+ * common to the row, and multiplies the scale only).  There and in the checkpoint
+ * 2^-118 takes the place of 1e-12, but for rows and groups that are zero: where eps is
+ * small, y is of order 1 however small h is.  (Squares are fp32: rows with magnitudes
+ * past 1e17 may have rstd 0, and ones below 1e-18 with eps = 0 lose digits of it.)
+ * dResidual and dGain may be NULL (0 and 1).  dH may be dX or dResidual
+ * (FMM_ERR_UNSUPPORTED for rows of more than 32768 columns, which are read twice). */
 int fmm_rmsnorm_q8(const fmm_norm_desc *desc, const void *dX, const void *dResidual, const void *dGain, void *dH,
                    int8_t *dCodes, float *dScales, int8_t *dSaved, float *dSavedScales, float *dRstd, void *stream);
 

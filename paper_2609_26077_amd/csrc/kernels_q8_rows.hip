@@ -7,11 +7,14 @@
 // from the same registers.
 //
 //   v_j = x_j (quantize) or h_j g_j with h = x + res in fp32 (norm)
-//   a = max(amax |v|, 1e-12),  q_j = rne(v_j (127 / a)),  s = a / 127
+//   a = max(amax |v|, floor),  q_j = rne(v_j (127 / a)),  s = a / 127
 //   norm: rstd = (mean h^2 + eps)^-1/2, and the stored scale is s rstd: the
 //   factor rstd of y = h rstd g is common to the row, so it cancels in the
 //   codes, which therefore do not depend on the order the squares are summed in.
 //   The checkpoint of h: the same rule over each group of 128 columns.
+//   The floor is 1e-12 for a row to quantize, and for one that is zero.  In the norm
+//   it is 2^-118, the least power of two whose 127 / a is far from infinity: rstd
+//   makes rows of any size ones of order 1.
 //
 // A magnitude is compared by its bits, where NaN exceeds infinity exceeds every
 // finite value: a row (or group) that holds one of the two gets scale NaN and
@@ -48,10 +51,11 @@ struct RowScale {
   float s;         // a / 127, NaN where the row holds NaN or infinity
   uint32_t keep;   // all ones, or zero there
 };
+template <bool NORM>
 __device__ __forceinline__ RowScale row_scale(uint32_t amax_bits) {
   RowScale k;
   const bool bad = amax_bits >= kInfBits;
-  const float a = bad ? 1.0f : fmaxf(__uint_as_float(amax_bits), 1e-12f);
+  const float a = bad ? 1.0f : fmaxf(__uint_as_float(amax_bits), NORM && amax_bits ? 0x1p-118f : 1e-12f);
   k.r = 127.0f / a;
   k.s = bad ? __uint_as_float(0x7fc00000u) : a / 127.0f;
   k.keep = bad ? 0u : ~0u;
@@ -105,7 +109,7 @@ __device__ __forceinline__ void save_chunk(const float (&h)[8], int8_t *codes, f
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) m = max(m, mag(h[i]));
-  const RowScale k = row_scale(max16(m));
+  const RowScale k = row_scale<true>(max16(m));
   if (col < pitch) {
     *reinterpret_cast<u32x2 *>(codes + col) = codes_of(h, k);
     if ((threadIdx.x & 15) == 0) scales[col / kGroup] = k.s;
@@ -177,7 +181,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rows_kernel(RowArgs a) 
 #pragma unroll
       for (int i = 0; i < 8; ++i) m = max(m, mag(h[c][i]));
     reduce_row<TPR>(sum, m, turn);
-    const RowScale k = row_scale(m);
+    const RowScale k = row_scale<NORM>(m);
     if (live) {
 #pragma unroll
       for (int c = 0; c < C; ++c) {
@@ -241,7 +245,7 @@ __global__ __launch_bounds__(1024) void long_rows_kernel(RowArgs a) {
       for (int i = 0; i < 8; ++i) m = max(m, mag(h[i]));
     }
     reduce_row<1024>(sum, m, turn);
-    const RowScale k = row_scale(m);
+    const RowScale k = row_scale<NORM>(m);
     for (int64_t col = 8 * (int64_t)threadIdx.x; col < a.pitch; col += 8 * 1024) {
       float h[8];
       chunk(col, h);

@@ -888,3 +888,29 @@ def test_rows_beyond_a_launch(torch, q8, rows, cols):
         want = q8.RMSNormQ8(len(part), cols, x.dtype).forward(part, part, gain, checkpoint=True)
         for got, v in zip(o, want):
             assert torch.equal(got[r0:r0 + len(part)], v)
+
+
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(5, 300), (600, 4096), (3, 33000)])
+def test_norm_of_small_rows(torch, q8, t, rows, cols):
+    """Rows far below 1e-12, eps 0: y is of order 1 and its codes, and the checkpoint's of h, are the nearest
+    multiples of a 127th of the largest magnitude, to the bar of the codes' rule; so is a gradient from them."""
+    size = 10.0 ** torch.linspace(-10, -17, rows)
+    x = (randn(torch, 1, rows, cols).cpu() * size[:, None]).to(dtype_of(torch, t)).cuda()
+    g = 1 + randn(torch, 2, cols, t=t, scale=0.2)
+    n = q8.RMSNormQ8(rows, cols, x.dtype, eps=0.0)
+    o = n.forward(x, None, g, checkpoint=True)
+    h = f64(x)
+    rstd = (h ** 2).mean(axis=1) ** -0.5
+    within(f64(o.rstd), rstd, 68 * U * rstd, "rstd")
+    y = h * rstd[:, None] * f64(g)
+    amax = np.abs(y).max(axis=1)
+    within(f64(o.scales), amax / 127, 76 * U * amax / 127, "scales")
+    got = ref.values(o.codes.cpu().numpy(), f64(o.scales), cols)
+    within(got, y, ((0.5 + 2.0 ** -15) * f64(o.scales) + 80 * U * amax)[:, None], "half a step of y")
+    P = ref.pitch(cols)
+    groups = np.pad(h, ((0, 0), (0, P - cols))).reshape(rows, -1, 128)
+    want = np.abs(groups).max(axis=2) / 127
+    within(f64(o.saved_scales), want, 2 * U * want, "the checkpoint's scales")
+    kept = ref.values(o.saved_codes.cpu().numpy(), f64(o.saved_scales), cols)
+    within(kept, h, np.repeat((0.5 + 2.0 ** -15) * f64(o.saved_scales), 128, axis=1)[:, :cols], "half a step of h")
