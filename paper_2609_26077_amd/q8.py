@@ -122,8 +122,9 @@ def _run(device, stream, call, *tensors):
     """call(stream handle), on the device and the stream.  A stream that the
     caller names may not be the one the inputs were allocated on: the allocator
     is told, so that it does not hand out their memory before the call is done.
-    A kernel that is handed host memory faults, so nothing else gets past here."""
-    if device.type != "cuda":
+    A kernel that is handed host memory faults, so nothing else gets past here (the
+    tensors are known to be on `device`; the first is never None)."""
+    if not tensors[0].is_cuda:
         raise ValueError(f"device {device}, expected a GPU")
     index = device.index
     if stream is None and torch.cuda.current_device() == index:
