@@ -51,6 +51,9 @@ class _Workspace:
     def __init__(self):
         self.lock, self.blocks = Lock(), {}
 
+    def __reduce__(self):       # a copy of an object starts without one
+        return _Workspace, ()
+
     def get(self, handle, nbytes, device):
         if torch.cuda.is_current_stream_capturing():
             return torch.empty(nbytes, dtype=torch.uint8, device=device)

@@ -238,6 +238,19 @@ def test_wrappers_refuse_host_memory(monkeypatch, stream):
             call()
 
 
+def test_objects_can_be_copied_and_pickled():
+    """As part of a model that is: the copy has the sizes, and a workspace of its own."""
+    import copy
+    import pickle
+    _, q8, n, lin = _objects("cpu")
+    for x in (n, lin):
+        for y in (copy.deepcopy(x), pickle.loads(pickle.dumps(x))):
+            assert type(y) is type(x) and y.dtype is x.dtype and y.device == x.device
+            assert bytes(y.desc) == bytes(x.desc)
+            held = [v for v in vars(y).values() if isinstance(v, q8._Workspace)]
+            assert len(held) == 1 and held[0] not in vars(x).values() and not held[0].blocks
+
+
 def test_handle_zero_is_the_default_stream(monkeypatch):
     """torch's own default stream has the handle 0, which a caller may pass on; torch
     makes of ExternalStream(0) a stream of its pool."""
