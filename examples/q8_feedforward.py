@@ -27,6 +27,9 @@ import torch  # noqa: E402
 from paper_2609_26077_amd import q8  # noqa: E402
 
 
+KEPT_PLANS = 8
+
+
 class FeedForward:
     """The layer's weights, and its forward and backward passes for any number of tokens."""
 
@@ -45,11 +48,17 @@ class FeedForward:
         self.gain_in = self.gain.to(self.dtype)
 
     def _plan(self, tokens):
-        if tokens not in self.plans:
-            self.plans[tokens] = (q8.RMSNormQ8(tokens, self.width, self.dtype, device=self.device),
-                                  q8.LinearQ8(tokens, self.hidden, self.width, self.dtype, device=self.device),
-                                  q8.LinearQ8(tokens, self.width, self.hidden, self.dtype, device=self.device))
-        return self.plans[tokens]
+        """The operators for this many tokens.  Those of the last few counts are kept, as
+        each that a backward pass came to holds a workspace."""
+        plan = self.plans.pop(tokens, None)
+        if plan is None:
+            plan = (q8.RMSNormQ8(tokens, self.width, self.dtype, device=self.device),
+                    q8.LinearQ8(tokens, self.hidden, self.width, self.dtype, device=self.device),
+                    q8.LinearQ8(tokens, self.width, self.hidden, self.dtype, device=self.device))
+            if len(self.plans) == KEPT_PLANS:
+                del self.plans[next(iter(self.plans))]      # the one that was used longest ago
+        self.plans[tokens] = plan
+        return plan
 
     def forward(self, x, residual, train=False):
         """(out, h, what backward needs or None)"""

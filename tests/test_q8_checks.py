@@ -328,6 +328,19 @@ def test_backward_calls_that_may_overlap_share_no_workspace(monkeypatch):
         assert blocks[4] == blocks[0]                   # (a stream's calls are in its order: they may share)
 
 
+def test_example_keeps_few_plans():
+    """A prompt may have any number of tokens; what is kept for each must not pile up."""
+    import torch
+    from examples import q8_feedforward as example
+    layer = example.FeedForward.__new__(example.FeedForward)
+    layer.width, layer.hidden, layer.dtype, layer.device, layer.plans = 256, 512, torch.bfloat16, "cpu", {}
+    one = layer._plan(1)
+    for tokens in range(2, 100):
+        assert layer._plan(tokens) is layer._plan(tokens) and layer._plan(1) is one
+        assert len(layer.plans) <= example.KEPT_PLANS
+    assert layer._plan(2)[0].rows == 2
+
+
 # ---- the reference itself ------------------------------------------------------------------
 def test_reference_gradient_is_the_losses_derivative():
     """The norm's gradient formula against central differences, binary64."""
