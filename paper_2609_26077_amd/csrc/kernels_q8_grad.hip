@@ -13,9 +13,11 @@
 //
 // Two launches, or three.  The first lays the operands out along the contracted axes
 // (transposes through LDS, converted on the way, padded with zeros to the
-// product's 64-position step) and leaves dY's column sums by 64-row tiles; it
-// moves about 14 bytes for each element of dY and the codes, a tenth of the
-// products' time.  The second runs both products' tiles and adds up the column
+// product's 64-position step) and leaves dY's column sums by 64-row tiles.  It moves
+// 3 bytes a code (1 in, 2 out) and, for an element of dY, 4 bytes in bf16 (6 where
+// N is no multiple of 64: dY by rows as well), 10 in fp16 and 16 in fp32: 470 MB in 95
+// of 910 us for 8192 x 8192 x 4096 bf16, 16 MB in 6.4 of 17 for 256 x 2048 x 2048, 31 MB
+// in 10.4 of 41 for 1000 x 1302 x 1472 fp32.  The second runs both products' tiles and adds up the column
 // sums.  Where a product has few tiles and a long axis, its tiles' axis is split
 // into runs, and the third adds the runs' sums.
 #include <hip/hip_runtime.h>
@@ -269,13 +271,16 @@ struct Cut {
 // t = max(start + chain steps of a run, of either; start + work of both / CUs) us,
 // a product's work being its tile's `work` times steps and tiles; runs cost a launch
 // and the traffic of their sums besides.  The form is the int8 product's (a step moves
-// and multiplies as much), the constants the best of six sets on 80 shapes, each with
-// either product and with both: 1.3% over the best of the six on average, 20% at worst.
+// and multiplies as much).  Against all cuts (up to 24 of them a shape, drawn where
+// there are more) on 1918 shapes of the three types, with either product and with both:
+// 3.6% over the fastest on average, more than 10% on 13% of them, 59% at worst (11874 x
+// 323 x 4468 fp16, 358 us for 225 with dW in four runs: dW's tiles come after dX's, so
+// that a long chain of theirs begins late, which the cost does not know).
 // Without runs few tiles with a long axis leave most of the chip idle: 8192 tokens of
 // 512 x 512 channels 42 -> 32 us, of 1024 x 1024 87 -> 65 to 69.  A tile for each, not
 // one for both: 2000 tokens of 300 x 2000 in fp16 37.6 -> 32.1.  The longer ring where
 // each CU has a workgroup at most: 1000 x 1302 x 1472 fp32 49 -> 43, 2048^3 bf16 54 ->
-// 47; 13436 tokens of 2023 x 124, the worst of the 80, 69 -> 74.
+// 47; but 13436 tokens of 2023 x 124 69 -> 74.
 Cut cut_of(const int64_t (&m)[2], const int64_t (&n)[2], const int64_t (&steps)[2], int ncu) {
   constexpr int kEdge[4] = {64, 128, 256, 128};
   constexpr double kStart[4] = {3.2, 4.5, 7.5, 4.0}, kChain[4] = {0.20, 0.47, 1.2, 0.36},

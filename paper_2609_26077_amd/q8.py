@@ -45,8 +45,7 @@ class _Workspace:
     call that is being captured gets a block of the graph's, since its replays may
     run beside later calls.  (A block that all objects' calls share, from the
     allocator, costs more: 256 tokens of 2048 x 2048 21 us, 17.5 where three objects
-    with their own take turns, as a write has to reach lines that every L2 still
-    holds.)"""
+    with their own take turns.)"""
 
     def __init__(self):
         self.lock, self.blocks = Lock(), {}
