@@ -148,9 +148,10 @@ void launch_few(const GemmProblem &g, hipStream_t s) {
 //   3000 x 1000 x 4000             106/104    36.2/37.6  31.1/32.7  21.8/24.5  17.3/20.3  20.9/28.6  40.0/49.7
 //   2048 x 4096 x 4096             199/202    93.8/98.6  77.5/81.9  52.3/62.0  -          34.9/38.4  42.7/51.1
 //   2048 x 8192 x 8192             1167/1173  634/648    501/513    232/232    -          143/147    113/115
-// (a 64 x 32 shape was the cheapest by this rule on 1 shape in 4000 and is not kept: it
-// is the fastest by up to 30% for about 256 tokens of 2048 channels and a long contracted
-// axis, which start, chain and work do not tell from 64 x 8192 x 8192, where it is not.)
+// (A 64 x 32 shape was the cheapest by this rule on 1 shape in 4000 and is not kept.  It
+// would be the fastest by up to 30% for about 256 tokens of 2048 channels and a long
+// contracted axis, which start, chain and work do not tell from 64 x 8192 x 8192: there
+// it takes 21.2 us for 14.9 with cached operands, 23.1 for 26.1 from HBM.)
 struct Shape {
   int tm, tn, waves;            // tile, and the waves that share its contracted axis
   float start, chain, work;
