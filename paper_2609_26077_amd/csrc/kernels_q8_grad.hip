@@ -272,7 +272,7 @@ struct Cut {
 // a product's work being its tile's `work` times steps and tiles; runs cost a launch
 // and the traffic of their sums besides.  The form is the int8 product's (a step moves
 // and multiplies as much).  Against all cuts (up to 24 of them a shape, drawn where
-// there are more) on 1918 shapes of the three types, with either product and with both:
+// there are more) on 1917 shapes of the three types, with either product and with both:
 // 3.6% over the fastest on average, more than 10% on 13% of them, 59% at worst (11874 x
 // 323 x 4468 fp16, 358 us for 225 with dW in four runs: dW's tiles come after dX's, so
 // that a long chain of theirs begins late, which the cost does not know).
