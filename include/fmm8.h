@@ -547,6 +547,96 @@ int fmm_q8_linear_backward(const fmm_q8_desc *desc, const void *dDy, const int8_
  * contracted axis of each is split into.  want_dx, want_dw: which of them are wanted. */
 const char *fmm_q8_linear_backward_kernel(const fmm_q8_desc *desc, int want_dx, int want_dw, int32_t runs[2]);
 
+/* ---- linear layers on e4m3 blocks ------------------------------------------
+ *
+ * Linear layers on e4m3 operands as they are stored, by expert or not, with 8-bit
+ * gradients; and the clipping of many gradients by their global norm.
+ *
+ * Codes.  A block is 128 columns of a row (activations, gradients) or 128 x 128 (a
+ * weight); those past the last whole block are part of one.  Its scale is
+ * 2^e, e the least integer >= -126 with a <= 448 2^e, a the largest magnitude of the
+ * block's finite values (e = 0 where a = 0); the code of x is the e4m3 number nearest
+ * x 2^-e, ties to even, and a code for NaN (0x7f, 0xff) for NaN and infinities.  Codes are one byte
+ * each, rows padded with zeros to fmm_q8_pitch(cols); scales are the bytes e + 127
+ * (E8M0), [rows][fmm_f8_scale_pitch(cols)] or, of a weight, [ceil(rows / 128)][...].  A
+ * layer of experts has its weights and their scales one after the other.  Codes from
+ * elsewhere may be used: scale bytes 1 to 254, zeros in the padding of codes, and
+ * values (code times scale) that fp32 holds.
+ *
+ * Sums.  fp32 outputs: codes and scales as bf16 on the bf16 matrix cores, fp32 sums (values
+ * below 2^-126 keep bf16's digits there).  16-bit outputs: the fp8 matrix cores, which
+ * keep 13 bits below the largest product of each group of eight, and fp32 sums.  Each result
+ * is rounded once, to nearest even.
+ *
+ * Alignment: codes and scales 16 bytes, scratch 256, others their element
+ * (FMM_ERR_ARG).  Asynchronous on `stream`; nothing is allocated on the device or
+ * synchronized, so calls may be captured into a graph; repeated calls agree bit for bit. */
+
+/* Bytes of one row of scales: ceil(cols / 128) rounded up to 16 (-1 if cols < 0). */
+int64_t fmm_f8_scale_pitch(int64_t cols);
+
+/* dCodes, dScales = the codes of the rows of dX (rows x cols, `type`), a scale for each
+ * 128 columns; of `count` weights (rows x cols each), a scale for each 128 x 128.  At most
+ * 2^30 rows, 2^22 columns and weights and, padded, 2^34 elements (FMM_ERR_UNSUPPORTED). */
+int fmm_f8_quantize(int type, int64_t rows, int64_t cols, const void *dX, uint8_t *dCodes, uint8_t *dScales, void *stream);
+int fmm_f8_quantize_weight(int type, int64_t count, int64_t rows, int64_t cols, const void *dX, uint8_t *dCodes,
+                           uint8_t *dScales, void *stream);
+
+/* dOut (count x rows x cols, `type`) = the values that codes stand for, a scale for each
+ * 1 x 128 (block_rows 1) or 128 x 128 (block_rows 128; FMM_ERR_ARG for others). */
+int fmm_f8_dequantize(int type, int64_t count, int64_t rows, int64_t cols, int block_rows, const uint8_t *dCodes,
+                      const uint8_t *dScales, void *dOut, void *stream);
+
+typedef struct {
+  /* tokens, experts (>= 1), output channels, input channels.  Each at most 2^22, 4096
+   * experts, and every matrix padded to 128 (rows for each expert) at most 2^34
+   * elements (FMM_ERR_UNSUPPORTED) */
+  int64_t rows, experts, N, K;
+  int32_t type;      /* FMM_F32, FMM_BF16 or FMM_F16: the output, or its gradient and the gradients from it */
+} fmm_f8_desc;
+
+/* dC[m] (rows x N, `type`) = A[m] W[e]^T + dBias[e], e the expert of row m: the values of
+ * the codes dA (rows x K) and dW (experts x N x K).  dOffsets (int32 [experts + 1], on the
+ * device): expert e has the rows dOffsets[e] .. dOffsets[e + 1] - 1; NULL: there is
+ * one expert, with every row.  Rows of no expert are left as they were.  Offsets count as raised to the
+ * largest before them and cut to 0 .. rows, so whatever they hold nothing outside
+ * the matrices is touched.  dBias (fp32 [experts][N]) may be NULL. */
+int fmm_f8_matmul(const fmm_f8_desc *desc, const uint8_t *dA, const uint8_t *dSa, const uint8_t *dW, const uint8_t *dSw,
+                  const int32_t *dOffsets, const float *dBias, void *dC, void *stream);
+
+/* The kernel that fmm_f8_matmul launches for these sizes on the current device, with its
+ * tile.  A static string; NULL for sizes that the call refuses. */
+const char *fmm_f8_matmul_kernel(const fmm_f8_desc *desc);
+
+/* The gradients of that product from dDy = d loss / d C (rows x N) and the operands of
+ * the forward pass, on 8-bit operands again:
+ *   dDx[m] (rows x K) = Q(dDy)[m] W[e], codes of 128 columns of a row of dDy;
+ *   dDw[e] (experts x N x K) = Q(dDy)^T Q(A) over the expert's rows, codes of 128 rows of a
+ *   column counted from the expert's first row, of dDy and of the values of dA;
+ *   dDbias[e] (fp32, experts x N) = sums of dDy's columns over the expert's rows.
+ * Experts without rows get zeros.  Any of the three may be NULL (not wanted), and the
+ * operands that only it needs with it.  dScratch: at least the size below
+ * (FMM_ERR_WORKSPACE). */
+int fmm_f8_linear_backward_scratch_size(const fmm_f8_desc *desc, size_t *bytes);
+int fmm_f8_linear_backward(const fmm_f8_desc *desc, const void *dDy, const uint8_t *dA, const uint8_t *dSa,
+                           const uint8_t *dW, const uint8_t *dSw, const int32_t *dOffsets, void *dDx, void *dDw,
+                           float *dDbias, void *dScratch, size_t scratch_bytes, void *stream);
+
+/* The kernel of its products, with the tiles of dDx and dDw; want_dx, want_dw: which are wanted. */
+const char *fmm_f8_linear_backward_kernel(const fmm_f8_desc *desc, int want_dx, int want_dw);
+
+/* Clipping by the global norm of `count` tensors (host arrays: element type, number of elements
+ * >= 0, device addresses of each, read before the call returns):
+ *   dNorm (fp32, one) = sqrt(sum of the squares of all elements), summed in binary64,
+ *   dOut[i] = dIn[i] min(1, most / (norm + 1e-6)).
+ * most >= 0.  dOut[i] may be dIn[i]; else outputs must not overlap inputs or one another.  A
+ * norm of infinity gives the factor 0, NaN gives NaN everywhere.  At most 122880 tensors
+ * and 2^42 elements (FMM_ERR_UNSUPPORTED).  dScratch: 8-byte aligned, at least the size below
+ * (FMM_ERR_WORKSPACE). */
+size_t fmm_clip_scratch_size(void);
+int fmm_clip(const int32_t *types, const int64_t *sizes, void *const *dIn, void *const *dOut, int64_t count, float most,
+             float *dNorm, void *dScratch, size_t scratch_bytes, void *stream);
+
 /* ---- misc ---------------------------------------------------------------- */
 
 const char *fmm_status_string(int status);

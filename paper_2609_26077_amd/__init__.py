@@ -98,8 +98,14 @@ class fmm_q8_desc(ctypes.Structure):
     _fields_ = [("M", ctypes.c_int64), ("N", ctypes.c_int64), ("K", ctypes.c_int64), ("type", ctypes.c_int32)]
 
 
+class fmm_f8_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("experts", ctypes.c_int64), ("N", ctypes.c_int64), ("K", ctypes.c_int64),
+                ("type", ctypes.c_int32)]
+
+
 _norm_p = ctypes.POINTER(fmm_norm_desc)
 _q8_p = ctypes.POINTER(fmm_q8_desc)
+_f8_p = ctypes.POINTER(fmm_f8_desc)
 _size_p = ctypes.POINTER(ctypes.c_size_t)
 
 _SIGS = {
@@ -154,6 +160,17 @@ _SIGS = {
     "fmm_q8_linear_backward": (ctypes.c_int, [_q8_p] + [_vp] * 9 + [ctypes.c_size_t, _vp]),
     "fmm_q8_linear_backward_kernel": (ctypes.c_char_p, [_q8_p, ctypes.c_int, ctypes.c_int,
                                                         ctypes.POINTER(ctypes.c_int32)]),
+    "fmm_f8_scale_pitch": (_i64, [_i64]),
+    "fmm_f8_quantize": (ctypes.c_int, [ctypes.c_int, _i64, _i64] + [_vp] * 4),
+    "fmm_f8_quantize_weight": (ctypes.c_int, [ctypes.c_int, _i64, _i64, _i64] + [_vp] * 4),
+    "fmm_f8_dequantize": (ctypes.c_int, [ctypes.c_int, _i64, _i64, _i64, ctypes.c_int] + [_vp] * 4),
+    "fmm_f8_matmul": (ctypes.c_int, [_f8_p] + [_vp] * 8),
+    "fmm_f8_matmul_kernel": (ctypes.c_char_p, [_f8_p]),
+    "fmm_f8_linear_backward_scratch_size": (ctypes.c_int, [_f8_p, _size_p]),
+    "fmm_f8_linear_backward": (ctypes.c_int, [_f8_p] + [_vp] * 10 + [ctypes.c_size_t, _vp]),
+    "fmm_f8_linear_backward_kernel": (ctypes.c_char_p, [_f8_p, ctypes.c_int, ctypes.c_int]),
+    "fmm_clip_scratch_size": (ctypes.c_size_t, []),
+    "fmm_clip": (ctypes.c_int, [_vp] * 4 + [_i64, ctypes.c_float, _vp, _vp, ctypes.c_size_t, _vp]),
     "fmm_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "fmm_last_error_detail": (ctypes.c_char_p, []),
     "fmm_device_check": (ctypes.c_int, [ctypes.c_int]),
@@ -562,6 +579,69 @@ def fmm_q8_linear_backward_kernel(desc: fmm_q8_desc, want_dx=True, want_dw=True)
     runs = (ctypes.c_int32 * 2)()
     name = _lib.fmm_q8_linear_backward_kernel(desc, int(want_dx), int(want_dw), runs)
     return name and (name.decode(), tuple(runs))
+
+
+# Linear layers on e4m3 blocks, and clipping (f8.py and grads.py wrap these)
+
+
+def fmm_f8_scale_pitch(cols: int) -> int:
+    return _lib.fmm_f8_scale_pitch(int(cols))
+
+
+def fmm_f8_quantize(type, rows, cols, X, codes, scales, stream=None) -> None:
+    _check(_lib.fmm_f8_quantize(type, rows, cols, _ptr(X), _ptr(codes), _ptr(scales), _stream(stream)), "fmm_f8_quantize")
+
+
+def fmm_f8_quantize_weight(type, count, rows, cols, X, codes, scales, stream=None) -> None:
+    _check(_lib.fmm_f8_quantize_weight(type, count, rows, cols, _ptr(X), _ptr(codes), _ptr(scales), _stream(stream)),
+           "fmm_f8_quantize_weight")
+
+
+def fmm_f8_dequantize(type, count, rows, cols, block_rows, codes, scales, out, stream=None) -> None:
+    _check(_lib.fmm_f8_dequantize(type, count, rows, cols, block_rows, _ptr(codes), _ptr(scales), _ptr(out),
+                                  _stream(stream)), "fmm_f8_dequantize")
+
+
+def fmm_f8_matmul(desc: fmm_f8_desc, A, sa, W, sw, offsets, bias, C, stream=None) -> None:
+    _check(_lib.fmm_f8_matmul(desc, _ptr(A), _ptr(sa), _ptr(W), _ptr(sw), _ptr(offsets), _ptr(bias), _ptr(C),
+                              _stream(stream)), "fmm_f8_matmul")
+
+
+def fmm_f8_matmul_kernel(desc: fmm_f8_desc):
+    """The kernel that a product of these sizes launches, with its tile (None if they are refused)."""
+    name = _lib.fmm_f8_matmul_kernel(desc)
+    return name and name.decode()
+
+
+def fmm_f8_linear_backward_scratch_size(desc: fmm_f8_desc) -> int:
+    n = ctypes.c_size_t()
+    _check(_lib.fmm_f8_linear_backward_scratch_size(desc, ctypes.byref(n)), "fmm_f8_linear_backward_scratch_size")
+    return n.value
+
+
+def fmm_f8_linear_backward(desc: fmm_f8_desc, dY, A, sa, W, sw, offsets, dX, dW, dbias, scratch, scratch_bytes: int,
+                           stream=None) -> None:
+    _check(_lib.fmm_f8_linear_backward(desc, _ptr(dY), _ptr(A), _ptr(sa), _ptr(W), _ptr(sw), _ptr(offsets), _ptr(dX),
+                                       _ptr(dW), _ptr(dbias), _ptr(scratch), scratch_bytes, _stream(stream)),
+           "fmm_f8_linear_backward")
+
+
+def fmm_f8_linear_backward_kernel(desc: fmm_f8_desc, want_dx=True, want_dw=True):
+    """The kernel of the gradients' products, with the tiles of dX and dW (None if they are refused)."""
+    name = _lib.fmm_f8_linear_backward_kernel(desc, int(want_dx), int(want_dw))
+    return name and name.decode()
+
+
+def fmm_clip_scratch_size() -> int:
+    return _lib.fmm_clip_scratch_size()
+
+
+def fmm_clip(types, sizes, ins, outs, most, norm, scratch, scratch_bytes: int, stream=None) -> None:
+    """types, sizes: sequences of numbers; ins, outs: of tensors."""
+    n = len(ins)
+    _check(_lib.fmm_clip((ctypes.c_int32 * n)(*types), (_i64 * n)(*sizes), (_vp * n)(*map(_ptr, ins)),
+                         (_vp * n)(*map(_ptr, outs)), n, most, _ptr(norm), _ptr(scratch), scratch_bytes,
+                         _stream(stream)), "fmm_clip")
 
 
 def fmm_status_string(status: int) -> str:

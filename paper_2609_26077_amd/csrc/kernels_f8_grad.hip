@@ -1,0 +1,304 @@
+// The gradients of the e4m3 linear layers, on e4m3 operands throughout:
+//   dX = Q(dY) W, blocks of Q(dY) along a row;  dW = Q(dY)^T Q(X), blocks of 128 rows
+// counted from the expert's first row, X being the codes of the forward pass.
+//
+// The layout pass brings every operand into rows along its contracted axis: dY
+// by rows (dyr) and by columns (dyt), X by columns (xt), W by columns (wt).  W's
+// codes move as they are, a 128 x 128 block's scale being that of its transpose;
+// X's are rounded again where the new block's scale is larger than the old one
+// (codes below 2^-15 of the block's largest).  It also leaves dY's column sums by block.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "f8_gemm.h"
+
+namespace fmm {
+namespace f8 {
+namespace {
+
+struct LayoutArgs {
+  const void *dy;
+  const uint8_t *a, *sa, *w, *sw;
+  const int32_t *offsets;
+  uint8_t *dyr, *sdyr;      // [rows][Np], [rows][spn]
+  uint8_t *dyt, *sdyt;      // [N][Bp], [N][sbp]: column 128 j is the first row of the j-th block of rows
+  uint8_t *xt, *sxt;        // [K][Bp], [K][sbp]
+  uint8_t *wt, *swt;        // [experts][K][Np], [experts][K / 128][spn]
+  float *colsum;            // [blocks][N]
+  int64_t Np, Kp, spn, spk, Bp, sbp;
+  int rows, experts, N, K;
+  int blocks, bn, bk;                // blocks of rows (at most), of N, of K
+  int jobs_dy, jobs_a, jobs_w;
+  int want_dx, want_dw, want_db;
+};
+
+// 4 x 4 bytes: words of rows to words of columns
+__device__ __forceinline__ void transpose4(uint32_t (&w)[4]) {
+  const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400), b = __builtin_amdgcn_perm(w[1], w[0], 0x07030602);
+  const uint32_t c = __builtin_amdgcn_perm(w[3], w[2], 0x05010400), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602);
+  w[0] = __builtin_amdgcn_perm(c, a, 0x05040100);
+  w[1] = __builtin_amdgcn_perm(c, a, 0x07060302);
+  w[2] = __builtin_amdgcn_perm(d, b, 0x05040100);
+  w[3] = __builtin_amdgcn_perm(d, b, 0x07060302);
+}
+
+// One 128 x 128 tile a workgroup: thread t has eight columns of rows 8 (t / 16) .. + 7.
+// The transpose goes through LDS in pieces of eight bytes (eight rows of a column);
+// piece p of column n sits at p ^ (n / 8), so that both directions spread over the banks.
+struct Tile {
+  u32x2 out[128][16];
+  uint32_t most[4][128];
+  float sum[4][128];
+};
+
+// the tile's columns n < cols to rows of dst
+__device__ __forceinline__ void store_columns(const Tile &tile, uint8_t *dst, int64_t pitch, int cols) {
+  const int t = threadIdx.x, c = t & 7;
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    const int n = 32 * p + (t >> 3), k = n >> 3;
+    if (n < cols) {
+      const u32x4 v = *reinterpret_cast<const u32x4 *>(&tile.out[n][(2 * c ^ k) & ~1]);
+      *reinterpret_cast<u32x4 *>(dst + n * pitch + 16 * c) = k & 1 ? (u32x4){v[2], v[3], v[0], v[1]} : v;
+    }
+  }
+}
+
+// codes by columns of v, and their scales to scales[n * pitch]
+__device__ __forceinline__ void columns(Tile &tile, const float (&v)[8][8], uint8_t *dst, int64_t pitch, uint8_t *scales,
+                                        int64_t scale_pitch, int cols) {
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, rg = t >> 4, cg = t & 15;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    uint32_t a = 0;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) a = max(a, magnitude(v[r][i]));
+    a = max(a, (uint32_t)__shfl_xor((int)a, 16));
+    a = max(a, (uint32_t)__shfl_xor((int)a, 32));
+    if (lane < 16) tile.most[wave][8 * cg + i] = a;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int n = 8 * cg + i;
+    const uint32_t b = scale_byte(max(max(tile.most[0][n], tile.most[1][n]), max(tile.most[2][n], tile.most[3][n])));
+    const float s = scale_value(b);
+    if (rg == 0 && n < cols) scales[n * scale_pitch] = (uint8_t)b;
+    u32x2 q;
+    q[0] = codes4(v[0][i], v[1][i], v[2][i], v[3][i], s);
+    q[1] = codes4(v[4][i], v[5][i], v[6][i], v[7][i], s);
+    tile.out[n][rg ^ cg] = q;
+  }
+  __syncthreads();
+  store_columns(tile, dst, pitch, cols);
+}
+
+template <int T>
+__global__ __launch_bounds__(256) void layout_kernel(LayoutArgs g) {
+  __shared__ Tile tile;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, rg = t >> 4, cg = t & 15;
+  int id = blockIdx.x;
+  if (id >= g.jobs_dy + g.jobs_a) {
+    // W: rows n, columns k
+    id -= g.jobs_dy + g.jobs_a;
+    const int kb = id % g.bk, nb = id / g.bk % g.bn, e = id / g.bk / g.bn;
+    const int n0 = nb * kBlock, k0 = kb * kBlock;
+    const uint8_t *src = g.w + ((int64_t)e * g.N + n0) * g.Kp + k0;
+    u32x2 q[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+      q[r] = n0 + 8 * rg + r < g.N ? *reinterpret_cast<const u32x2 *>(src + (8 * rg + r) * g.Kp + 8 * cg) : (u32x2){0, 0};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t lo[4] = {q[0][h], q[1][h], q[2][h], q[3][h]}, hi[4] = {q[4][h], q[5][h], q[6][h], q[7][h]};
+      transpose4(lo);
+      transpose4(hi);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) tile.out[8 * cg + 4 * h + i][rg ^ cg] = (u32x2){lo[i], hi[i]};
+    }
+    __syncthreads();
+    store_columns(tile, g.wt + ((int64_t)e * g.K + k0) * g.Np + n0, g.Np, g.K - k0);
+    if (t == 0) g.swt[((int64_t)e * g.bk + kb) * g.spn + nb] = g.sw[((int64_t)e * g.bn + nb) * g.spk + kb];
+    return;
+  }
+  const bool is_dy = id < g.jobs_dy;
+  if (!is_dy) id -= g.jobs_dy;
+  const int bc = is_dy ? g.bn : g.bk, block = id / bc, cb = id % bc, c0 = cb * kBlock, cols = (is_dy ? g.N : g.K) - c0;
+  Experts x(g.offsets, g.experts, g.rows, kBlock);
+  if (block >= x.total) return;
+  const Span s = x.find(block);
+  const int row0 = s.lo + (block - s.tiles) * kBlock, rows = s.hi - row0;
+  const int64_t sb = (int64_t)s.wides * kScalePad + block - s.tiles;   // the block's scales
+  float v[8][8];
+  if (is_dy) {
+    const elem_t<T> *src = static_cast<const elem_t<T> *>(g.dy) + (int64_t)(row0 + 8 * rg) * g.N + c0 + 8 * cg;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) q8::load8<T>(src + (int64_t)r * g.N, 8 * rg + r < rows ? cols - 8 * cg : 0, v[r]);
+    if (g.want_dx) {
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        uint32_t a = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a = max(a, magnitude(v[r][i]));
+        const uint32_t b = scale_byte(q8::max16(a));
+        const float sc = scale_value(b);
+        const int64_t row = row0 + 8 * rg + r;
+        if (8 * rg + r < rows) {
+          u32x2 q;
+          q[0] = codes4(v[r][0], v[r][1], v[r][2], v[r][3], sc);
+          q[1] = codes4(v[r][4], v[r][5], v[r][6], v[r][7], sc);
+          *reinterpret_cast<u32x2 *>(g.dyr + row * g.Np + c0 + 8 * cg) = q;
+          if (cg == 0) g.sdyr[row * g.spn + cb] = (uint8_t)b;
+        }
+      }
+    }
+    if (g.want_db) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float c = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) c += v[r][i];
+        c += __shfl_xor(c, 16);
+        c += __shfl_xor(c, 32);
+        if (lane < 16) tile.sum[wave][8 * cg + i] = c;
+      }
+      __syncthreads();
+      if (t < 128 && t < cols)
+        g.colsum[(int64_t)block * g.N + c0 + t] = (tile.sum[0][t] + tile.sum[1][t]) + (tile.sum[2][t] + tile.sum[3][t]);
+    }
+    if (g.want_dw)
+      columns(tile, v, g.dyt + c0 * g.Bp + (int64_t)block * kBlock, g.Bp, g.sdyt + c0 * g.sbp + sb, g.sbp, cols);
+  } else {
+    const uint8_t *src = g.a + (int64_t)(row0 + 8 * rg) * g.Kp + c0 + 8 * cg;
+    const uint8_t *scales = g.sa + (int64_t)(row0 + 8 * rg) * g.spk + cb;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      u32x2 q = {0, 0};
+      uint32_t b = 127;
+      if (8 * rg + r < rows) {
+        q = *reinterpret_cast<const u32x2 *>(src + r * g.Kp);
+        b = scales[r * g.spk];
+      }
+      values8(q, scale_value(b), v[r]);
+    }
+    columns(tile, v, g.xt + c0 * g.Bp + (int64_t)block * kBlock, g.Bp, g.sxt + c0 * g.sbp + sb, g.sbp, cols);
+  }
+}
+
+template <class E, int OUT, bool WEIGHTS>
+__global__ __launch_bounds__(256) void grad_kernel(Product g) {
+  Work w;
+  if (!work_of<64, 64, WEIGHTS>(g, blockIdx.x, OUT == FMM_F32 ? 4 : 2, w)) return;
+  const int wave = threadIdx.x >> 6;
+  gemm_tile<E, OUT, WEIGHTS>(g, w, 32 * (wave >> 1), 32 * (wave & 1));
+}
+
+__global__ __launch_bounds__(256) void bias_kernel(const int32_t *offsets, int experts, int rows, int N, const float *colsum,
+                                                   float *dbias) {
+  const int per = (N + 255) / 256, e = blockIdx.x / per, n = (blockIdx.x - e * per) * 256 + threadIdx.x;
+  Experts x(offsets, experts, rows, kBlock);
+  const Span s = x.at(e);
+  if (n >= N) return;
+  const int blocks = (s.hi - s.lo + kBlock - 1) / kBlock;
+  float c = 0.0f;
+#pragma unroll 4
+  for (int i = 0; i < blocks; ++i) c += colsum[(int64_t)(s.tiles + i) * N + n];
+  dbias[(int64_t)e * N + n] = c;
+}
+
+size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+
+struct Layout {
+  size_t dyr, sdyr, dyt, sdyt, xt, sxt, wt, swt, colsum, total;
+  int64_t blocks, Np, Bp, spn, sbp;
+};
+Layout layout_of(int64_t rows, int64_t experts, int64_t N, int64_t K) {
+  Layout l;
+  const int64_t full = std::min(experts, rows);      // experts that may have rows
+  l.blocks = rows / kBlock + full;
+  l.Np = pitch_of(N);
+  l.Bp = l.blocks * kBlock;
+  l.spn = scale_pitch_of(N);
+  l.sbp = kScalePad * (l.blocks / kScalePad + full);
+  size_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const size_t here = at;
+    at = align256(at + (size_t)bytes);
+    return here;
+  };
+  l.dyr = take(rows * l.Np);
+  l.sdyr = take(rows * l.spn);
+  l.dyt = take(N * l.Bp);
+  l.sdyt = take(N * l.sbp);
+  l.xt = take(K * l.Bp);
+  l.sxt = take(K * l.sbp);
+  l.wt = take(experts * K * l.Np);
+  l.swt = take(experts * (pitch_of(K) / kBlock) * l.spn);
+  l.colsum = take(4 * l.blocks * N);
+  l.total = at;
+  return l;
+}
+
+template <class E, int T>
+int launch(const GradArgs &a, int ncu, hipStream_t s) {
+  const Layout l = layout_of(a.rows, a.experts, a.N, a.K);
+  LayoutArgs g = {};
+  g.dy = a.dy; g.a = a.a; g.sa = a.sa; g.w = a.w; g.sw = a.sw; g.offsets = a.offsets;
+  g.dyr = a.ws + l.dyr; g.sdyr = a.ws + l.sdyr;
+  g.dyt = a.ws + l.dyt; g.sdyt = a.ws + l.sdyt;
+  g.xt = a.ws + l.xt; g.sxt = a.ws + l.sxt;
+  g.wt = a.ws + l.wt; g.swt = a.ws + l.swt;
+  g.colsum = reinterpret_cast<float *>(a.ws + l.colsum);
+  g.Np = l.Np; g.Kp = pitch_of(a.K); g.spn = l.spn; g.spk = scale_pitch_of(a.K); g.Bp = l.Bp; g.sbp = l.sbp;
+  g.rows = (int)a.rows; g.experts = (int)a.experts; g.N = (int)a.N; g.K = (int)a.K;
+  g.blocks = (int)l.blocks; g.bn = (int)(l.Np / kBlock); g.bk = (int)(g.Kp / kBlock);
+  g.want_dx = a.dx != nullptr; g.want_dw = a.dw != nullptr; g.want_db = a.dbias != nullptr;
+  g.jobs_dy = g.want_dx || g.want_dw || g.want_db ? g.blocks * g.bn : 0;
+  g.jobs_a = g.want_dw ? g.blocks * g.bk : 0;
+  g.jobs_w = g.want_dx && a.rows > 0 ? g.experts * g.bn * g.bk : 0;
+  const int jobs = g.jobs_dy + g.jobs_a + g.jobs_w;
+  if (jobs > 0) layout_kernel<T><<<dim3((unsigned)jobs), 256, 0, s>>>(g);
+
+  Product x = {};
+  x.offsets = a.offsets; x.experts = g.experts; x.rows = g.rows; x.N = g.K; x.splits = 1;
+  x.tiles_n = (g.K + 63) / 64;
+  if (a.dx && a.rows > 0) {
+    Product p = x;
+    p.a = {g.dyr, g.sdyr, g.Np, g.spn, 0, 0};
+    p.b = {g.wt, g.swt, g.Np, g.spn, a.K * g.Np, (int64_t)g.bk * g.spn};
+    p.C = a.dx; p.M = g.rows; p.steps = g.bn;
+    p.tiles_m = g.rows / 64 + std::min(g.experts, g.rows);
+    grad_kernel<E, T, true><<<dim3((unsigned)(p.tiles_m * p.tiles_n)), 256, 0, s>>>(p);
+  }
+  if (a.dw) {
+    Product p = x;
+    p.a = {g.dyt, g.sdyt, g.Bp, g.sbp, 0, 0};
+    p.b = {g.xt, g.sxt, g.Bp, g.sbp, 0, 0};
+    p.C = a.dw; p.M = g.N; p.steps = g.blocks; p.axis = 1;
+    p.tiles_m = (g.N + 63) / 64;
+    grad_kernel<E, T, false><<<dim3((unsigned)(g.experts * p.tiles_m * p.tiles_n)), 256, 0, s>>>(p);
+  }
+  if (a.dbias)
+    bias_kernel<<<dim3((unsigned)(g.experts * ((g.N + 255) / 256))), 256, 0, s>>>(a.offsets, g.experts, g.rows, g.N, g.colsum,
+                                                                                  a.dbias);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t grad_scratch(int, int64_t rows, int64_t experts, int64_t N, int64_t K, int) {
+  return layout_of(rows, experts, N, K).total;
+}
+
+const char *grad_kernel_name(int, int64_t, int64_t, int64_t, int64_t, bool, bool, int) { return "grad_kernel 64x64 64x64"; }
+
+int launch_grad(int type, const GradArgs &a, int ncu, void *stream) {
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (type == FMM_F32) return launch<F8Exact, FMM_F32>(a, ncu, s);
+  if (type == FMM_BF16) return launch<F8, FMM_BF16>(a, ncu, s);
+  return launch<F8, FMM_F16>(a, ncu, s);
+}
+
+}  // namespace f8
+}  // namespace fmm

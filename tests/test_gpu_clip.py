@@ -1,0 +1,151 @@
+"""Clipping by the global norm on the GPU against binary64.
+
+Bars: squares of fp32 values are exact in binary64 but for 2^-53 each, so the norm is off by its
+rounding to fp32, 2^-24 relative (2^-23 here, for the sums' own roundings); the factor is rounded to
+fp32 (2^-24), its product with an element to fp32 (2^-24) and to the element's type (u_T)."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+HALF_ULP = {"float32": 2.0 ** -24, "bfloat16": 2.0 ** -8, "float16": 2.0 ** -11}
+SMALLEST = {"float32": 2.0 ** -149, "bfloat16": 2.0 ** -133, "float16": 2.0 ** -24}
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    return torch
+
+
+@pytest.fixture(scope="module")
+def grads():
+    from paper_2609_26077_amd import grads
+    return grads
+
+
+def tensors(torch, sizes, dtypes, seed=0, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return [(torch.randn(n, generator=g) * scale * 10.0 ** (i % 4 - 2)).to(dtypes[i % len(dtypes)]).cuda()
+            for i, n in enumerate(sizes)]
+
+
+def check(torch, grads, ts, most, inplace):
+    up = [t.double().cpu().numpy() for t in ts]
+    want = np.sqrt(sum((u ** 2).sum() for u in up))
+    outs = [t.clone() if inplace else torch.full_like(t, 7.0) for t in ts]
+    norm = grads.clip(outs, most) if inplace else grads.clip(ts, most, out=outs)
+    assert norm.dtype == torch.float32 and norm.shape == ()
+    assert abs(float(norm) - want) <= 2.0 ** -23 * want
+    c = min(1.0, most / (want + 1e-6))
+    for u, o in zip(up, outs):
+        n = str(o.dtype).split(".")[1]
+        # (the factor's own norm is binary64: 2^-50 of it)
+        assert (np.abs(o.double().cpu().numpy() - u * c)
+                <= (HALF_ULP[n] + 2.5 * 2.0 ** -24) * np.abs(u * c) + SMALLEST[n]).all()
+        if c == 1.0:
+            assert np.array_equal(o.double().cpu().numpy(), u)
+
+
+SIZES = {"one": [1], "one large": [100003], "few": [5, 0, 16384, 16385, 7, 1], "many": [(37 * i) % 401 for i in range(300)],
+         "wide": [1 << 20, 3, 2000001, 0, 0, 99], "empty": [0, 0]}
+
+
+@pytest.mark.parametrize("inplace", [False, True])
+@pytest.mark.parametrize("types", ["float32", "bfloat16", "float16", "mixed"])
+@pytest.mark.parametrize("sizes", list(SIZES))
+@pytest.mark.parametrize("most", [0.5, 1e9, 0.0])
+def test_clip(torch, grads, sizes, types, inplace, most):
+    all_types = [torch.float32, torch.bfloat16, torch.float16]
+    dtypes = all_types if types == "mixed" else [getattr(torch, types)]
+    check(torch, grads, tensors(torch, SIZES[sizes], dtypes), most, inplace)
+
+
+@pytest.mark.parametrize("offset", [1, 3])
+def test_views_off_alignment(torch, grads, offset):
+    buf = torch.randn(50000, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).cuda()
+    parts = [buf[offset:offset + 17001], buf[20000 + offset:20000 + offset + 333].view(9, 37)]
+    rest = buf.clone()
+    check(torch, grads, parts, 0.25, False)
+    grads.clip(parts, 0.25)
+    mask = torch.ones(50000, dtype=torch.bool)
+    mask[offset:offset + 17001] = False
+    mask[20000 + offset:20000 + offset + 333] = False
+    assert torch.equal(buf.cpu()[mask], rest.cpu()[mask])
+
+
+def test_magnitudes_that_fp32_cannot_square(torch, grads):
+    for scale in (1e25, 1e-30):
+        ts = [torch.full((1000,), scale, device="cuda"), torch.full((24,), -scale, device="cuda")]
+        out = [torch.empty_like(t) for t in ts]
+        norm = grads.clip(ts, 2.0, out=out)
+        want = 32.0 * float(np.float32(scale))
+        assert abs(float(norm) - want) <= 2.0 ** -23 * want
+        c = min(1.0, 2.0 / (want + 1e-6))
+        for t, o in zip(ts, out):
+            x = float(np.float32(scale)) * c * np.sign(float(t[0]))
+            assert abs(float(o[0]) - x) <= 3 * 2.0 ** -24 * abs(x) + 2.0 ** -149 and bool((o == o[0]).all())
+
+
+def test_norms_that_are_not_finite(torch, grads):
+    for bad, zeros in ((float("inf"), True), (float("nan"), False)):
+        ts = [torch.ones(100, device="cuda"), torch.ones(33, device="cuda", dtype=torch.bfloat16)]
+        ts[1][5] = bad
+        out = [torch.empty_like(t) for t in ts]
+        norm = grads.clip(ts, 1.0, out=out)
+        assert float(norm) == bad or (np.isnan(bad) and np.isnan(float(norm)))
+        if zeros:
+            assert bool((out[0] == 0).all()) and bool(torch.isnan(out[1][5])) and int((out[1] == 0).sum()) == 32
+        else:
+            assert bool(torch.isnan(out[0]).all()) and bool(torch.isnan(out[1]).all())
+
+
+def test_repeats_and_graphs(torch, grads):
+    """Equal bit for bit from call to call, and in replays of two graphs with eager calls between."""
+    ts = tensors(torch, [(101 * i) % 5003 for i in range(150)], [torch.float32, torch.bfloat16])
+    out = [torch.empty_like(t) for t in ts]
+    norm = grads.clip(ts, 0.5, out=out)
+    want = [o.clone() for o in out]
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        o = [torch.empty_like(t) for t in ts]
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            n = grads.clip(ts, 0.5, out=o)
+        graphs.append((g, n, o))
+    for _ in range(3):
+        for g, n, o in graphs:
+            for x in o:
+                x.zero_()
+            g.replay()
+            again = grads.clip(ts, 0.5, out=out)
+            torch.cuda.synchronize()
+            assert torch.equal(n, norm) and torch.equal(again, norm)
+            assert all(torch.equal(x, y) for x, y in zip(o, want)) and all(torch.equal(x, y) for x, y in zip(out, want))
+
+
+def test_another_stream(torch, grads):
+    ts = tensors(torch, [100000, 33], [torch.float32])
+    out = [torch.empty_like(t) for t in ts]
+    want = grads.clip(ts, 0.5, out=out)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    out2 = [torch.empty_like(t) for t in ts]
+    s.wait_stream(torch.cuda.current_stream())
+    norm = grads.clip(ts, 0.5, out=out2, stream=s)
+    s.synchronize()
+    assert torch.equal(norm, want) and all(torch.equal(a, b) for a, b in zip(out, out2))
+
+
+def test_the_binding_forwards(torch, grads):
+    import paper_2609_26077_amd as fm
+    ts = tensors(torch, [1000, 5], [torch.float32])
+    out, out2 = ([torch.empty_like(t) for t in ts] for _ in range(2))
+    want = grads.clip(ts, 0.5, out=out)
+    norm = torch.empty((), device="cuda")
+    n = fm.fmm_clip_scratch_size()
+    fm.fmm_clip([fm.FMM_F32] * 2, [1000, 5], ts, out2, 0.5, norm, torch.empty(n, dtype=torch.uint8, device="cuda"), n)
+    assert torch.equal(norm, want) and all(torch.equal(a, b) for a, b in zip(out, out2))
