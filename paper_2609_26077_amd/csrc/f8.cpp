@@ -46,7 +46,7 @@ Product product(const fmm_f8_desc &d) {
   p.rows = p.M = (int)d.rows;
   p.N = (int)d.N;
   p.steps = (int)(p.a.pitch / kBlock);
-  p.splits = 1;
+  p.out_bytes = type_bytes(d.type);
   return p;
 }
 

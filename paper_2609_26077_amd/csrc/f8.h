@@ -52,10 +52,8 @@ struct Product {
   int experts, rows;         // rows: of A, or of the contracted axis
   int M, N;                  // rows of C (axis: of each C), columns
   int steps;                 // 128-byte steps of the contracted axis (axis: at most)
-  int axis;
+  int axis, out_bytes;       // out_bytes: of an element of C
   int tiles_m, tiles_n;      // (tiles_m with experts and not axis: at most)
-  int splits;                // the contracted axis in this many runs (axis, or no experts); if more
-  float *partial;            // than one, their sums go here: [splits][M][N] for each expert
 };
 
 int launch_matmul(int type, const Product &p, int ncu, void *stream);

@@ -1,17 +1,38 @@
-// The product of the e4m3 layers: C = A B^T over rows that are contiguous along
-// the contracted axis, a scale byte for each 128 of them.
+// The matrix-core product of the e4m3 layers: C = A B^T over rows that are
+// contiguous along the contracted axis, a scale byte for each 128 of them.
+//
+// Tiles, LDS rows and the ring of half-slots that global_load_lds fills are those of the
+// int8 product (q8_gemm.h): a step is 128 bytes of every row of the tile, which here is
+// one block, so a row has one scale for it.  A lane takes 32 codes of its row for
+// each half step t: the 16-byte chunks 4 t + h and 4 t + 2 + h of the row in lane half h.  Which
+// positions they are does not matter as long as both sides agree.
+//
+// A step of a wave is a chain of slots: slot (t, i) multiplies row tile i of A by the wave's row tiles of
+// B, half step t.  A's fragments are read a slot ahead, B's a half step ahead, so that a
+// 256 tile's wave holds 48 registers of them beside its 128 sums (a whole half step
+// of both ahead would take 96).  The barrier stands before the last slot.
+//
+// Scales stay out of LDS, which the ring of the larger tiles fills: a lane keeps four
+// steps' bytes of each of its rows as a word, shifted right by a byte a step.  The
+// following words are loaded at the start of the last step of four and waited for at
+// its barrier, where few of the ring's transfers are on their way.
 #pragma once
 
 #include <hip/hip_runtime.h>
 
 #include "device.h"
 #include "f8_types.h"
+#include "q8_gemm.h"
 
 namespace fmm {
 namespace f8 {
 
+using q8::kStep;
+using q8::swz128;
+using q8::v16f;
 typedef int v8i __attribute__((ext_vector_type(8)));
-typedef float v16f __attribute__((ext_vector_type(16)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+using q8::v4i;
 
 // What a workgroup has to do: a tile of C, its rows of A and B, and the steps
 // of 128 codes that it contracts.
@@ -19,7 +40,8 @@ struct Work {
   const uint8_t *a, *b, *sa, *sb;   // codes and scales of the tile's first rows, from the first step on
   int rows_a, rows_b;               // rows that exist (of the tile and past it)
   int steps;
-  void *C;                          // the tile's first output
+  void *C;                          // the matrix that the tile is of ...
+  int m0, n0, M;                    // ... its first output, and the row that ends its expert's
   const float *bias;                // of its first column, or null
 };
 
@@ -28,94 +50,348 @@ struct Work {
 // the sums keep fp32's digits, where the fp8 cores keep 13 bits below the largest
 // product of each group of eight.
 struct F8 {
-  static __device__ __forceinline__ v16f mma(v8i b, uint32_t sb, v8i a, uint32_t sa, v16f c) {
+  typedef v16f acc;
+  static constexpr bool kScaled = false;      // (the sums leave as they are)
+  typedef v8i op;
+  static __device__ __forceinline__ op prepare(v8i q, uint32_t) { return q; }
+  static __device__ __forceinline__ v16f mma(const op &b, uint32_t sb, const op &a, uint32_t sa, v16f c) {
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b, a, c, 0, 0, 0, (int)sb, 0, (int)sa);
+  }
+  static __device__ __forceinline__ v4f mma16(const op &b, uint32_t sb, const op &a, uint32_t sa, v4f c) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, c, 0, 0, 0, (int)sb, 0, (int)sa);
   }
 };
 struct F8Exact {
-  static __device__ __forceinline__ v16f mma(v8i b, uint32_t sb, v8i a, uint32_t sa, v16f c) {
-    const float fa = dev::e8m0_at(sa, 0), fb = dev::e8m0_at(sb, 0);
+  typedef v16f acc;
+  static constexpr bool kScaled = false;
+  struct op {
+    dev::v8bf v[4];
+  };
+  static __device__ __forceinline__ op prepare(v8i q, uint32_t s) {
+    op o;
+    const float f = dev::e8m0_at(s, 0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dev::dequant8((uint32_t)b[2 * i], (uint32_t)b[2 * i + 1], fb),
-                                                  dev::dequant8((uint32_t)a[2 * i], (uint32_t)a[2 * i + 1], fa), c, 0, 0, 0);
+    for (int i = 0; i < 4; ++i) o.v[i] = dev::dequant8((uint32_t)q[2 * i], (uint32_t)q[2 * i + 1], f);
+    return o;
+  }
+  static __device__ __forceinline__ v16f mma(const op &b, uint32_t, const op &a, uint32_t, v16f c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.v[i], a.v[i], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ v4f mma16(const op &b, uint32_t, const op &a, uint32_t, v4f c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.v[i], a.v[i], c, 0, 0, 0);
     return c;
   }
 };
 
-// The work of workgroup `id` (wave-uniform); false: none.
+// The work of workgroup `id` (wave-uniform); false: none.  Order as in the int8 product:
+// the ids of one XCD get a contiguous range of items, tiles run in groups of GM tile rows.
 template <int TM, int TN, bool WEIGHTS>
-__device__ __forceinline__ bool work_of(const Product &g, int id, int out_bytes, Work &w) {
+__device__ __forceinline__ bool work_of(const Product &g, int id, Work &w) {
+  constexpr int GM = TM == 256 ? 4 : 8;
   Span s;
-  int tm, tn, m0, split = 0;
+  int tm, tn, part;
   if (g.axis) {
-    const int per = g.tiles_m * g.tiles_n, e = id / (per * g.splits);
-    id -= e * per * g.splits;
-    split = id / per;
-    id -= split * per;
-    tm = id % g.tiles_m;
-    tn = id / g.tiles_m;
-    m0 = tm * TM;
+    q8::item_of<GM>(id, g.tiles_m * g.tiles_n * g.experts, g.tiles_m, g.tiles_n, tm, tn, part);
     Experts x(g.offsets, g.experts, g.rows, kBlock);
-    s = x.at(e);
+    s = x.at(part);
+    s.expert = part;
+    w.m0 = tm * TM;
+    w.M = g.M;
   } else {
     Experts x(g.offsets, g.experts, g.rows, TM);
-    tm = id / g.tiles_n;
-    tn = id % g.tiles_n;
-    if (tm >= x.total) return false;
+    if (id >= x.total * g.tiles_n) return false;
+    q8::item_of<GM>(id, x.total * g.tiles_n, x.total, g.tiles_n, tm, tn, part);
     s = x.find(tm);
-    m0 = s.lo + (tm - s.tiles) * TM;
+    w.m0 = s.lo + (tm - s.tiles) * TM;
+    w.M = s.hi;
   }
-  const int n0 = tn * TN;
+  w.n0 = tn * TN;
   const int64_t e = s.expert;
-  w.a = g.a.codes + e * g.a.expert_codes + m0 * g.a.pitch;
-  w.sa = g.a.scales + e * g.a.expert_scales + m0 * g.a.scale_pitch;
-  w.b = g.b.codes + e * g.b.expert_codes + n0 * g.b.pitch;
-  w.sb = g.b.scales + e * g.b.expert_scales + (WEIGHTS ? n0 / kBlock : n0) * g.b.scale_pitch;
-  w.rows_a = (g.axis ? g.M : s.hi) - m0;
-  w.rows_b = g.N - n0;
+  w.a = g.a.codes + e * g.a.expert_codes + w.m0 * g.a.pitch;
+  w.sa = g.a.scales + e * g.a.expert_scales + w.m0 * g.a.scale_pitch;
+  w.b = g.b.codes + e * g.b.expert_codes + w.n0 * g.b.pitch;
+  w.sb = g.b.scales + e * g.b.expert_scales + (WEIGHTS ? w.n0 / kBlock : w.n0) * g.b.scale_pitch;
+  w.rows_a = w.M - w.m0;
+  w.rows_b = g.N - w.n0;
   w.steps = g.steps;
-  int64_t row = m0;
+  w.C = g.C;
   if (g.axis) {
     w.steps = (s.hi - s.lo + kBlock - 1) / kBlock;
     w.a += (int64_t)s.tiles * kBlock;
     w.b += (int64_t)s.tiles * kBlock;
     w.sa += (int64_t)s.wides * kScalePad;
     w.sb += (int64_t)s.wides * kScalePad;
-    row += e * g.M;
+    w.C = static_cast<uint8_t *>(g.C) + e * g.M * g.N * g.out_bytes;
   }
-  w.C = static_cast<uint8_t *>(g.C) + (row * g.N + n0) * out_bytes;
-  w.bias = g.bias ? g.bias + e * g.N + n0 : nullptr;
+  w.bias = g.bias ? g.bias + e * g.N + w.n0 : nullptr;
   return true;
 }
 
-// One wave, one 32 x 32 tile, operands straight from memory.  Lane (r, h) takes 32 of
-// a row's 64 codes; which ones does not matter as long as both sides agree.
-template <class E, int OUT, bool WEIGHTS>
-__device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, int mw, int nw) {
-  const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
-  if (mw >= w.rows_a || nw >= w.rows_b) return;
-  const int ra = min(mw + r, w.rows_a - 1), rb = min(nw + r, w.rows_b - 1);
-  const uint8_t *a = w.a + ra * g.a.pitch + 32 * h, *b = w.b + rb * g.b.pitch + 32 * h;
-  const uint8_t *sa = w.sa + ra * g.a.scale_pitch, *sb = w.sb + (WEIGHTS ? rb / kBlock : rb) * g.b.scale_pitch;
-  v16f acc = {};
-  for (int s = 0; s < w.steps; ++s) {
-    const uint32_t ea = sa[s], eb = sb[s];
+template <class E, class T, int OUT, bool WEIGHTS>
+__device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4 *lds_raw) {
+  constexpr int J = T::JA, MI = T::MI, NI = T::NI, SB = WEIGHTS ? 1 : NI, Q = 2 * MI;
+  static_assert(!WEIGHTS || NI * 32 <= kBlock, "one scale of the weights for a wave's columns");
+  const uint8_t *lds = reinterpret_cast<const uint8_t *>(lds_raw);
+  const int t = threadIdx.x, lane = t & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int wm = wave / T::WN, wn = wave % T::WN;
+  const int r32 = lane & 31, h = lane >> 5;
+  const int ns = w.steps;
+
+  // scales of steps 4 i .. 4 i + 3, the first in the low byte
+  uint32_t psa[MI], psb[SB];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const v8i fa = *reinterpret_cast<const v8i *>(a + (int64_t)s * kBlock + 64 * t);
-      const v8i fb = *reinterpret_cast<const v8i *>(b + (int64_t)s * kBlock + 64 * t);
-      acc = E::mma(fb, eb, fa, ea, acc);
+  for (int i = 0; i < MI; ++i) psa[i] = (uint32_t)(min((wm * MI + i) * 32 + r32, w.rows_a - 1) * g.a.scale_pitch);
+#pragma unroll
+  for (int j = 0; j < SB; ++j) {
+    const int row = WEIGHTS ? min(wn * NI * 32, w.rows_b - 1) / kBlock : min((wn * NI + j) * 32 + r32, w.rows_b - 1);
+    psb[j] = (uint32_t)(row * g.b.scale_pitch);
+  }
+  uint32_t sa[MI], sb[SB], na[MI], nb[SB];
+  auto load_scales = [&](int step) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i) na[i] = *reinterpret_cast<const uint32_t *>(w.sa + step + psa[i]);
+#pragma unroll
+    for (int j = 0; j < SB; ++j) nb[j] = *reinterpret_cast<const uint32_t *>(w.sb + step + psb[j]);
+  };
+  auto have_scales = [&] {   // (the compiler waits for what load_scales started)
+#pragma unroll
+    for (int i = 0; i < MI; ++i) asm volatile("" : "+v"(na[i]));
+#pragma unroll
+    for (int j = 0; j < SB; ++j) asm volatile("" : "+v"(nb[j]));
+  };
+  auto take_scales = [&] {
+#pragma unroll
+    for (int i = 0; i < MI; ++i) sa[i] = na[i];
+#pragma unroll
+    for (int j = 0; j < SB; ++j) sb[j] = nb[j];
+  };
+  auto shift_scales = [&] {
+#pragma unroll
+    for (int i = 0; i < MI; ++i) sa[i] >>= 8;
+#pragma unroll
+    for (int j = 0; j < SB; ++j) sb[j] >>= 8;
+  };
+
+  // what this wave transfers of each side: rows 8 (wave J + j) + lane / 8, j < J;
+  // rows past the end repeat the last one
+  const int lrow = lane >> 3, lpos = lane & 7;
+  uint32_t offa[J], offb[J];
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const int row = 8 * (wave * J + j) + lrow;
+    const uint32_t c = 16u * (uint32_t)(lpos ^ swz128(row));
+    offa[j] = (uint32_t)(min(row, w.rows_a - 1) * g.a.pitch) + c;
+    offb[j] = (uint32_t)(min(row, w.rows_b - 1) * g.b.pitch) + c;
+  }
+  const uint8_t *pa = w.a, *pb = w.b;   // the next step's
+  const uint32_t base = dma::lds_addr(lds_raw) + wave * J * 1024;
+  uint32_t wa = 0, wb = T::kHalf, ra = 0, rb = T::kHalf;   // half-slots to fill and to read next, in bytes
+  auto turn = [](uint32_t &x) {
+    x += 2 * T::kHalf;
+    if (x >= T::kLds) x -= T::kLds;
+  };
+  // half q of the next step's rows of A, of B
+  auto start_a = [&](int q) {
+#pragma unroll
+    for (int j = q * J / 2; j < (q + 1) * J / 2; ++j) dma::copy16(offa[j], pa, base + wa + j * 1024);
+    if (q == 1) {
+      turn(wa);
+      pa += kStep;
+    }
+  };
+  auto start_b = [&](int q) {
+#pragma unroll
+    for (int j = q * J / 2; j < (q + 1) * J / 2; ++j) dma::copy16(offb[j], pb, base + wb + j * 1024);
+    if (q == 1) {
+      turn(wb);
+      pb += kStep;
+    }
+  };
+
+  v16f acc[MI][NI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NI; ++j) acc[i][j] = (v16f){};
+
+  // byte of chunk h of the lane's row in the first 32-row tile of each side (chunk 2 u + h: xor 32 u)
+  const uint32_t ca = (uint32_t)(wm * MI * 32 + r32) * kStep + 16u * (uint32_t)(h ^ swz128(r32));
+  const uint32_t cb = (uint32_t)(wn * NI * 32 + r32) * kStep + 16u * (uint32_t)(h ^ swz128(r32));
+  auto read = [&](uint32_t at, int half) {
+    const v4i lo = *reinterpret_cast<const v4i *>(lds + (at ^ (64u * half)));
+    const v4i hi = *reinterpret_cast<const v4i *>(lds + (at ^ (64u * half + 32u)));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  constexpr int kBufs = T::kWhole ? 4 : 2;
+  v8i fa[kBufs], fb[kBufs][NI];
+  auto load_a = [&](int half, int i, int buf) { fa[buf] = read(ra + ca + i * 32 * kStep, half); };
+  auto load_b = [&](int half, int buf) {
+#pragma unroll
+    for (int j = 0; j < NI; ++j) fb[buf][j] = read(rb + cb + j * 32 * kStep, half);
+  };
+  // every wave's transfers of the next step have landed (where `later`, kLater of
+  // this wave's may be on their way) and its reads of this one are done
+  auto next_step = [&](bool later) {
+    constexpr int kLater = 2 * J * (T::H - 2) + J;   // H - 2 whole steps, and A of one more
+    if (later) dma::wait_vmcnt<kLater>(); else dma::wait_vmcnt<0>();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+
+  if (ns > 0) {
+    load_scales(0);
+#pragma unroll
+    for (int s = 0; s < T::H - 1; ++s)
+      if (s < ns) {
+        start_a(0); start_a(1); start_b(0); start_b(1);
+      }
+    if (T::H - 1 < ns) {
+      start_a(0); start_a(1);
+    }
+    next_step(T::H - 1 < ns);
+    have_scales();
+    take_scales();
+    if constexpr (T::kWhole) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        load_a(u, 0, u);
+        load_b(u, u);
+      }
+      if (T::H - 1 < ns) {
+        start_b(0); start_b(1);
+      }
+      if (T::H < ns) {
+        start_a(0); start_a(1);
+      }
+    } else {
+      if (T::H - 1 < ns) start_b(0);
+      load_b(0, 0);
+      load_a(0, 0, 0);
     }
   }
-  // lane (r, h), element e: row r, column 8 (e / 4) + 4 h + e % 4
-  if (mw + r >= w.rows_a) return;
-  elem_t<OUT> *out = static_cast<elem_t<OUT> *>(w.C) + (int64_t)(mw + r) * g.N + nw;
+  // A step; FULL: H + 1 steps or more come after it.  LAST: of four, the
+  // following ones' scales are on their way.  The steps of the loop are FULL ones without a branch: where control
+  // flow joins, the compiler waits for every LDS read that is under way.
+  auto step = [&](int s, auto BUF, auto FULL, auto LAST) {
+    constexpr bool full = decltype(FULL)::value;
+    const bool one = full || s + 1 < ns, more = full || s + T::H - 1 < ns, far = full || s + T::H < ns,
+               far1 = full || s + T::H + 1 < ns;
+    if constexpr (T::kWhole) {
+      // Small tiles: all of a step's fragments are read while the step before is
+      // multiplied.  B of s + H and A of s + H + 1 go where A and B of s were.
+      constexpr int b = 2 * decltype(BUF)::value;
+      if (one) {
+        next_step(far);
+        if constexpr (decltype(LAST)::value) have_scales();
+        turn(ra);
+        turn(rb);
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const int n = 8 * (e >> 2) + 4 * h + (e & 3);
-    if (nw + n < w.rows_b) out[n] = (elem_t<OUT>)(acc[e] + (w.bias ? w.bias[nw + n] : 0.0f));
+        for (int u = 0; u < 2; ++u) {
+          load_a(u, 0, 2 - b + u);
+          load_b(u, 2 - b + u);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (far) {
+          start_b(0); start_b(1);
+        }
+        if (far1) {
+          start_a(0); start_a(1);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        acc[0][0] = E::mma(E::prepare(fb[b + u][0], sb[0]), sb[0],
+                           E::prepare(fa[b + u], sa[0]), sa[0], acc[0][0]);
+    } else {
+      typename E::op ob[NI];
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        const int half = q / MI, i = q % MI;
+        if (q == Q - 1) {
+          if (one) {
+            // B of s + H may fill A's half-slot of s, and A of s + H + 1 then B's
+            next_step(far);
+            if constexpr (decltype(LAST)::value) have_scales();
+            turn(ra);
+            turn(rb);
+            load_b(0, 0);
+            load_a(0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (far) start_b(0);
+          }
+        } else {
+          load_a((q + 1) / MI, (q + 1) % MI, (q + 1) & 1);
+          if (q == 0) load_b(1, 1);
+          __builtin_amdgcn_sched_barrier(0);   // (left to itself the compiler reads a fragment just before it is used)
+        }
+        if (i == 0) {
+#pragma unroll
+          for (int j = 0; j < NI; ++j) ob[j] = E::prepare(fb[half][j], sb[WEIGHTS ? 0 : j]);
+        }
+        const typename E::op oa = E::prepare(fa[q & 1], sa[i]);
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+          acc[i][j] = E::mma(ob[j], sb[WEIGHTS ? 0 : j], oa, sa[i], acc[i][j]);
+        if (q == Q / 4 - 1 && more) start_b(1);
+        if (q == Q / 2 - 1 && far) start_a(0);
+        if (q == 3 * Q / 4 - 1 && far) start_a(1);
+      }
+    }
+    shift_scales();
+  };
+  const std::integral_constant<int, 0> even;
+  const std::integral_constant<int, 1> odd;
+  const std::true_type yes;
+  const std::false_type no;
+  int s = 0;
+  for (; s + 3 + T::H + 1 < ns; s += 4) {
+    step(s, even, yes, no);
+    step(s + 1, odd, yes, no);
+    step(s + 2, even, yes, no);
+    load_scales(s + 4);
+    step(s + 3, odd, yes, yes);
+    take_scales();
   }
+  // (s is a multiple of four here)
+  for (; s < ns; s += T::kWhole ? 2 : 1) {
+    step(s, even, no, no);
+    if (T::kWhole && s + 1 < ns) step(s + 1, odd, no, no);
+    const int next = s + (T::kWhole ? 2 : 1);
+    if ((next & 3) == 0 && next < ns) {
+      load_scales(next);
+      take_scales();
+    }
+  }
+
+  // lane l, accumulator e of tile (i, j): row 32 i + l % 32 of C, column 32 j + 8 (e / 4) + 4 h + e % 4
+  if (w.bias) {
+#pragma unroll
+    for (int j = 0; j < NI; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int n = (wn * NI + j) * 32 + 8 * q + 4 * h, left = w.rows_b - n;
+        float b[4] = {};
+        if (left > 0) q8::load4(w.bias + n, left, b);
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += b[e];
+      }
+  }
+  __syncthreads();
+  q8::GemmProblem out = {};
+  out.M = w.M;
+  out.N = g.N;
+  const int mw = w.m0 + wm * MI * 32, nw = w.n0 + wn * NI * 32;
+  uint8_t *share = reinterpret_cast<uint8_t *>(lds_raw) + wave * (T::kLds / T::kWaves);
+  if (mw + MI * 32 <= out.M && nw + NI * 32 <= out.N) q8::store_tile<E, T, OUT, true>(out, w.C, acc, mw, nw, share);
+  else q8::store_tile<E, T, OUT, false>(out, w.C, acc, mw, nw, share);
 }
 
 }  // namespace f8

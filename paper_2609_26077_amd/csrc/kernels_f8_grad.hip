@@ -46,14 +46,14 @@ __device__ __forceinline__ void transpose4(uint32_t (&w)[4]) {
 // One 128 x 128 tile a workgroup: thread t has eight columns of rows 8 (t / 16) .. + 7.
 // The transpose goes through LDS in pieces of eight bytes (eight rows of a column);
 // piece p of column n sits at p ^ (n / 8), so that both directions spread over the banks.
-struct Tile {
+struct Turn {
   u32x2 out[128][16];
   uint32_t most[4][128];
   float sum[4][128];
 };
 
 // the tile's columns n < cols to rows of dst
-__device__ __forceinline__ void store_columns(const Tile &tile, uint8_t *dst, int64_t pitch, int cols) {
+__device__ __forceinline__ void store_columns(const Turn &tile, uint8_t *dst, int64_t pitch, int cols) {
   const int t = threadIdx.x, c = t & 7;
 #pragma unroll
   for (int p = 0; p < 4; ++p) {
@@ -66,7 +66,7 @@ __device__ __forceinline__ void store_columns(const Tile &tile, uint8_t *dst, in
 }
 
 // codes by columns of v, and their scales to scales[n * pitch]
-__device__ __forceinline__ void columns(Tile &tile, const float (&v)[8][8], uint8_t *dst, int64_t pitch, uint8_t *scales,
+__device__ __forceinline__ void columns(Turn &tile, const float (&v)[8][8], uint8_t *dst, int64_t pitch, uint8_t *scales,
                                         int64_t scale_pitch, int cols) {
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, rg = t >> 4, cg = t & 15;
 #pragma unroll
@@ -96,7 +96,7 @@ __device__ __forceinline__ void columns(Tile &tile, const float (&v)[8][8], uint
 
 template <int T>
 __global__ __launch_bounds__(256) void layout_kernel(LayoutArgs g) {
-  __shared__ Tile tile;
+  __shared__ Turn tile;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, rg = t >> 4, cg = t & 15;
   int id = blockIdx.x;
   if (id >= g.jobs_dy + g.jobs_a) {
@@ -186,12 +186,12 @@ __global__ __launch_bounds__(256) void layout_kernel(LayoutArgs g) {
   }
 }
 
-template <class E, int OUT, bool WEIGHTS>
-__global__ __launch_bounds__(256) void grad_kernel(Product g) {
+template <class E, class T, int OUT, bool WEIGHTS>
+__global__ __launch_bounds__(T::kThreads, 2) void grad_kernel(Product g) {
+  __shared__ uint4 lds[T::kLds / 16];
   Work w;
-  if (!work_of<64, 64, WEIGHTS>(g, blockIdx.x, OUT == FMM_F32 ? 4 : 2, w)) return;
-  const int wave = threadIdx.x >> 6;
-  gemm_tile<E, OUT, WEIGHTS>(g, w, 32 * (wave >> 1), 32 * (wave & 1));
+  if (!work_of<T::TM, T::TN, WEIGHTS>(g, blockIdx.x, w)) return;
+  gemm_tile<E, T, OUT, WEIGHTS>(g, w, lds);
 }
 
 __global__ __launch_bounds__(256) void bias_kernel(const int32_t *offsets, int experts, int rows, int N, const float *colsum,
@@ -242,6 +242,7 @@ Layout layout_of(int64_t rows, int64_t experts, int64_t N, int64_t K) {
 
 template <class E, int T>
 int launch(const GradArgs &a, int ncu, hipStream_t s) {
+  using TX = q8::Tile128;
   const Layout l = layout_of(a.rows, a.experts, a.N, a.K);
   LayoutArgs g = {};
   g.dy = a.dy; g.a = a.a; g.sa = a.sa; g.w = a.w; g.sw = a.sw; g.offsets = a.offsets;
@@ -261,23 +262,23 @@ int launch(const GradArgs &a, int ncu, hipStream_t s) {
   if (jobs > 0) layout_kernel<T><<<dim3((unsigned)jobs), 256, 0, s>>>(g);
 
   Product x = {};
-  x.offsets = a.offsets; x.experts = g.experts; x.rows = g.rows; x.N = g.K; x.splits = 1;
-  x.tiles_n = (g.K + 63) / 64;
+  x.offsets = a.offsets; x.experts = g.experts; x.rows = g.rows; x.N = g.K; x.out_bytes = type_bytes(T);
+  x.tiles_n = (g.K + TX::TN - 1) / TX::TN;
   if (a.dx && a.rows > 0) {
     Product p = x;
     p.a = {g.dyr, g.sdyr, g.Np, g.spn, 0, 0};
     p.b = {g.wt, g.swt, g.Np, g.spn, a.K * g.Np, (int64_t)g.bk * g.spn};
     p.C = a.dx; p.M = g.rows; p.steps = g.bn;
-    p.tiles_m = g.rows / 64 + std::min(g.experts, g.rows);
-    grad_kernel<E, T, true><<<dim3((unsigned)(p.tiles_m * p.tiles_n)), 256, 0, s>>>(p);
+    p.tiles_m = g.rows / TX::TM + std::min(g.experts, g.rows);
+    grad_kernel<E, TX, T, true><<<dim3((unsigned)(p.tiles_m * p.tiles_n)), TX::kThreads, 0, s>>>(p);
   }
   if (a.dw) {
     Product p = x;
     p.a = {g.dyt, g.sdyt, g.Bp, g.sbp, 0, 0};
     p.b = {g.xt, g.sxt, g.Bp, g.sbp, 0, 0};
     p.C = a.dw; p.M = g.N; p.steps = g.blocks; p.axis = 1;
-    p.tiles_m = (g.N + 63) / 64;
-    grad_kernel<E, T, false><<<dim3((unsigned)(g.experts * p.tiles_m * p.tiles_n)), 256, 0, s>>>(p);
+    p.tiles_m = (g.N + TX::TM - 1) / TX::TM;
+    grad_kernel<E, TX, T, false><<<dim3((unsigned)(g.experts * p.tiles_m * p.tiles_n)), TX::kThreads, 0, s>>>(p);
   }
   if (a.dbias)
     bias_kernel<<<dim3((unsigned)(g.experts * ((g.N + 255) / 256))), 256, 0, s>>>(a.offsets, g.experts, g.rows, g.N, g.colsum,

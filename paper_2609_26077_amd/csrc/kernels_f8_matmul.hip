@@ -2,7 +2,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <type_traits>
 
 #include "f8_gemm.h"
 
@@ -10,29 +9,231 @@ namespace fmm {
 namespace f8 {
 namespace {
 
-template <class E, int OUT>
-__global__ __launch_bounds__(256) void matmul_kernel(Product g) {
+template <class E, class T, int OUT>
+__global__ __launch_bounds__(T::kThreads, 2) void matmul_kernel(Product g) {
+  __shared__ uint4 lds[T::kLds / 16];
   Work w;
-  if (!work_of<64, 64, true>(g, blockIdx.x, OUT == FMM_F32 ? 4 : 2, w)) return;
-  const int wave = threadIdx.x >> 6;
-  gemm_tile<E, OUT, true>(g, w, 32 * (wave >> 1), 32 * (wave & 1));
+  if (!work_of<T::TM, T::TN, true>(g, blockIdx.x, w)) return;
+  gemm_tile<E, T, OUT, true>(g, w, lds);
+}
+
+// Few tokens: the weights are read once and that bounds it, so what counts is
+// bytes in flight.  A workgroup takes 16 NT channels and 16 MT tokens (of one expert) and splits
+// the contracted axis over its W waves, each of which brings its own 128-byte
+// pieces of those rows into its own part of LDS, D pieces ahead, whole lines at
+// a time, and waits for nobody until the waves' sums meet in LDS at the end, where they
+// are added in the waves' order.  Rows in LDS are swizzled as in the tile kernel.
+// The scales of 128 steps go through LDS too, wave 0 bringing them before its
+// first pieces.
+template <class E, int MT, int NT, int W, int D, int OUT>
+__global__ __launch_bounds__(64 * W) void few_tokens_kernel(Product g) {
+  constexpr int kPiece = 16 * (MT + NT) * kStep;
+  constexpr int kMoves = 2 * (MT + NT);            // transfers of a piece: eight rows each
+  constexpr int kLds = W * D * kPiece, kSeg = 128, kScales = 16 * MT * kSeg;
+  static_assert(MT * NT * 1024 <= D * kPiece && kLds + kScales + 1024 <= 160 * 1024, "the sums fit, and the pieces");
+  static_assert(kBlock % (16 * NT) == 0 && kSeg % W == 0, "one scale of the weights, whole turns of the waves");
+  __shared__ uint4 lds_raw[(kLds + kScales + 1024) / 16];
+  const int lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Experts x(g.offsets, g.experts, g.rows, 16 * MT);
+  const int tm = blockIdx.x / g.tiles_n, n0 = 16 * NT * (blockIdx.x - tm * g.tiles_n);
+  if (tm >= x.total) return;
+  const Span s = x.find(tm);
+  const int m0 = s.lo + 16 * MT * (tm - s.tiles), rows_a = s.hi - m0, rows_b = g.N - n0;
+  const int64_t ex = s.expert;
+  const uint8_t *pa = g.a.codes + m0 * g.a.pitch, *pw = g.b.codes + ex * g.b.expert_codes + n0 * g.b.pitch;
+  const uint8_t *psa = g.a.scales + m0 * g.a.scale_pitch;
+  const uint8_t *psw = g.b.scales + ex * g.b.expert_scales + n0 / kBlock * g.b.scale_pitch;
+  const uint32_t base0 = dma::lds_addr(lds_raw), base = base0 + wave * D * kPiece;
+  const uint8_t *lds = reinterpret_cast<const uint8_t *>(lds_raw), *mine = lds + wave * D * kPiece;
+  // rows past the end repeat the last one
+  const int lrow = lane >> 3, lpos = lane & 7;
+  uint32_t offw[2 * NT], offa[2 * MT];
+#pragma unroll
+  for (int j = 0; j < 2 * NT; ++j) {
+    const int row = 8 * j + lrow;
+    offw[j] = (uint32_t)(min(row, rows_b - 1) * g.b.pitch) + 16u * (uint32_t)(lpos ^ swz128(row));
+  }
+#pragma unroll
+  for (int j = 0; j < 2 * MT; ++j) {
+    const int row = 8 * j + lrow;
+    offa[j] = (uint32_t)(min(row, rows_a - 1) * g.a.pitch) + 16u * (uint32_t)(lpos ^ swz128(row));
+  }
+  auto start = [&](int k, int slot) {
+    const uint32_t dst = base + slot * kPiece;
+#pragma unroll
+    for (int j = 0; j < 2 * NT; ++j) dma::copy16(offw[j], pw + (int64_t)k * kStep, dst + j * 1024);
+#pragma unroll
+    for (int j = 0; j < 2 * MT; ++j) dma::copy16(offa[j], pa + (int64_t)k * kStep, dst + (2 * NT + j) * 1024);
+  };
+  // byte of chunk 4 u + h of row r of the first 16
+  uint32_t chunk[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) chunk[u] = r * kStep + 16u * (uint32_t)((4 * u + h) ^ swz128(r));
+
+  v4f acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = (v4f){};
+  for (int seg = 0; seg < g.steps; seg += kSeg) {
+    const int end = min(seg + kSeg, g.steps);
+    if (seg > 0) __syncthreads();   // (everyone has read the last scales)
+    if (wave == 0) {
+      // 16-byte chunk c of a row of scales sits at c ^ (row mod 8); chunks past the row's end repeat its last
+      const int last = (int)((g.a.scale_pitch - seg) / 16) - 1;
+#pragma unroll
+      for (int j = 0; j < 2 * MT; ++j)
+        dma::copy16((uint32_t)(min(8 * j + lrow, rows_a - 1) * g.a.scale_pitch) + 16u * (uint32_t)min(lpos ^ lrow, last),
+                    psa + seg, base0 + kLds + j * 1024);
+      dma::copy16(16u * (uint32_t)min(lpos, last), psw + seg, base0 + kLds + kScales);
+    }
+#pragma unroll
+    for (int d = 0; d < D; ++d)
+      if (seg + wave + d * W < end) start(seg + wave + d * W, d);
+    if (wave == 0) {
+      if (seg + (D - 1) * W < end) dma::wait_vmcnt<D * kMoves>(); else dma::wait_vmcnt<0>();
+    }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    int slot = 0;
+    for (int k = seg + wave; k < end; k += W) {
+      // this piece has landed; the D - 1 after it, if there are as many, may be on their way
+      if (k + (D - 1) * W < end) dma::wait_vmcnt<(D - 1) * kMoves>(); else dma::wait_vmcnt<0>();
+      const uint8_t *p = mine + slot * kPiece;
+      const int kk = k - seg;
+      uint32_t ea[MT];
+#pragma unroll
+      for (int i = 0; i < MT; ++i) ea[i] = lds[kLds + (16 * i + r) * kSeg + 16 * ((kk >> 4) ^ (r & 7)) + (kk & 15)];
+      const uint32_t ew = lds[kLds + kScales + kk];
+      v8i fw[NT], fa[MT];
+      auto read = [&](int row) {
+        const v4i lo = *reinterpret_cast<const v4i *>(p + row * kStep + chunk[0]);
+        const v4i hi = *reinterpret_cast<const v4i *>(p + row * kStep + chunk[1]);
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      };
+#pragma unroll
+      for (int j = 0; j < NT; ++j) fw[j] = read(16 * j);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) fa[i] = read(16 * (NT + i));
+      // the slot has been read: fill it again
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (k + D * W < end) start(k + D * W, slot);
+      slot = slot + 1 == D ? 0 : slot + 1;
+      typename E::op ow[NT];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) ow[j] = E::prepare(fw[j], ew);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const typename E::op oa = E::prepare(fa[i], ea[i]);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = E::mma16(ow[j], ew, oa, ea[i], acc[i][j]);
+      }
+    }
+  }
+  // (a wave's sums go where its pieces were)
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+      *reinterpret_cast<v4f *>(const_cast<uint8_t *>(mine) + ((i * NT + j) * 64 + lane) * 16) = acc[i][j];
+  __syncthreads();
+  // lane l, element e of tile (i, j): token 16 i + l % 16, channel 16 j + 4 (l / 16) + e
+  for (int e = wave; e < MT * NT; e += W) {
+    const int m = 16 * (e / NT) + r, n = 16 * (e % NT) + 4 * h;
+    const uint8_t *p = lds + (e * 64 + lane) * 16;
+    v4f c = *reinterpret_cast<const v4f *>(p);
+#pragma unroll
+    for (int i = 1; i < W; ++i) c += *reinterpret_cast<const v4f *>(p + i * D * kPiece);
+    if (m < rows_a && n < rows_b) {
+      float bias[4] = {}, v[4];
+      if (g.bias) q8::load4(g.bias + ex * g.N + n0 + n, rows_b - n, bias);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = c[q] + bias[q];
+      q8::store4<OUT>(static_cast<elem_t<OUT> *>(g.C) + (int64_t)(m0 + m) * g.N + n0 + n, rows_b - n, v);
+    }
+  }
+}
+
+// The shapes of workgroup: t = start + max(chain pieces, work pieces groups / CUs) us, as for
+// the int8 product.
+struct Shape {
+  int tm, tn, waves;            // tile, and the waves that share its contracted axis
+  float start, chain, work;
+  bool one;                     // only where each CU has one group at most
+};
+constexpr Shape kShapes[] = {
+    {16, 16, 8, 1.7f, 0.30f, 0.57f, false}, {32, 32, 4, 2.2f, 0.37f, 0.61f, false},
+    {64, 64, 1, 3.2f, 0.19f, 0.28f, false}, {128, 128, 1, 3.3f, 0.45f, 0.60f, true},
+    {128, 128, 1, 3.6f, 0.47f, 0.62f, false}, {256, 256, 1, 8.7f, 1.2f, 1.8f, false},
+};
+constexpr int kShapeCount = sizeof(kShapes) / sizeof(kShapes[0]);
+constexpr double kMaxGroups = 1 << 22;
+
+int pick(int type, const Product &g, int ncu) {
+  const int shapes = type == FMM_F32 ? kShapeCount - 1 : kShapeCount;
+  // experts with rows, at most, and each one's rows if they were even
+  const double experts = std::max(1, std::min(g.experts, g.rows)), rows = g.rows / experts;
+  int best = shapes - 1;
+  double least = 1e300;
+  for (int i = 0; i < shapes; ++i) {
+    const Shape &p = kShapes[i];
+    const double groups = experts * std::ceil(rows / p.tm) * ((g.N + p.tn - 1) / p.tn);
+    if (groups > kMaxGroups || (p.one && groups > ncu)) continue;
+    const double pieces = (g.steps + p.waves - 1) / p.waves;
+    const double t = p.start + std::max(p.chain * pieces, p.work * pieces * groups / ncu);
+    if (t < least) {
+      best = i;
+      least = t;
+    }
+  }
+  return best;
+}
+
+template <class E, int MT, int NT, int W, int D, int OUT>
+void launch_few(Product g, hipStream_t s) {
+  g.tiles_n = (g.N + 16 * NT - 1) / (16 * NT);
+  g.tiles_m = g.rows / (16 * MT) + std::min(g.experts, g.rows);
+  few_tokens_kernel<E, MT, NT, W, D, OUT><<<dim3((unsigned)(g.tiles_m * g.tiles_n)), 64 * W, 0, s>>>(g);
+}
+
+template <class E, class T, int OUT>
+void launch_tiles(Product g, hipStream_t s) {
+  g.tiles_n = (g.N + T::TN - 1) / T::TN;
+  g.tiles_m = g.rows / T::TM + std::min(g.experts, g.rows);
+  matmul_kernel<E, T, OUT><<<dim3((unsigned)(g.tiles_m * g.tiles_n)), T::kThreads, 0, s>>>(g);
+}
+
+template <class E, int OUT>
+void launch(int shape, const Product &g, hipStream_t s) {
+  switch (shape) {
+    case 0: return launch_few<E, 1, 1, 8, 2, OUT>(g, s);
+    case 1: return launch_few<E, 2, 2, 4, 2, OUT>(g, s);
+    case 2: return launch_tiles<E, q8::Tile64, OUT>(g, s);
+    case 3: return launch_tiles<E, q8::Tile128Ahead, OUT>(g, s);
+    case 4: return launch_tiles<E, q8::Tile128, OUT>(g, s);
+  }
+  if constexpr (OUT != FMM_F32) launch_tiles<E, q8::Tile256, OUT>(g, s);
 }
 
 }  // namespace
 
-int launch_matmul(int type, const Product &p, int ncu, void *stream) {
-  Product g = p;
-  g.tiles_n = (g.N + 63) / 64;
-  g.tiles_m = g.rows / 64 + std::min(g.experts, g.rows);
-  const dim3 grid((unsigned)(g.tiles_m * g.tiles_n));
-  const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (type == FMM_F32) matmul_kernel<F8Exact, FMM_F32><<<grid, 256, 0, s>>>(g);
-  else if (type == FMM_BF16) matmul_kernel<F8, FMM_BF16><<<grid, 256, 0, s>>>(g);
-  else matmul_kernel<F8, FMM_F16><<<grid, 256, 0, s>>>(g);
-  return hipGetLastError();
+const char *matmul_kernel_name(int type, const Product &p, int ncu) {
+  static const char *const names[kShapeCount] = {
+      "few_tokens_kernel 16x16", "few_tokens_kernel 32x32", "matmul_kernel 64x64", "matmul_kernel 128x128 ahead",
+      "matmul_kernel 128x128", "matmul_kernel 256x256"};
+  return names[pick(type, p, ncu)];
 }
 
-const char *matmul_kernel_name(int, const Product &, int) { return "matmul_kernel 64x64"; }
+int launch_matmul(int type, const Product &p, int ncu, void *stream) {
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const int shape = pick(type, p, ncu);
+  if (type == FMM_F32) launch<F8Exact, FMM_F32>(shape, p, s);
+  else if (type == FMM_BF16) launch<F8, FMM_BF16>(shape, p, s);
+  else launch<F8, FMM_F16>(shape, p, s);
+  return hipGetLastError();
+}
 
 }  // namespace f8
 }  // namespace fmm
