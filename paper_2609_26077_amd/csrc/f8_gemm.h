@@ -34,6 +34,21 @@ typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 using q8::v4i;
 
+// dma::copy16 if `some` > 0 and dma::wait_vmcnt<N> (else <0>), conditions that the compiler does not
+// see as control flow: where that joins, it waits for every LDS read that is under way.
+__device__ __forceinline__ void copy16_if(int some, uint32_t off, const uint8_t *base, uint32_t m0) {
+  asm volatile(
+      "s_cmp_le_i32 %3, 0\n\ts_cbranch_scc1 .Lnone%=\n\ts_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1\n.Lnone%=:" ::"v"(off),
+      "s"(base), "s"(m0), "s"(some)
+      : "memory", "m0", "scc");
+}
+template <int N>
+__device__ __forceinline__ void wait_vmcnt_if(int some) {
+  asm volatile("s_cmp_gt_i32 %0, 0\n\ts_cbranch_scc1 .Lsome%=\n\ts_waitcnt vmcnt(0)\n.Lsome%=:\n\ts_waitcnt vmcnt(%1)" ::"s"(some),
+               "n"(N)
+               : "memory", "scc");
+}
+
 // What a workgroup has to do: a tile of C, its rows of A and B, and the steps
 // of 128 codes that it contracts.
 struct Work {
@@ -139,7 +154,7 @@ __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = wave / T::WN, wn = wave % T::WN;
   const int r32 = lane & 31, h = lane >> 5;
-  const int ns = w.steps;
+  const int ns = __builtin_amdgcn_readfirstlane(w.steps);
 
   // scales of steps 4 i .. 4 i + 3, the first in the low byte
   uint32_t psa[MI], psb[SB];
@@ -194,18 +209,18 @@ __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4
     x += 2 * T::kHalf;
     if (x >= T::kLds) x -= T::kLds;
   };
-  // half q of the next step's rows of A, of B
-  auto start_a = [&](int q) {
+  // half q of the next step's rows of A, of B, if there is such a step
+  auto start_a = [&](int q, int some) {
 #pragma unroll
-    for (int j = q * J / 2; j < (q + 1) * J / 2; ++j) dma::copy16(offa[j], pa, base + wa + j * 1024);
+    for (int j = q * J / 2; j < (q + 1) * J / 2; ++j) copy16_if(some, offa[j], pa, base + wa + j * 1024);
     if (q == 1) {
       turn(wa);
       pa += kStep;
     }
   };
-  auto start_b = [&](int q) {
+  auto start_b = [&](int q, int some) {
 #pragma unroll
-    for (int j = q * J / 2; j < (q + 1) * J / 2; ++j) dma::copy16(offb[j], pb, base + wb + j * 1024);
+    for (int j = q * J / 2; j < (q + 1) * J / 2; ++j) copy16_if(some, offb[j], pb, base + wb + j * 1024);
     if (q == 1) {
       turn(wb);
       pb += kStep;
@@ -233,11 +248,11 @@ __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4
 #pragma unroll
     for (int j = 0; j < NI; ++j) fb[buf][j] = read(rb + cb + j * 32 * kStep, half);
   };
-  // every wave's transfers of the next step have landed (where `later`, kLater of
+  // every wave's transfers of the next step have landed (where later > 0, kLater of
   // this wave's may be on their way) and its reads of this one are done
-  auto next_step = [&](bool later) {
+  auto next_step = [&](int later) {
     constexpr int kLater = 2 * J * (T::H - 2) + J;   // H - 2 whole steps, and A of one more
-    if (later) dma::wait_vmcnt<kLater>(); else dma::wait_vmcnt<0>();
+    wait_vmcnt_if<kLater>(later);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
@@ -247,14 +262,13 @@ __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4
   if (ns > 0) {
     load_scales(0);
 #pragma unroll
-    for (int s = 0; s < T::H - 1; ++s)
-      if (s < ns) {
-        start_a(0); start_a(1); start_b(0); start_b(1);
+    for (int s = 0; s < T::H; ++s) {
+      start_a(0, ns - s); start_a(1, ns - s);
+      if (s < T::H - 1) {
+        start_b(0, ns - s); start_b(1, ns - s);
       }
-    if (T::H - 1 < ns) {
-      start_a(0); start_a(1);
     }
-    next_step(T::H - 1 < ns);
+    next_step(ns - T::H + 1);
     have_scales();
     take_scales();
     if constexpr (T::kWhole) {
@@ -263,68 +277,52 @@ __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4
         load_a(u, 0, u);
         load_b(u, u);
       }
-      if (T::H - 1 < ns) {
-        start_b(0); start_b(1);
-      }
-      if (T::H < ns) {
-        start_a(0); start_a(1);
-      }
+      start_b(0, ns - T::H + 1); start_b(1, ns - T::H + 1);
+      start_a(0, ns - T::H); start_a(1, ns - T::H);
     } else {
-      if (T::H - 1 < ns) start_b(0);
+      start_b(0, ns - T::H + 1);
       load_b(0, 0);
       load_a(0, 0, 0);
     }
   }
-  // A step; FULL: H + 1 steps or more come after it.  LAST: of four, the
-  // following ones' scales are on their way.  The steps of the loop are FULL ones without a branch: where control
-  // flow joins, the compiler waits for every LDS read that is under way.
-  auto step = [&](int s, auto BUF, auto FULL, auto LAST) {
-    constexpr bool full = decltype(FULL)::value;
-    const bool one = full || s + 1 < ns, more = full || s + T::H - 1 < ns, far = full || s + T::H < ns,
-               far1 = full || s + T::H + 1 < ns;
+  // A step, without control flow: after the last one it reads fragments that nobody
+  // uses.  LAST: of four, the following ones' scales are on their way.
+  auto step = [&](int s, auto BUF, auto LAST) {
+    const int far = ns - s - T::H, more = far + 1, far1 = far - 1;
     if constexpr (T::kWhole) {
       // Small tiles: all of a step's fragments are read while the step before is
       // multiplied.  B of s + H and A of s + H + 1 go where A and B of s were.
       constexpr int b = 2 * decltype(BUF)::value;
-      if (one) {
-        next_step(far);
-        if constexpr (decltype(LAST)::value) have_scales();
-        turn(ra);
-        turn(rb);
+      next_step(far);
+      if constexpr (decltype(LAST)::value) have_scales();
+      turn(ra);
+      turn(rb);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          load_a(u, 0, 2 - b + u);
-          load_b(u, 2 - b + u);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        if (far) {
-          start_b(0); start_b(1);
-        }
-        if (far1) {
-          start_a(0); start_a(1);
-        }
+      for (int u = 0; u < 2; ++u) {
+        load_a(u, 0, 2 - b + u);
+        load_b(u, 2 - b + u);
       }
+      __builtin_amdgcn_sched_barrier(0);
+      start_b(0, far); start_b(1, far);
+      start_a(0, far1); start_a(1, far1);
 #pragma unroll
       for (int u = 0; u < 2; ++u)
-        acc[0][0] = E::mma(E::prepare(fb[b + u][0], sb[0]), sb[0],
-                           E::prepare(fa[b + u], sa[0]), sa[0], acc[0][0]);
+        acc[0][0] = E::mma(E::prepare(fb[b + u][0], sb[0]), sb[0], E::prepare(fa[b + u], sa[0]), sa[0], acc[0][0]);
     } else {
       typename E::op ob[NI];
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
         const int half = q / MI, i = q % MI;
         if (q == Q - 1) {
-          if (one) {
-            // B of s + H may fill A's half-slot of s, and A of s + H + 1 then B's
-            next_step(far);
-            if constexpr (decltype(LAST)::value) have_scales();
-            turn(ra);
-            turn(rb);
-            load_b(0, 0);
-            load_a(0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
-            if (far) start_b(0);
-          }
+          // B of s + H may fill A's half-slot of s, and A of s + H + 1 then B's
+          next_step(far);
+          if constexpr (decltype(LAST)::value) have_scales();
+          turn(ra);
+          turn(rb);
+          load_b(0, 0);
+          load_a(0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+          start_b(0, far);
         } else {
           load_a((q + 1) / MI, (q + 1) % MI, (q + 1) & 1);
           if (q == 0) load_b(1, 1);
@@ -336,11 +334,10 @@ __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4
         }
         const typename E::op oa = E::prepare(fa[q & 1], sa[i]);
 #pragma unroll
-        for (int j = 0; j < NI; ++j)
-          acc[i][j] = E::mma(ob[j], sb[WEIGHTS ? 0 : j], oa, sa[i], acc[i][j]);
-        if (q == Q / 4 - 1 && more) start_b(1);
-        if (q == Q / 2 - 1 && far) start_a(0);
-        if (q == 3 * Q / 4 - 1 && far) start_a(1);
+        for (int j = 0; j < NI; ++j) acc[i][j] = E::mma(ob[j], sb[WEIGHTS ? 0 : j], oa, sa[i], acc[i][j]);
+        if (q == Q / 4 - 1) start_b(1, more);
+        if (q == Q / 2 - 1) start_a(0, far);
+        if (q == 3 * Q / 4 - 1) start_a(1, far);
       }
     }
     shift_scales();
@@ -349,24 +346,16 @@ __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4
   const std::integral_constant<int, 1> odd;
   const std::true_type yes;
   const std::false_type no;
-  int s = 0;
-  for (; s + 3 + T::H + 1 < ns; s += 4) {
-    step(s, even, yes, no);
-    step(s + 1, odd, yes, no);
-    step(s + 2, even, yes, no);
-    load_scales(s + 4);
-    step(s + 3, odd, yes, yes);
+  for (int s = 0; s < ns; ++s) {
+    step(s, even, no);
+    if (++s == ns) break;
+    step(s, odd, no);
+    if (++s == ns) break;
+    step(s, even, no);
+    if (++s == ns) break;
+    load_scales(s + 1 < ns ? s + 1 : s - 3);
+    step(s, odd, yes);
     take_scales();
-  }
-  // (s is a multiple of four here)
-  for (; s < ns; s += T::kWhole ? 2 : 1) {
-    step(s, even, no, no);
-    if (T::kWhole && s + 1 < ns) step(s + 1, odd, no, no);
-    const int next = s + (T::kWhole ? 2 : 1);
-    if ((next & 3) == 0 && next < ns) {
-      load_scales(next);
-      take_scales();
-    }
   }
 
   // lane l, accumulator e of tile (i, j): row 32 i + l % 32 of C, column 32 j + 8 (e / 4) + 4 h + e % 4
