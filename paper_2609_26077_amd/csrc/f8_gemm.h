@@ -346,6 +346,25 @@ __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4
   const std::integral_constant<int, 1> odd;
   const std::true_type yes;
   const std::false_type no;
+  // a wave whose part of the tile lies past the matrix (or the expert's rows) only transfers
+  const bool idle = (wm * MI * 32 >= w.rows_a || wn * NI * 32 >= w.rows_b);
+  if (idle) {
+    for (int s = 0; s < ns; ++s) {
+      const int far = ns - s - T::H;
+      if constexpr (T::kWhole) {
+        next_step(far);
+        start_b(0, far); start_b(1, far);
+        start_a(0, far - 1); start_a(1, far - 1);
+      } else {
+        start_b(1, far + 1);
+        start_a(0, far); start_a(1, far);
+        next_step(far);
+        start_b(0, far);
+      }
+    }
+    __syncthreads();
+    return;
+  }
   for (int s = 0; s < ns; ++s) {
     step(s, even, no);
     if (++s == ns) break;
