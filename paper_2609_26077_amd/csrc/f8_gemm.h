@@ -109,6 +109,7 @@ __device__ __forceinline__ bool work_of(const Product &g, int id, Work &w) {
   Span s;
   int tm, tn, part;
   if (g.axis) {
+    if (id >= g.tiles_m * g.tiles_n * g.experts) return false;
     q8::item_of<GM>(id, g.tiles_m * g.tiles_n * g.experts, g.tiles_m, g.tiles_n, tm, tn, part);
     Experts x(g.offsets, g.experts, g.rows, kBlock);
     s = x.at(part);

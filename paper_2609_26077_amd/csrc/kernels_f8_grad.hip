@@ -186,25 +186,42 @@ __global__ __launch_bounds__(256) void layout_kernel(LayoutArgs g) {
   }
 }
 
-template <class E, class T, int OUT, bool WEIGHTS>
-__global__ __launch_bounds__(T::kThreads, 2) void grad_kernel(Product g) {
-  __shared__ uint4 lds[T::kLds / 16];
-  Work w;
-  if (!work_of<T::TM, T::TN, WEIGHTS>(g, blockIdx.x, w)) return;
-  gemm_tile<E, T, OUT, WEIGHTS>(g, w, lds);
-}
+struct GradGemms {
+  Product x, w;              // dX, dW
+  int x_first;               // dX's tiles come before dW's: the ones with the longer chain
+  int items0, items;         // workgroups of the first, of both
+  const float *colsum;
+  float *dbias;
+};
 
-__global__ __launch_bounds__(256) void bias_kernel(const int32_t *offsets, int experts, int rows, int N, const float *colsum,
-                                                   float *dbias) {
-  const int per = (N + 255) / 256, e = blockIdx.x / per, n = (blockIdx.x - e * per) * 256 + threadIdx.x;
-  Experts x(offsets, experts, rows, kBlock);
+// Tiles TX of dX and TW of dW (equal workgroups), then dY's column sums by expert.
+template <class E, class TX, class TW, int OUT>
+__global__ __launch_bounds__(TX::kThreads, 2) void grad_kernel(GradGemms g) {
+  static_assert(TX::kThreads == TW::kThreads, "one launch");
+  __shared__ uint4 lds[(TX::kLds > TW::kLds ? TX::kLds : TW::kLds) / 16];
+  int id = blockIdx.x;
+  if (id < g.items) {
+    Work w;
+    const bool first = id < g.items0;
+    if (!first) id -= g.items0;
+    if (first == (g.x_first != 0)) {
+      if (work_of<TX::TM, TX::TN, true>(g.x, id, w)) gemm_tile<E, TX, OUT, true>(g.x, w, lds);
+    } else {
+      if (work_of<TW::TM, TW::TN, false>(g.w, id, w)) gemm_tile<E, TW, OUT, false>(g.w, w, lds);
+    }
+    return;
+  }
+  const int N = g.w.M, per = (N + TX::kThreads - 1) / TX::kThreads;
+  id -= g.items;
+  const int e = id / per, n = (id - e * per) * TX::kThreads + threadIdx.x;
+  Experts x(g.w.offsets, g.w.experts, g.w.rows, kBlock);
   const Span s = x.at(e);
   if (n >= N) return;
   const int blocks = (s.hi - s.lo + kBlock - 1) / kBlock;
   float c = 0.0f;
 #pragma unroll 4
-  for (int i = 0; i < blocks; ++i) c += colsum[(int64_t)(s.tiles + i) * N + n];
-  dbias[(int64_t)e * N + n] = c;
+  for (int i = 0; i < blocks; ++i) c += g.colsum[(int64_t)(s.tiles + i) * N + n];
+  g.dbias[(int64_t)e * N + n] = c;
 }
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -240,9 +257,59 @@ Layout layout_of(int64_t rows, int64_t experts, int64_t N, int64_t K) {
   return l;
 }
 
+// The tile of each product: 0: 64, 1: 128, 2: 256, 3: 128 with the longer ring (2 and 3 of both, or
+// neither: their workgroups are larger).
+struct Cut {
+  int x, w;
+};
+
+// t = max(start + chain steps, of either; start + work of both / CUs) us, as for the forward products.
+Cut cut_of(int type, int64_t rows, int64_t experts, int64_t N, int64_t K, bool dx, bool dw, int ncu) {
+  /*FIT*/
+  constexpr int kEdge[4] = {64, 128, 256, 128};
+  constexpr double kCost[2][3][4] = {{{3.2, 3.6, 8.7, 3.3}, {0.19, 0.47, 1.2, 0.45}, {0.28, 0.62, 1.8, 0.60}},
+                                     {{3.2, 3.6, 0.0, 3.3}, {0.30, 0.80, 0.0, 0.70}, {0.45, 1.00, 0.0, 1.10}}};
+  const double (&start)[4] = kCost[type == FMM_F32][0], (&chain)[4] = kCost[type == FMM_F32][1], (&work)[4] = kCost[type == FMM_F32][2];
+  // experts with rows, at most, and each one's rows if they were even
+  const double full = std::max<double>(1, std::min(experts, rows)), each = rows / full;
+  const double steps_x = dx ? (N + kBlock - 1) / kBlock : 0, steps_w = dw ? std::ceil(each / kBlock) : 0;
+  Cut best = {};
+  double least = 1e300;
+  for (int x = 0; x < 4; ++x)
+    for (int w = 0; w < 4; ++w) {
+      if (x != w && (x > 1 || w > 1)) continue;
+      if (x == 2 && type == FMM_F32) continue;
+      const double tx = dx ? full * std::ceil(each / kEdge[x]) * std::ceil((double)K / kEdge[x]) : 0;
+      const double tw = dw ? full * std::ceil((double)N / kEdge[w]) * std::ceil((double)K / kEdge[w]) : 0;
+      if (x == 3 && tx + tw > ncu) continue;
+      const double long_x = start[x] + chain[x] * steps_x, long_w = start[w] + chain[w] * steps_w;
+      const double busy = std::max(dx ? start[x] : 0, dw ? start[w] : 0) + (work[x] * steps_x * tx + work[w] * steps_w * tw) / ncu;
+      const double t = std::max(std::max(dx ? long_x : 0, dw ? long_w : 0), busy);
+      if (t < least) {
+        least = t;
+        best = {x, w};
+      }
+    }
+  return best;
+}
+
+template <class E, int T, class TX, class TW>
+void launch_gemms(GradGemms g, const GradArgs &a, hipStream_t s) {
+  g.x.tiles_n = (g.x.N + TX::TN - 1) / TX::TN;
+  g.x.tiles_m = g.x.rows / TX::TM + std::min(g.x.experts, g.x.rows);
+  g.w.tiles_n = (g.w.N + TW::TN - 1) / TW::TN;
+  g.w.tiles_m = (g.w.M + TW::TM - 1) / TW::TM;
+  const int x = a.dx ? g.x.tiles_m * g.x.tiles_n : 0, w = a.dw ? g.w.experts * g.w.tiles_m * g.w.tiles_n : 0;
+  const int db = a.dbias ? g.w.experts * ((g.w.M + TX::kThreads - 1) / TX::kThreads) : 0;
+  g.x_first = g.x.steps * g.w.experts >= g.w.steps;
+  // (whole turns over the XCDs, so that the second's order is the first's)
+  g.items0 = (int)round_up(g.x_first ? x : w, 8);
+  g.items = g.items0 + (g.x_first ? w : x);
+  if (g.items + db > 0) grad_kernel<E, TX, TW, T><<<dim3((unsigned)(g.items + db)), TX::kThreads, 0, s>>>(g);
+}
+
 template <class E, int T>
 int launch(const GradArgs &a, int ncu, hipStream_t s) {
-  using TX = q8::Tile128;
   const Layout l = layout_of(a.rows, a.experts, a.N, a.K);
   LayoutArgs g = {};
   g.dy = a.dy; g.a = a.a; g.sa = a.sa; g.w = a.w; g.sw = a.sw; g.offsets = a.offsets;
@@ -261,28 +328,23 @@ int launch(const GradArgs &a, int ncu, hipStream_t s) {
   const int jobs = g.jobs_dy + g.jobs_a + g.jobs_w;
   if (jobs > 0) layout_kernel<T><<<dim3((unsigned)jobs), 256, 0, s>>>(g);
 
-  Product x = {};
-  x.offsets = a.offsets; x.experts = g.experts; x.rows = g.rows; x.N = g.K; x.out_bytes = type_bytes(T);
-  x.tiles_n = (g.K + TX::TN - 1) / TX::TN;
-  if (a.dx && a.rows > 0) {
-    Product p = x;
-    p.a = {g.dyr, g.sdyr, g.Np, g.spn, 0, 0};
-    p.b = {g.wt, g.swt, g.Np, g.spn, a.K * g.Np, (int64_t)g.bk * g.spn};
-    p.C = a.dx; p.M = g.rows; p.steps = g.bn;
-    p.tiles_m = g.rows / TX::TM + std::min(g.experts, g.rows);
-    grad_kernel<E, TX, T, true><<<dim3((unsigned)(p.tiles_m * p.tiles_n)), TX::kThreads, 0, s>>>(p);
-  }
-  if (a.dw) {
-    Product p = x;
-    p.a = {g.dyt, g.sdyt, g.Bp, g.sbp, 0, 0};
-    p.b = {g.xt, g.sxt, g.Bp, g.sbp, 0, 0};
-    p.C = a.dw; p.M = g.N; p.steps = g.blocks; p.axis = 1;
-    p.tiles_m = (g.N + TX::TM - 1) / TX::TM;
-    grad_kernel<E, TX, T, false><<<dim3((unsigned)(g.experts * p.tiles_m * p.tiles_n)), TX::kThreads, 0, s>>>(p);
-  }
-  if (a.dbias)
-    bias_kernel<<<dim3((unsigned)(g.experts * ((g.N + 255) / 256))), 256, 0, s>>>(a.offsets, g.experts, g.rows, g.N, g.colsum,
-                                                                                  a.dbias);
+  GradGemms q = {};
+  q.colsum = g.colsum; q.dbias = a.dbias;
+  q.x.offsets = a.offsets; q.x.experts = g.experts; q.x.rows = g.rows; q.x.N = g.K; q.x.out_bytes = type_bytes(T);
+  q.w = q.x;
+  q.x.a = {g.dyr, g.sdyr, g.Np, g.spn, 0, 0};
+  q.x.b = {g.wt, g.swt, g.Np, g.spn, a.K * g.Np, (int64_t)g.bk * g.spn};
+  q.x.C = a.dx; q.x.M = g.rows; q.x.steps = g.bn;
+  q.w.a = {g.dyt, g.sdyt, g.Bp, g.sbp, 0, 0};
+  q.w.b = {g.xt, g.sxt, g.Bp, g.sbp, 0, 0};
+  q.w.C = a.dw; q.w.M = g.N; q.w.steps = g.blocks; q.w.axis = 1;
+  const Cut cut = cut_of(T, a.rows, a.experts, a.N, a.K, a.dx, a.dw, ncu);
+  if (cut.x == 3) launch_gemms<E, T, q8::Tile128Ahead, q8::Tile128Ahead>(q, a, s);
+  else if (cut.x == 1 && cut.w == 1) launch_gemms<E, T, q8::Tile128, q8::Tile128>(q, a, s);
+  else if (cut.x == 1) launch_gemms<E, T, q8::Tile128, q8::Tile64>(q, a, s);
+  else if (cut.x == 0 && cut.w == 1) launch_gemms<E, T, q8::Tile64, q8::Tile128>(q, a, s);
+  else if (cut.x == 0) launch_gemms<E, T, q8::Tile64, q8::Tile64>(q, a, s);
+  else if constexpr (T != FMM_F32) launch_gemms<E, T, q8::Tile256, q8::Tile256>(q, a, s);
   return hipGetLastError();
 }
 
@@ -292,7 +354,14 @@ size_t grad_scratch(int, int64_t rows, int64_t experts, int64_t N, int64_t K, in
   return layout_of(rows, experts, N, K).total;
 }
 
-const char *grad_kernel_name(int, int64_t, int64_t, int64_t, int64_t, bool, bool, int) { return "grad_kernel 64x64 64x64"; }
+const char *grad_kernel_name(int type, int64_t rows, int64_t experts, int64_t N, int64_t K, bool dx, bool dw, int ncu) {
+  static const char *const small[2][2] = {{"grad_kernel 64x64 64x64", "grad_kernel 64x64 128x128"},
+                                          {"grad_kernel 128x128 64x64", "grad_kernel 128x128 128x128"}};
+  const Cut c = cut_of(type, rows, experts, N, K, dx, dw, ncu);
+  if (c.x == 2) return "grad_kernel 256x256 256x256";
+  if (c.x == 3) return "grad_kernel 128x128 128x128 ahead";
+  return small[c.x][c.w];
+}
 
 int launch_grad(int type, const GradArgs &a, int ncu, void *stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);

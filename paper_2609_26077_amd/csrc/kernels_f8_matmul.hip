@@ -160,13 +160,14 @@ __global__ __launch_bounds__(64 * W) void few_tokens_kernel(Product g) {
 // the int8 product.
 struct Shape {
   int tm, tn, waves;            // tile, and the waves that share its contracted axis
-  float start, chain, work;
   bool one;                     // only where each CU has one group at most
+  float start, chain, work;     // of 16-bit outputs, and of fp32
+  float start32, chain32, work32;
 };
 constexpr Shape kShapes[] = {
-    {16, 16, 8, 1.7f, 0.30f, 0.57f, false}, {32, 32, 4, 2.2f, 0.37f, 0.61f, false},
-    {64, 64, 1, 3.2f, 0.19f, 0.28f, false}, {128, 128, 1, 3.3f, 0.45f, 0.60f, true},
-    {128, 128, 1, 3.6f, 0.47f, 0.62f, false}, {256, 256, 1, 8.7f, 1.2f, 1.8f, false},
+    {16, 16, 8, false, 3.12f, 0.20f, 0.58f, 3.56f, 0.41f, 0.57f},  {32, 32, 4, false, 3.34f, 0.35f, 0.72f, 3.63f, 0.50f, 0.84f},
+    {64, 64, 1, false, 3.67f, 0.30f, 0.30f, 3.73f, 0.56f, 0.43f},  {128, 128, 1, true, 3.78f, 0.55f, 0.49f, 3.77f, 0.82f, 1.22f},
+    {128, 128, 1, false, 3.62f, 0.65f, 0.60f, 3.68f, 0.92f, 0.82f}, {256, 256, 1, false, 7.3f, 1.1f, 1.75f, 0.0f, 0.0f, 0.0f},
 };
 constexpr int kShapeCount = sizeof(kShapes) / sizeof(kShapes[0]);
 constexpr double kMaxGroups = 1 << 22;
@@ -182,7 +183,8 @@ int pick(int type, const Product &g, int ncu) {
     const double groups = experts * std::ceil(rows / p.tm) * ((g.N + p.tn - 1) / p.tn);
     if (groups > kMaxGroups || (p.one && groups > ncu)) continue;
     const double pieces = (g.steps + p.waves - 1) / p.waves;
-    const double t = p.start + std::max(p.chain * pieces, p.work * pieces * groups / ncu);
+    const double t = type == FMM_F32 ? p.start32 + std::max(p.chain32 * pieces, p.work32 * pieces * groups / ncu)
+                                     : p.start + std::max(p.chain * pieces, p.work * pieces * groups / ncu);
     if (t < least) {
       best = i;
       least = t;
