@@ -79,7 +79,7 @@ struct Tensor {
   int64_t n;
   int type;
 };
-constexpr int kClipBlocks = 1024;          // partial sums of a call
+constexpr int kClipBlocks = 2048;          // partial sums of a call
 constexpr int kClipTable = 120;            // tensors of a launch
 constexpr int64_t kMaxClipElements = 1ll << 42;
 int launch_clip(const Tensor *t, int count, float most, float *norm, double *partial, void *stream);

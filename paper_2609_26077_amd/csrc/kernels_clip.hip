@@ -44,41 +44,50 @@ __device__ __forceinline__ int tensor_of(const Table &t, int chunk) {
   return lo;
 }
 
+// A whole chunk's loads are under way at once: kLoads vectors a thread.
+constexpr int kLoads = kChunk / (8 * 256);
+
+template <int T>
+struct Part {
+  q8::Raw8<T> raw[kLoads];
+  __device__ __forceinline__ Part(const void *in, int64_t n) {
+    const elem_t<T> *p = static_cast<const elem_t<T> *>(in);
+    const int at = 8 * threadIdx.x;
+    if (n == kChunk) {
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) raw[u] = q8::raw8<T>(p + at + 2048 * u, 8);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) raw[u] = q8::raw8<T>(p + at + 2048 * u, n - at - 2048 * u);
+    }
+  }
+};
+
 template <int T>
 __device__ __forceinline__ double squares(const void *in, int64_t n) {
-  const elem_t<T> *p = static_cast<const elem_t<T> *>(in);
+  const Part<T> x(in, n);
   double s = 0.0;
-  for (int64_t i = 8 * threadIdx.x; i < n; i += 8 * 256 * 4) {
-    q8::Raw8<T> raw[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) raw[u] = q8::raw8<T>(p + i + 2048 * u, n - i - 2048 * u);
+  for (int u = 0; u < kLoads; ++u) {
+    float v[8];
+    q8::floats8<T>(x.raw[u], v);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      float v[8];
-      q8::floats8<T>(raw[u], v);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) s = fma((double)v[k], (double)v[k], s);
-    }
+    for (int k = 0; k < 8; ++k) s = fma((double)v[k], (double)v[k], s);
   }
   return s;
 }
 
 template <int T>
 __device__ __forceinline__ void scale(const void *in, void *out, int64_t n, float c) {
-  const elem_t<T> *p = static_cast<const elem_t<T> *>(in);
-  elem_t<T> *q = static_cast<elem_t<T> *>(out);
-  for (int64_t i = 8 * threadIdx.x; i < n; i += 8 * 256 * 4) {
-    q8::Raw8<T> raw[4];
+  const Part<T> x(in, n);
+  elem_t<T> *q = static_cast<elem_t<T> *>(out) + 8 * threadIdx.x;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) raw[u] = q8::raw8<T>(p + i + 2048 * u, n - i - 2048 * u);
+  for (int u = 0; u < kLoads; ++u) {
+    float v[8];
+    q8::floats8<T>(x.raw[u], v);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      float v[8];
-      q8::floats8<T>(raw[u], v);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] *= c;
-      q8::store8<T>(q + i + 2048 * u, n - i - 2048 * u, v);
-    }
+    for (int k = 0; k < 8; ++k) v[k] *= c;
+    q8::store8<T>(q + 2048 * u, n - 8 * (int)threadIdx.x - 2048 * u, v);
   }
 }
 

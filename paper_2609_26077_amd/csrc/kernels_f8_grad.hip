@@ -43,37 +43,42 @@ __device__ __forceinline__ void transpose4(uint32_t (&w)[4]) {
   w[3] = __builtin_amdgcn_perm(d, b, 0x07060302);
 }
 
-// One 128 x 128 tile a workgroup: thread t has eight columns of rows 8 (t / 16) .. + 7.
-// The transpose goes through LDS in pieces of eight bytes (eight rows of a column);
-// piece p of column n sits at p ^ (n / 8), so that both directions spread over the banks.
+// One 128 x 128 tile a workgroup of 512: thread t has eight columns of rows 4 (t / 16) .. + 3.
+// (Of 256 with eight rows each: 1000 x 1302 x 1472 fp32, where a CU has one tile or two, 11.9 us.)
+// The transpose goes through LDS in pieces of four bytes (four rows of a column);
+// piece p of column n sits at p ^ 2 (n / 8), so that both directions spread over the banks
+// and sixteen bytes stay together but for their order.
+constexpr int kRows = 4, kLayoutThreads = 512;
+
 struct Turn {
-  u32x2 out[128][16];
-  uint32_t most[4][128];
-  float sum[4][128];
+  uint32_t out[128][32];
+  uint32_t most[8][128];
+  float sum[8][128];
 };
+__device__ __forceinline__ int piece(int p, int n) { return p ^ (2 * (n >> 3) & 31); }
 
 // the tile's columns n < cols to rows of dst
 __device__ __forceinline__ void store_columns(const Turn &tile, uint8_t *dst, int64_t pitch, int cols) {
   const int t = threadIdx.x, c = t & 7;
 #pragma unroll
-  for (int p = 0; p < 4; ++p) {
-    const int n = 32 * p + (t >> 3), k = n >> 3;
+  for (int p = 0; p < 2; ++p) {
+    const int n = 64 * p + (t >> 3);
     if (n < cols) {
-      const u32x4 v = *reinterpret_cast<const u32x4 *>(&tile.out[n][(2 * c ^ k) & ~1]);
-      *reinterpret_cast<u32x4 *>(dst + n * pitch + 16 * c) = k & 1 ? (u32x4){v[2], v[3], v[0], v[1]} : v;
+      const u32x4 v = *reinterpret_cast<const u32x4 *>(&tile.out[n][piece(4 * c, n) & ~3]);
+      *reinterpret_cast<u32x4 *>(dst + n * pitch + 16 * c) = n >> 3 & 1 ? (u32x4){v[2], v[3], v[0], v[1]} : v;
     }
   }
 }
 
 // codes by columns of v, and their scales to scales[n * pitch]
-__device__ __forceinline__ void columns(Turn &tile, const float (&v)[8][8], uint8_t *dst, int64_t pitch, uint8_t *scales,
+__device__ __forceinline__ void columns(Turn &tile, const float (&v)[kRows][8], uint8_t *dst, int64_t pitch, uint8_t *scales,
                                         int64_t scale_pitch, int cols) {
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, rg = t >> 4, cg = t & 15;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     uint32_t a = 0;
 #pragma unroll
-    for (int r = 0; r < 8; ++r) a = max(a, magnitude(v[r][i]));
+    for (int r = 0; r < kRows; ++r) a = max(a, magnitude(v[r][i]));
     a = max(a, (uint32_t)__shfl_xor((int)a, 16));
     a = max(a, (uint32_t)__shfl_xor((int)a, 32));
     if (lane < 16) tile.most[wave][8 * cg + i] = a;
@@ -82,20 +87,19 @@ __device__ __forceinline__ void columns(Turn &tile, const float (&v)[8][8], uint
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int n = 8 * cg + i;
-    const uint32_t b = scale_byte(max(max(tile.most[0][n], tile.most[1][n]), max(tile.most[2][n], tile.most[3][n])));
-    const float s = scale_value(b);
+    uint32_t a = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) a = max(a, tile.most[k][n]);
+    const uint32_t b = scale_byte(a);
     if (rg == 0 && n < cols) scales[n * scale_pitch] = (uint8_t)b;
-    u32x2 q;
-    q[0] = codes4(v[0][i], v[1][i], v[2][i], v[3][i], s);
-    q[1] = codes4(v[4][i], v[5][i], v[6][i], v[7][i], s);
-    tile.out[n][rg ^ cg] = q;
+    tile.out[n][piece(rg, n)] = codes4(v[0][i], v[1][i], v[2][i], v[3][i], scale_value(b));
   }
   __syncthreads();
   store_columns(tile, dst, pitch, cols);
 }
 
 template <int T>
-__global__ __launch_bounds__(256) void layout_kernel(LayoutArgs g) {
+__global__ __launch_bounds__(kLayoutThreads) void layout_kernel(LayoutArgs g) {
   __shared__ Turn tile;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, rg = t >> 4, cg = t & 15;
   int id = blockIdx.x;
@@ -104,18 +108,17 @@ __global__ __launch_bounds__(256) void layout_kernel(LayoutArgs g) {
     id -= g.jobs_dy + g.jobs_a;
     const int kb = id % g.bk, nb = id / g.bk % g.bn, e = id / g.bk / g.bn;
     const int n0 = nb * kBlock, k0 = kb * kBlock;
-    const uint8_t *src = g.w + ((int64_t)e * g.N + n0) * g.Kp + k0;
-    u32x2 q[8];
+    const uint8_t *src = g.w + ((int64_t)e * g.N + n0 + kRows * rg) * g.Kp + k0 + 8 * cg;
+    u32x2 q[kRows];
 #pragma unroll
-    for (int r = 0; r < 8; ++r)
-      q[r] = n0 + 8 * rg + r < g.N ? *reinterpret_cast<const u32x2 *>(src + (8 * rg + r) * g.Kp + 8 * cg) : (u32x2){0, 0};
+    for (int r = 0; r < kRows; ++r)
+      q[r] = n0 + kRows * rg + r < g.N ? *reinterpret_cast<const u32x2 *>(src + r * g.Kp) : (u32x2){0, 0};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      uint32_t lo[4] = {q[0][h], q[1][h], q[2][h], q[3][h]}, hi[4] = {q[4][h], q[5][h], q[6][h], q[7][h]};
-      transpose4(lo);
-      transpose4(hi);
+      uint32_t w[4] = {q[0][h], q[1][h], q[2][h], q[3][h]};
+      transpose4(w);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) tile.out[8 * cg + 4 * h + i][rg ^ cg] = (u32x2){lo[i], hi[i]};
+      for (int i = 0; i < 4; ++i) tile.out[8 * cg + 4 * h + i][piece(rg, 8 * cg)] = w[i];
     }
     __syncthreads();
     store_columns(tile, g.wt + ((int64_t)e * g.K + k0) * g.Np + n0, g.Np, g.K - k0);
@@ -130,21 +133,24 @@ __global__ __launch_bounds__(256) void layout_kernel(LayoutArgs g) {
   const Span s = x.find(block);
   const int row0 = s.lo + (block - s.tiles) * kBlock, rows = s.hi - row0;
   const int64_t sb = (int64_t)s.wides * kScalePad + block - s.tiles;   // the block's scales
-  float v[8][8];
+  float v[kRows][8];
   if (is_dy) {
-    const elem_t<T> *src = static_cast<const elem_t<T> *>(g.dy) + (int64_t)(row0 + 8 * rg) * g.N + c0 + 8 * cg;
+    const elem_t<T> *src = static_cast<const elem_t<T> *>(g.dy) + (int64_t)(row0 + kRows * rg) * g.N + c0 + 8 * cg;
+    q8::Raw8<T> raw[kRows];
 #pragma unroll
-    for (int r = 0; r < 8; ++r) q8::load8<T>(src + (int64_t)r * g.N, 8 * rg + r < rows ? cols - 8 * cg : 0, v[r]);
+    for (int r = 0; r < kRows; ++r) raw[r] = q8::raw8<T>(src + (int64_t)r * g.N, kRows * rg + r < rows ? cols - 8 * cg : 0);
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) q8::floats8<T>(raw[r], v[r]);
     if (g.want_dx) {
 #pragma unroll
-      for (int r = 0; r < 8; ++r) {
+      for (int r = 0; r < kRows; ++r) {
         uint32_t a = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) a = max(a, magnitude(v[r][i]));
         const uint32_t b = scale_byte(q8::max16(a));
         const float sc = scale_value(b);
-        const int64_t row = row0 + 8 * rg + r;
-        if (8 * rg + r < rows) {
+        const int64_t row = row0 + kRows * rg + r;
+        if (kRows * rg + r < rows) {
           u32x2 q;
           q[0] = codes4(v[r][0], v[r][1], v[r][2], v[r][3], sc);
           q[1] = codes4(v[r][4], v[r][5], v[r][6], v[r][7], sc);
@@ -158,30 +164,34 @@ __global__ __launch_bounds__(256) void layout_kernel(LayoutArgs g) {
       for (int i = 0; i < 8; ++i) {
         float c = 0.0f;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) c += v[r][i];
+        for (int r = 0; r < kRows; ++r) c += v[r][i];
         c += __shfl_xor(c, 16);
         c += __shfl_xor(c, 32);
         if (lane < 16) tile.sum[wave][8 * cg + i] = c;
       }
       __syncthreads();
-      if (t < 128 && t < cols)
-        g.colsum[(int64_t)block * g.N + c0 + t] = (tile.sum[0][t] + tile.sum[1][t]) + (tile.sum[2][t] + tile.sum[3][t]);
+      if (t < 128 && t < cols) {
+        float c = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) c += tile.sum[k][t];
+        g.colsum[(int64_t)block * g.N + c0 + t] = c;
+      }
     }
     if (g.want_dw)
       columns(tile, v, g.dyt + c0 * g.Bp + (int64_t)block * kBlock, g.Bp, g.sdyt + c0 * g.sbp + sb, g.sbp, cols);
   } else {
-    const uint8_t *src = g.a + (int64_t)(row0 + 8 * rg) * g.Kp + c0 + 8 * cg;
-    const uint8_t *scales = g.sa + (int64_t)(row0 + 8 * rg) * g.spk + cb;
+    const uint8_t *src = g.a + (int64_t)(row0 + kRows * rg) * g.Kp + c0 + 8 * cg;
+    const uint8_t *scales = g.sa + (int64_t)(row0 + kRows * rg) * g.spk + cb;
+    u32x2 q[kRows];
+    uint32_t b[kRows];
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      u32x2 q = {0, 0};
-      uint32_t b = 127;
-      if (8 * rg + r < rows) {
-        q = *reinterpret_cast<const u32x2 *>(src + r * g.Kp);
-        b = scales[r * g.spk];
-      }
-      values8(q, scale_value(b), v[r]);
+    for (int r = 0; r < kRows; ++r) {
+      const bool some = kRows * rg + r < rows;
+      q[r] = some ? *reinterpret_cast<const u32x2 *>(src + r * g.Kp) : (u32x2){0, 0};
+      b[r] = some ? scales[r * g.spk] : 127u;
     }
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) values8(q[r], scale_value(b[r]), v[r]);
     columns(tile, v, g.xt + c0 * g.Bp + (int64_t)block * kBlock, g.Bp, g.sxt + c0 * g.sbp + sb, g.sbp, cols);
   }
 }
@@ -326,7 +336,7 @@ int launch(const GradArgs &a, int ncu, hipStream_t s) {
   g.jobs_a = g.want_dw ? g.blocks * g.bk : 0;
   g.jobs_w = g.want_dx && a.rows > 0 ? g.experts * g.bn * g.bk : 0;
   const int jobs = g.jobs_dy + g.jobs_a + g.jobs_w;
-  if (jobs > 0) layout_kernel<T><<<dim3((unsigned)jobs), 256, 0, s>>>(g);
+  if (jobs > 0) layout_kernel<T><<<dim3((unsigned)jobs), kLayoutThreads, 0, s>>>(g);
 
   GradGemms q = {};
   q.colsum = g.colsum; q.dbias = a.dbias;

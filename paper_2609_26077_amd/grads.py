@@ -3,33 +3,53 @@ many gradients, and clipping by it.  Checks and marshalling only: the arithmetic
 happens in the library's HIP kernels."""
 from __future__ import annotations
 
-import ctypes
-
+import numpy as np
 import torch
 
-from . import _check, _lib, fmm_clip_scratch_size
+from . import FMM_F32, _check, _lib, fmm_clip_scratch_size
 from .q8 import TYPES, _run
 
 _SCRATCH = fmm_clip_scratch_size()
 
 
-def _list(ts, name):
-    ts = list(ts)
-    for t in ts:
-        if not isinstance(t, torch.Tensor):
-            raise ValueError(f"{name}: expected torch.Tensors, got {type(t).__name__}")
-    if not all(map(torch.Tensor.is_contiguous, ts)):
+# What a call costs is the walk over its tensors (six questions to each, 50 ns a question), so they are
+# asked by map, and all else is done on arrays.
+_Tensor = torch.Tensor
+
+
+def _table(ts, name):
+    """(types, sizes, addresses, device index) of tensors."""
+    if not set(map(type, ts)) <= {_Tensor, torch.nn.Parameter}:
+        for t in ts:
+            if not isinstance(t, _Tensor):
+                raise ValueError(f"{name}: expected torch.Tensors, got {type(t).__name__}")
+    if not all(map(_Tensor.is_contiguous, ts)):
         i = next(i for i, t in enumerate(ts) if not t.is_contiguous())
         raise ValueError(f"{name}[{i}]: not contiguous")
-    return ts
+    try:
+        types = np.array([TYPES[t.dtype] for t in ts], dtype=np.int32)
+    except KeyError:
+        raise ValueError(f"{name}: dtypes {set(t.dtype for t in ts)}, expected float32, bfloat16 or float16") from None
+    devices = set(map(_Tensor.get_device, ts))
+    if len(devices) > 1:
+        raise ValueError(f"{name}: on {sorted(str(d) for d in set(t.device for t in ts))}, expected one device")
+    return (types, np.array(list(map(_Tensor.numel, ts)), dtype=np.int64),
+            np.array(list(map(_Tensor.data_ptr, ts)), dtype=np.int64), devices.pop())
 
 
-def _apart(spans, what):
-    """Refuse memory ranges that overlap: workgroups write them in any order."""
-    spans.sort()
-    for (_, end), (start, _) in zip(spans, spans[1:]):
-        if start < end:
-            raise ValueError(f"{what}: tensors overlap")
+def _apart(to, size, at, what):
+    """Refuse outputs that overlap one another, or an input other than their own: workgroups
+    read and write them in any order."""
+    some = size > 0
+    order = np.argsort(to[some], kind="stable")
+    start, end = to[some][order], (to + size)[some][order]
+    clash = (start[1:] < end[:-1]).any()
+    if not clash and at is not to:
+        other = some & (at != to)
+        first = np.searchsorted(end, at[other], side="right")       # the first output that ends past the input's start
+        clash = (np.append(start, np.iinfo(np.int64).max)[first] < (at + size)[other]).any()
+    if clash:
+        raise ValueError(f"{what}: tensors overlap")
 
 
 def clip(grads, max_norm, out=None, stream=None):
@@ -42,41 +62,28 @@ def clip(grads, max_norm, out=None, stream=None):
     most = float(max_norm)
     if not most >= 0.0:
         raise ValueError(f"max_norm: {max_norm}, expected a number >= 0")
-    ins = _list(grads, "grads")
+    ins = list(grads)
     if not ins:
         raise ValueError("grads: no tensors")
-    outs = ins if out is None else _list(out, "out")
-    if len(outs) != len(ins):
-        raise ValueError(f"out: {len(outs)} tensors, expected {len(ins)}")
-    dev, n = ins[0].device, len(ins)
-    dtypes = [t.dtype for t in ins]
-    try:
-        types = [TYPES[d] for d in dtypes]
-    except KeyError:
-        raise ValueError(f"grads: dtypes {set(dtypes)}, expected float32, bfloat16 or float16") from None
-    if any(t.device != dev for t in ins):
-        raise ValueError(f"grads: on {[str(d) for d in {t.device for t in ins}]}, expected one device")
-    sizes, at = list(map(torch.Tensor.numel, ins)), list(map(torch.Tensor.data_ptr, ins))
-    to = at
+    types, sizes, at, index = _table(ins, "grads")
+    n, dev, to = len(ins), ins[0].device, at
+    nbytes = sizes * np.where(types == FMM_F32, 4, 2)
+    outs = () if out is None else list(out)
     if out is not None:
-        to = list(map(torch.Tensor.data_ptr, outs))
-        if [t.dtype for t in outs] != dtypes or list(map(torch.Tensor.numel, outs)) != sizes:
+        if len(outs) != n:
+            raise ValueError(f"out: {len(outs)} tensors, expected {n}")
+        to_types, to_sizes, to, to_index = _table(outs, "out")
+        if (to_types != types).any() or (to_sizes != sizes).any():
             raise ValueError("out: other dtypes or sizes than grads")
-        if any(t.device != dev for t in outs):
-            raise ValueError(f"out: not on {dev}")
-    width = [4 if t == 0 else 2 for t in types]
-    written = [(p, p + s * w) for p, s, w in zip(to, sizes, width) if s]
-    if out is not None:
-        # an output may be its own input, and nothing else's (an input may come twice)
-        written += {(p, p + s * w) for p, q, s, w in zip(at, to, sizes, width) if s and p != q}
-    _apart(written, "grads" if out is None else "out")
+        if to_index != index:
+            raise ValueError(f"out: on {outs[0].device}, expected {dev}")
+    _apart(to, nbytes, at, "grads" if out is None else "out")
 
     def call(handle):
         norm = torch.empty((), dtype=torch.float32, device=dev)
         scratch = torch.empty(_SCRATCH, dtype=torch.uint8, device=dev)
-        _check(_lib.fmm_clip((ctypes.c_int32 * n)(*types), (ctypes.c_int64 * n)(*sizes), (ctypes.c_void_p * n)(*at),
-                             (ctypes.c_void_p * n)(*to), n, most, norm.data_ptr(), scratch.data_ptr(), _SCRATCH, handle),
-               "fmm_clip")
+        _check(_lib.fmm_clip(types.ctypes.data, sizes.ctypes.data, at.ctypes.data, to.ctypes.data, n, most, norm.data_ptr(),
+                             scratch.data_ptr(), _SCRATCH, handle), "fmm_clip")
         return norm
 
-    return _run(dev, stream, call, *ins, *(outs if out is not None else ()))
+    return _run(dev, stream, call, *ins, *outs)
