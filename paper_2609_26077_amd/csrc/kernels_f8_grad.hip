@@ -309,7 +309,7 @@ void launch_gemms(GradGemms g, const GradArgs &a, hipStream_t s) {
   g.x.tiles_m = g.x.rows / TX::TM + std::min(g.x.experts, g.x.rows);
   g.w.tiles_n = (g.w.N + TW::TN - 1) / TW::TN;
   g.w.tiles_m = (g.w.M + TW::TM - 1) / TW::TM;
-  const int x = a.dx ? g.x.tiles_m * g.x.tiles_n : 0, w = a.dw ? g.w.experts * g.w.tiles_m * g.w.tiles_n : 0;
+  const int x = a.dx ? g.x.tiles_m * g.x.tiles_n : 0, w = a.dw ? g.w.experts * (int)round_up(g.w.tiles_m * g.w.tiles_n, 8) : 0;
   const int db = a.dbias ? g.w.experts * ((g.w.M + TX::kThreads - 1) / TX::kThreads) : 0;
   g.x_first = g.x.steps * g.w.experts >= g.w.steps;
   // (whole turns over the XCDs, so that the second's order is the first's)
