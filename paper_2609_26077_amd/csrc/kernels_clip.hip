@@ -20,9 +20,11 @@ namespace f8 {
 namespace {
 
 using q8::elem_t;
+using q8::u32x4;
 
 constexpr int kTable = kClipTable;
-constexpr int kChunk = 16384;      // elements of a tensor that a workgroup takes at a time
+constexpr int kChunk = 8192;       // elements of a tensor that a workgroup takes at a time
+constexpr int kScaleBlocks = 8192; // workgroups of the second pass, at most
 
 struct Table {
   const void *in[kTable];
@@ -43,7 +45,6 @@ __device__ __forceinline__ int tensor_of(const Table &t, int chunk) {
   }
   return lo;
 }
-
 // A whole chunk's loads are under way at once: kLoads vectors a thread.
 constexpr int kLoads = kChunk / (8 * 256);
 
@@ -77,6 +78,23 @@ __device__ __forceinline__ double squares(const void *in, int64_t n) {
   return s;
 }
 
+// eight consecutive elements, of which those before n exist
+template <int T>
+__device__ __forceinline__ void store(elem_t<T> *p, int64_t n, const float (&v)[8]) {
+  if (n < 8) {
+    q8::store8<T>(p, n, v);
+  } else if constexpr (T == FMM_F32) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const u32x4 w = {__float_as_uint(v[4 * h]), __float_as_uint(v[4 * h + 1]), __float_as_uint(v[4 * h + 2]), __float_as_uint(v[4 * h + 3])};
+      __builtin_nontemporal_store(w, reinterpret_cast<q8::u32x4_a4 *>(p + 4 * h));
+    }
+  } else {
+    const u32x4 w = {q8::pack2<T>(v[0], v[1]), q8::pack2<T>(v[2], v[3]), q8::pack2<T>(v[4], v[5]), q8::pack2<T>(v[6], v[7])};
+    __builtin_nontemporal_store(w, reinterpret_cast<q8::u32x4_a2 *>(p));
+  }
+}
+
 template <int T>
 __device__ __forceinline__ void scale(const void *in, void *out, int64_t n, float c) {
   const Part<T> x(in, n);
@@ -87,7 +105,7 @@ __device__ __forceinline__ void scale(const void *in, void *out, int64_t n, floa
     q8::floats8<T>(x.raw[u], v);
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] *= c;
-    q8::store8<T>(q + 2048 * u, n - 8 * (int)threadIdx.x - 2048 * u, v);
+    store<T>(q + 2048 * u, n - 8 * (int)threadIdx.x - 2048 * u, v);
   }
 }
 
@@ -105,8 +123,9 @@ __device__ __forceinline__ double sum256(double s, double *share) {
 __global__ __launch_bounds__(256) void squares_kernel(Table t, double *partial) {
   __shared__ double share[4];
   double s = 0.0;
-  for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
-    const int i = tensor_of(t, c), type = t.type[i];
+  for (int c = blockIdx.x, i = tensor_of(t, c); c < t.chunks; c += gridDim.x) {
+    while (c >= t.first[i + 1]) ++i;
+    const int type = t.type[i];
     const int64_t at = (int64_t)(c - t.first[i]) * kChunk, n = min(t.n[i] - at, (int64_t)kChunk);
     const uint8_t *p = static_cast<const uint8_t *>(t.in[i]) + at * (type == FMM_F32 ? 4 : 2);
     s += type == FMM_F32 ? squares<FMM_F32>(p, n) : type == FMM_BF16 ? squares<FMM_BF16>(p, n) : squares<FMM_F16>(p, n);
@@ -123,8 +142,9 @@ __global__ __launch_bounds__(256) void clip_kernel(Table t, const double *partia
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)s;
   const double ratio = (double)most / (s + 1e-6);
   const float f = ratio > 1.0 ? 1.0f : (float)ratio;     // (NaN stays)
-  for (int c = t.chunks - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
-    const int i = tensor_of(t, c), type = t.type[i];
+  for (int c = t.chunks - 1 - blockIdx.x, i = tensor_of(t, c); c >= 0; c -= gridDim.x) {
+    while (c < t.first[i]) --i;
+    const int type = t.type[i];
     if (f == 1.0f && t.in[i] == t.out[i]) continue;
     const int64_t at = (int64_t)(c - t.first[i]) * kChunk, n = min(t.n[i] - at, (int64_t)kChunk);
     const int64_t bytes = at * (type == FMM_F32 ? 4 : 2);
@@ -172,7 +192,7 @@ int launch_clip(const Tensor *t, int count, float most, float *norm, double *par
   for (int at = 0; at < count || !told;) {
     at = fill(t, count, at, b);
     if (b.chunks == 0 && told) continue;
-    clip_kernel<<<dim3((unsigned)std::max(1, std::min(b.chunks, 2048))), 256, 0, s>>>(b, partial, partials, most,
+    clip_kernel<<<dim3((unsigned)std::max(1, std::min(b.chunks, kScaleBlocks))), 256, 0, s>>>(b, partial, partials, most,
                                                                                       told ? nullptr : norm);
     told = true;
   }

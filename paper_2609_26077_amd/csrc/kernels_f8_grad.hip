@@ -43,26 +43,28 @@ __device__ __forceinline__ void transpose4(uint32_t (&w)[4]) {
   w[3] = __builtin_amdgcn_perm(d, b, 0x07060302);
 }
 
-// One 128 x 128 tile a workgroup of 512: thread t has eight columns of rows 4 (t / 16) .. + 3.
-// (Of 256 with eight rows each: 1000 x 1302 x 1472 fp32, where a CU has one tile or two, 11.9 us.)
+// One 128 x 128 tile a workgroup: thread t has eight columns of R rows from R (t / 16) on.  R is 4 where
+// a CU has few tiles and their latency counts, else 8 (1000 x 1302 x 1472 fp32 11.0 us for 11.9, 16384 x
+// 4096 x 2048 bf16 of 16 experts 120 us for 137).
 // The transpose goes through LDS in pieces of four bytes (four rows of a column);
 // piece p of column n sits at p ^ 2 (n / 8), so that both directions spread over the banks
 // and sixteen bytes stay together but for their order.
-constexpr int kRows = 4, kLayoutThreads = 512;
-
+template <int R>
 struct Turn {
+  static constexpr int kThreads = 2048 / R, kWaves = kThreads / 64;
   uint32_t out[128][32];
-  uint32_t most[8][128];
-  float sum[8][128];
+  uint32_t most[kWaves][128];
+  float sum[kWaves][128];
 };
 __device__ __forceinline__ int piece(int p, int n) { return p ^ (2 * (n >> 3) & 31); }
 
 // the tile's columns n < cols to rows of dst
-__device__ __forceinline__ void store_columns(const Turn &tile, uint8_t *dst, int64_t pitch, int cols) {
+template <int R>
+__device__ __forceinline__ void store_columns(const Turn<R> &tile, uint8_t *dst, int64_t pitch, int cols) {
   const int t = threadIdx.x, c = t & 7;
 #pragma unroll
-  for (int p = 0; p < 2; ++p) {
-    const int n = 64 * p + (t >> 3);
+  for (int p = 0; p < R / 2; ++p) {
+    const int n = Turn<R>::kThreads / 8 * p + (t >> 3);
     if (n < cols) {
       const u32x4 v = *reinterpret_cast<const u32x4 *>(&tile.out[n][piece(4 * c, n) & ~3]);
       *reinterpret_cast<u32x4 *>(dst + n * pitch + 16 * c) = n >> 3 & 1 ? (u32x4){v[2], v[3], v[0], v[1]} : v;
@@ -71,14 +73,15 @@ __device__ __forceinline__ void store_columns(const Turn &tile, uint8_t *dst, in
 }
 
 // codes by columns of v, and their scales to scales[n * pitch]
-__device__ __forceinline__ void columns(Turn &tile, const float (&v)[kRows][8], uint8_t *dst, int64_t pitch, uint8_t *scales,
+template <int R>
+__device__ __forceinline__ void columns(Turn<R> &tile, const float (&v)[R][8], uint8_t *dst, int64_t pitch, uint8_t *scales,
                                         int64_t scale_pitch, int cols) {
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, rg = t >> 4, cg = t & 15;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     uint32_t a = 0;
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) a = max(a, magnitude(v[r][i]));
+    for (int r = 0; r < R; ++r) a = max(a, magnitude(v[r][i]));
     a = max(a, (uint32_t)__shfl_xor((int)a, 16));
     a = max(a, (uint32_t)__shfl_xor((int)a, 32));
     if (lane < 16) tile.most[wave][8 * cg + i] = a;
@@ -89,18 +92,21 @@ __device__ __forceinline__ void columns(Turn &tile, const float (&v)[kRows][8], 
     const int n = 8 * cg + i;
     uint32_t a = 0;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) a = max(a, tile.most[k][n]);
+    for (int k = 0; k < Turn<R>::kWaves; ++k) a = max(a, tile.most[k][n]);
     const uint32_t b = scale_byte(a);
     if (rg == 0 && n < cols) scales[n * scale_pitch] = (uint8_t)b;
-    tile.out[n][piece(rg, n)] = codes4(v[0][i], v[1][i], v[2][i], v[3][i], scale_value(b));
+    const float s = scale_value(b);
+#pragma unroll
+    for (int r = 0; r < R; r += 4)
+      tile.out[n][piece((R * rg + r) / 4, n)] = codes4(v[r][i], v[r + 1][i], v[r + 2][i], v[r + 3][i], s);
   }
   __syncthreads();
   store_columns(tile, dst, pitch, cols);
 }
 
-template <int T>
-__global__ __launch_bounds__(kLayoutThreads) void layout_kernel(LayoutArgs g) {
-  __shared__ Turn tile;
+template <int T, int R>
+__global__ __launch_bounds__(Turn<R>::kThreads) void layout_kernel(LayoutArgs g) {
+  __shared__ Turn<R> tile;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, rg = t >> 4, cg = t & 15;
   int id = blockIdx.x;
   if (id >= g.jobs_dy + g.jobs_a) {
@@ -108,17 +114,20 @@ __global__ __launch_bounds__(kLayoutThreads) void layout_kernel(LayoutArgs g) {
     id -= g.jobs_dy + g.jobs_a;
     const int kb = id % g.bk, nb = id / g.bk % g.bn, e = id / g.bk / g.bn;
     const int n0 = nb * kBlock, k0 = kb * kBlock;
-    const uint8_t *src = g.w + ((int64_t)e * g.N + n0 + kRows * rg) * g.Kp + k0 + 8 * cg;
-    u32x2 q[kRows];
+    const uint8_t *src = g.w + ((int64_t)e * g.N + n0 + R * rg) * g.Kp + k0 + 8 * cg;
+    u32x2 q[R];
 #pragma unroll
-    for (int r = 0; r < kRows; ++r)
-      q[r] = n0 + kRows * rg + r < g.N ? *reinterpret_cast<const u32x2 *>(src + r * g.Kp) : (u32x2){0, 0};
+    for (int r = 0; r < R; ++r)
+      q[r] = n0 + R * rg + r < g.N ? *reinterpret_cast<const u32x2 *>(src + r * g.Kp) : (u32x2){0, 0};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      uint32_t w[4] = {q[0][h], q[1][h], q[2][h], q[3][h]};
-      transpose4(w);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) tile.out[8 * cg + 4 * h + i][piece(rg, 8 * cg)] = w[i];
+      for (int r = 0; r < R; r += 4) {
+        uint32_t w[4] = {q[r][h], q[r + 1][h], q[r + 2][h], q[r + 3][h]};
+        transpose4(w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tile.out[8 * cg + 4 * h + i][piece((R * rg + r) / 4, 8 * cg)] = w[i];
+      }
     }
     __syncthreads();
     store_columns(tile, g.wt + ((int64_t)e * g.K + k0) * g.Np + n0, g.Np, g.K - k0);
@@ -133,24 +142,24 @@ __global__ __launch_bounds__(kLayoutThreads) void layout_kernel(LayoutArgs g) {
   const Span s = x.find(block);
   const int row0 = s.lo + (block - s.tiles) * kBlock, rows = s.hi - row0;
   const int64_t sb = (int64_t)s.wides * kScalePad + block - s.tiles;   // the block's scales
-  float v[kRows][8];
+  float v[R][8];
   if (is_dy) {
-    const elem_t<T> *src = static_cast<const elem_t<T> *>(g.dy) + (int64_t)(row0 + kRows * rg) * g.N + c0 + 8 * cg;
-    q8::Raw8<T> raw[kRows];
+    const elem_t<T> *src = static_cast<const elem_t<T> *>(g.dy) + (int64_t)(row0 + R * rg) * g.N + c0 + 8 * cg;
+    q8::Raw8<T> raw[R];
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) raw[r] = q8::raw8<T>(src + (int64_t)r * g.N, kRows * rg + r < rows ? cols - 8 * cg : 0);
+    for (int r = 0; r < R; ++r) raw[r] = q8::raw8<T>(src + (int64_t)r * g.N, R * rg + r < rows ? cols - 8 * cg : 0);
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) q8::floats8<T>(raw[r], v[r]);
+    for (int r = 0; r < R; ++r) q8::floats8<T>(raw[r], v[r]);
     if (g.want_dx) {
 #pragma unroll
-      for (int r = 0; r < kRows; ++r) {
+      for (int r = 0; r < R; ++r) {
         uint32_t a = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) a = max(a, magnitude(v[r][i]));
         const uint32_t b = scale_byte(q8::max16(a));
         const float sc = scale_value(b);
-        const int64_t row = row0 + kRows * rg + r;
-        if (kRows * rg + r < rows) {
+        const int64_t row = row0 + R * rg + r;
+        if (R * rg + r < rows) {
           u32x2 q;
           q[0] = codes4(v[r][0], v[r][1], v[r][2], v[r][3], sc);
           q[1] = codes4(v[r][4], v[r][5], v[r][6], v[r][7], sc);
@@ -164,7 +173,7 @@ __global__ __launch_bounds__(kLayoutThreads) void layout_kernel(LayoutArgs g) {
       for (int i = 0; i < 8; ++i) {
         float c = 0.0f;
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) c += v[r][i];
+        for (int r = 0; r < R; ++r) c += v[r][i];
         c += __shfl_xor(c, 16);
         c += __shfl_xor(c, 32);
         if (lane < 16) tile.sum[wave][8 * cg + i] = c;
@@ -173,25 +182,25 @@ __global__ __launch_bounds__(kLayoutThreads) void layout_kernel(LayoutArgs g) {
       if (t < 128 && t < cols) {
         float c = 0.0f;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) c += tile.sum[k][t];
+        for (int k = 0; k < Turn<R>::kWaves; ++k) c += tile.sum[k][t];
         g.colsum[(int64_t)block * g.N + c0 + t] = c;
       }
     }
     if (g.want_dw)
       columns(tile, v, g.dyt + c0 * g.Bp + (int64_t)block * kBlock, g.Bp, g.sdyt + c0 * g.sbp + sb, g.sbp, cols);
   } else {
-    const uint8_t *src = g.a + (int64_t)(row0 + kRows * rg) * g.Kp + c0 + 8 * cg;
-    const uint8_t *scales = g.sa + (int64_t)(row0 + kRows * rg) * g.spk + cb;
-    u32x2 q[kRows];
-    uint32_t b[kRows];
+    const uint8_t *src = g.a + (int64_t)(row0 + R * rg) * g.Kp + c0 + 8 * cg;
+    const uint8_t *scales = g.sa + (int64_t)(row0 + R * rg) * g.spk + cb;
+    u32x2 q[R];
+    uint32_t b[R];
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-      const bool some = kRows * rg + r < rows;
+    for (int r = 0; r < R; ++r) {
+      const bool some = R * rg + r < rows;
       q[r] = some ? *reinterpret_cast<const u32x2 *>(src + r * g.Kp) : (u32x2){0, 0};
       b[r] = some ? scales[r * g.spk] : 127u;
     }
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) values8(q[r], scale_value(b[r]), v[r]);
+    for (int r = 0; r < R; ++r) values8(q[r], scale_value(b[r]), v[r]);
     columns(tile, v, g.xt + c0 * g.Bp + (int64_t)block * kBlock, g.Bp, g.sxt + c0 * g.sbp + sb, g.sbp, cols);
   }
 }
@@ -336,7 +345,8 @@ int launch(const GradArgs &a, int ncu, hipStream_t s) {
   g.jobs_a = g.want_dw ? g.blocks * g.bk : 0;
   g.jobs_w = g.want_dx && a.rows > 0 ? g.experts * g.bn * g.bk : 0;
   const int jobs = g.jobs_dy + g.jobs_a + g.jobs_w;
-  if (jobs > 0) layout_kernel<T><<<dim3((unsigned)jobs), kLayoutThreads, 0, s>>>(g);
+  if (jobs > 4 * ncu) layout_kernel<T, 8><<<dim3((unsigned)jobs), Turn<8>::kThreads, 0, s>>>(g);
+  else if (jobs > 0) layout_kernel<T, 4><<<dim3((unsigned)jobs), Turn<4>::kThreads, 0, s>>>(g);
 
   GradGemms q = {};
   q.colsum = g.colsum; q.dbias = a.dbias;
