@@ -53,6 +53,7 @@ struct Product {
   int M, N;                  // rows of C (axis: of each C), columns
   int steps;                 // 128-byte steps of the contracted axis (axis: at most)
   int axis, out_bytes;       // out_bytes: of an element of C
+  int turned;                // rows of a B that lies along the contracted axis
   int tiles_m, tiles_n;      // (tiles_m with experts and not axis: at most)
 };
 

@@ -12,6 +12,10 @@
 // 256 tile's wave holds 48 registers of them beside its 128 sums (a whole half step
 // of both ahead would take 96).  The barrier stands before the last slot.
 //
+// TURNED: B comes as it lies, rows along the contracted axis (dX's weights), in the 256 tile: a step is then 128 rows
+// of 256 bytes in LDS, 16-byte chunk c of row n at c ^ (n & 15), and a lane takes its codes eight at a time by
+// ds_read_b64_tr_b8, which hands lane l of sixteen byte l of eight rows of sixteen.
+//
 // Scales stay out of LDS, which the ring of the larger tiles fills: a lane keeps four
 // steps' bytes of each of its rows as a word, shifted right by a byte a step.  The
 // following words are loaded at the start of the last step of four and waited for at
@@ -105,7 +109,7 @@ struct F8Exact {
 // the ids of one XCD get a contiguous range of items, tiles run in groups of GM tile rows.  Where
 // the contracted axis is the experts', whose lengths differ, each expert's tiles are spread over the XCDs
 // (dW of 16384 x 4096 x 2048 of 16 experts with uneven rows, experts dealt to the XCDs: 270 us).
-template <int TM, int TN, bool WEIGHTS>
+template <int TM, int TN, bool WEIGHTS, bool TURNED = false>
 __device__ __forceinline__ bool work_of(const Product &g, int id, Work &w) {
   constexpr int GM = TM == 256 ? 4 : 8;
   Span s;
@@ -132,7 +136,7 @@ __device__ __forceinline__ bool work_of(const Product &g, int id, Work &w) {
   const int64_t e = s.expert;
   w.a = g.a.codes + e * g.a.expert_codes + w.m0 * g.a.pitch;
   w.sa = g.a.scales + e * g.a.expert_scales + w.m0 * g.a.scale_pitch;
-  w.b = g.b.codes + e * g.b.expert_codes + w.n0 * g.b.pitch;
+  w.b = g.b.codes + e * g.b.expert_codes + w.n0 * (TURNED ? 1 : g.b.pitch);
   w.sb = g.b.scales + e * g.b.expert_scales + (WEIGHTS ? w.n0 / kBlock : w.n0) * g.b.scale_pitch;
   w.rows_a = w.M - w.m0;
   w.rows_b = g.N - w.n0;
@@ -150,8 +154,11 @@ __device__ __forceinline__ bool work_of(const Product &g, int id, Work &w) {
   return true;
 }
 
-template <class E, class T, int OUT, bool WEIGHTS>
+typedef int v2i __attribute__((ext_vector_type(2)));
+
+template <class E, class T, int OUT, bool WEIGHTS, bool TURNED = false>
 __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4 *lds_raw) {
+  static_assert(!TURNED || (WEIGHTS && T::TN == 256 && T::JB == 4 && T::NI == 2), "rows of 256 bytes, sixteen a wave");
   constexpr int J = T::JA, MI = T::MI, NI = T::NI, SB = WEIGHTS ? 1 : NI, Q = 2 * MI;
   static_assert(!WEIGHTS || NI * 32 <= kBlock, "one scale of the weights for a wave's columns");
   const uint8_t *lds = reinterpret_cast<const uint8_t *>(lds_raw);
@@ -205,10 +212,14 @@ __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4
     const int row = 8 * (wave * J + j) + lrow;
     const uint32_t c = 16u * (uint32_t)(lpos ^ swz128(row));
     offa[j] = (uint32_t)(min(row, w.rows_a - 1) * g.a.pitch) + c;
-    offb[j] = (uint32_t)(min(row, w.rows_b - 1) * g.b.pitch) + c;
+    // (TURNED: rows 16 wave + 4 j + lane / 16; without the row's own offset, chunks past the row's end repeat its last)
+    if (TURNED) offb[j] = 16u * (uint32_t)min((lane & 15) ^ (4 * j + (lane >> 4)), (int)((g.b.pitch - w.n0) / 16) - 1);
+    else offb[j] = (uint32_t)(min(row, w.rows_b - 1) * g.b.pitch) + c;
   }
+  const uint32_t rowb = (uint32_t)((16 * wave + (lane >> 4)) * g.b.pitch);
+  int leftb = g.turned;   // rows from the next step's first on
   const uint8_t *pa = w.a, *pb = w.b;   // the next step's
-  const uint32_t base = dma::lds_addr(lds_raw) + wave * J * 1024;
+  const uint32_t base0 = dma::lds_addr(lds_raw), base = base0 + wave * J * 1024;
   uint32_t wa = 0, wb = T::kHalf, ra = 0, rb = T::kHalf;   // half-slots to fill and to read next, in bytes
   auto turn = [](uint32_t &x) {
     x += 2 * T::kHalf;
@@ -225,10 +236,15 @@ __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4
   };
   auto start_b = [&](int q, int some) {
 #pragma unroll
-    for (int j = q * J / 2; j < (q + 1) * J / 2; ++j) copy16_if(some, offb[j], pb, base + wb + j * 1024);
+    for (int j = q * J / 2; j < (q + 1) * J / 2; ++j) {
+      const uint32_t last = (uint32_t)((min(leftb, kBlock) - 1) * g.b.pitch);
+      const uint32_t off = TURNED ? min(rowb + 4 * j * (uint32_t)g.b.pitch, last) + offb[j] : offb[j];
+      copy16_if(some, off, pb, base + wb + j * 1024);
+    }
     if (q == 1) {
       turn(wb);
-      pb += kStep;
+      pb += TURNED ? kStep * g.b.pitch : kStep;
+      leftb -= kStep;
     }
   };
 
@@ -240,7 +256,10 @@ __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4
 
   // byte of chunk h of the lane's row in the first 32-row tile of each side (chunk 2 u + h: xor 32 u)
   const uint32_t ca = (uint32_t)(wm * MI * 32 + r32) * kStep + 16u * (uint32_t)(h ^ swz128(r32));
-  const uint32_t cb = (uint32_t)(wn * NI * 32 + r32) * kStep + 16u * (uint32_t)(h ^ swz128(r32));
+  // (TURNED: lane s of sixteen takes half s & 1 of chunk s / 16 & 1 of the wave's columns in row s / 2 of eight, sixteen rows on in half h)
+  const uint32_t cb = TURNED ? (uint32_t)((lane >> 1 & 7) + 16 * h) * 256 + 8u * (lane & 1) +
+                                   16u * (uint32_t)((4 * wn + (lane >> 4 & 1)) ^ (lane >> 1 & 7))
+                             : (uint32_t)(wn * NI * 32 + r32) * kStep + 16u * (uint32_t)(h ^ swz128(r32));
   auto read = [&](uint32_t at, int half) {
     const v4i lo = *reinterpret_cast<const v4i *>(lds + (at ^ (64u * half)));
     const v4i hi = *reinterpret_cast<const v4i *>(lds + (at ^ (64u * half + 32u)));
@@ -251,7 +270,20 @@ __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4
   auto load_a = [&](int half, int i, int buf) { fa[buf] = read(ra + ca + i * 32 * kStep, half); };
   auto load_b = [&](int half, int buf) {
 #pragma unroll
-    for (int j = 0; j < NI; ++j) fb[buf][j] = read(rb + cb + j * 32 * kStep, half);
+    for (int j = 0; j < NI; ++j) {
+      if constexpr (TURNED) {
+        // chunks 4 half + h and 4 half + 2 + h of sixteen rows, eight rows at a time
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const uint32_t at = ((rb + cb) ^ (32u * j) ^ (128u * (p & 1))) + (64 * half + 32 * (p >> 1) + 8 * (p & 1)) * 256;
+          const v2i v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) v2i *)(base0 + at));
+          fb[buf][j][2 * p] = v[0];
+          fb[buf][j][2 * p + 1] = v[1];
+        }
+      } else {
+        fb[buf][j] = read(rb + cb + j * 32 * kStep, half);
+      }
+    }
   };
   // every wave's transfers of the next step have landed (where later > 0, kLater of
   // this wave's may be on their way) and its reads of this one are done

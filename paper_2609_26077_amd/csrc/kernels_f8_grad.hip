@@ -3,7 +3,8 @@
 // counted from the expert's first row, X being the codes of the forward pass.
 //
 // The layout pass brings every operand into rows along its contracted axis: dY
-// by rows (dyr) and by columns (dyt), X by columns (xt), W by columns (wt).  W's
+// by rows (dyr) and by columns (dyt), X by columns (xt), W by columns (wt; the 256 tile reads W as
+// it lies, and only the scales are turned).  W's
 // codes move as they are, a 128 x 128 block's scale being that of its transpose;
 // X's are rounded again where the new block's scale is larger than the old one
 // (codes below 2^-15 of the block's largest).  It also leaves dY's column sums by block.
@@ -31,6 +32,7 @@ struct LayoutArgs {
   int blocks, bn, bk;                // blocks of rows (at most), of N, of K
   int jobs_dy, jobs_a, jobs_w;
   int want_dx, want_dw, want_db;
+  int scales_only;                   // of W: a job an expert
 };
 
 // 4 x 4 bytes: words of rows to words of columns
@@ -112,6 +114,13 @@ __global__ __launch_bounds__(Turn<R>::kThreads) void layout_kernel(LayoutArgs g)
   if (id >= g.jobs_dy + g.jobs_a) {
     // W: rows n, columns k
     id -= g.jobs_dy + g.jobs_a;
+    if (g.scales_only) {
+      for (int i = t; i < g.bn * g.bk; i += Turn<R>::kThreads) {
+        const int kb = i / g.bn, nb = i - kb * g.bn;
+        g.swt[((int64_t)id * g.bk + kb) * g.spn + nb] = g.sw[((int64_t)id * g.bn + nb) * g.spk + kb];
+      }
+      return;
+    }
     const int kb = id % g.bk, nb = id / g.bk % g.bn, e = id / g.bk / g.bn;
     const int n0 = nb * kBlock, k0 = kb * kBlock;
     const uint8_t *src = g.w + ((int64_t)e * g.N + n0 + R * rg) * g.Kp + k0 + 8 * cg;
@@ -214,6 +223,10 @@ struct GradGemms {
 };
 
 // Tiles TX of dX and TW of dW (equal workgroups), then dY's column sums by expert.
+// whether dX's tile reads W as it lies
+template <class TX>
+constexpr bool kTurned = TX::TM == 256;
+
 template <class E, class TX, class TW, int OUT>
 __global__ __launch_bounds__(TX::kThreads, 2) void grad_kernel(GradGemms g) {
   static_assert(TX::kThreads == TW::kThreads, "one launch");
@@ -224,7 +237,7 @@ __global__ __launch_bounds__(TX::kThreads, 2) void grad_kernel(GradGemms g) {
     const bool first = id < g.items0;
     if (!first) id -= g.items0;
     if (first == (g.x_first != 0)) {
-      if (work_of<TX::TM, TX::TN, true>(g.x, id, w)) gemm_tile<E, TX, OUT, true>(g.x, w, lds);
+      if (work_of<TX::TM, TX::TN, true, kTurned<TX>>(g.x, id, w)) gemm_tile<E, TX, OUT, true, kTurned<TX>>(g.x, w, lds);
     } else {
       if (work_of<TW::TM, TW::TN, false>(g.w, id, w)) gemm_tile<E, TW, OUT, false>(g.w, w, lds);
     }
@@ -249,7 +262,7 @@ struct Layout {
   size_t dyr, sdyr, dyt, sdyt, xt, sxt, wt, swt, colsum, total;
   int64_t blocks, Np, Bp, spn, sbp;
 };
-Layout layout_of(int64_t rows, int64_t experts, int64_t N, int64_t K) {
+Layout layout_of(int64_t rows, int64_t experts, int64_t N, int64_t K, bool turn_w) {
   Layout l;
   const int64_t full = std::min(experts, rows);      // experts that may have rows
   l.blocks = rows / kBlock + full;
@@ -269,7 +282,7 @@ Layout layout_of(int64_t rows, int64_t experts, int64_t N, int64_t K) {
   l.sdyt = take(N * l.sbp);
   l.xt = take(K * l.Bp);
   l.sxt = take(K * l.sbp);
-  l.wt = take(experts * K * l.Np);
+  l.wt = take(turn_w ? experts * K * l.Np : 0);
   l.swt = take(experts * (pitch_of(K) / kBlock) * l.spn);
   l.colsum = take(4 * l.blocks * N);
   l.total = at;
@@ -329,7 +342,9 @@ void launch_gemms(GradGemms g, const GradArgs &a, hipStream_t s) {
 
 template <class E, int T>
 int launch(const GradArgs &a, int ncu, hipStream_t s) {
-  const Layout l = layout_of(a.rows, a.experts, a.N, a.K);
+  const Cut cut = cut_of(T, a.rows, a.experts, a.N, a.K, a.dx, a.dw, ncu);
+  const bool turn_w = a.dx && cut.x != 2;
+  const Layout l = layout_of(a.rows, a.experts, a.N, a.K, turn_w);
   LayoutArgs g = {};
   g.dy = a.dy; g.a = a.a; g.sa = a.sa; g.w = a.w; g.sw = a.sw; g.offsets = a.offsets;
   g.dyr = a.ws + l.dyr; g.sdyr = a.ws + l.sdyr;
@@ -343,7 +358,8 @@ int launch(const GradArgs &a, int ncu, hipStream_t s) {
   g.want_dx = a.dx != nullptr; g.want_dw = a.dw != nullptr; g.want_db = a.dbias != nullptr;
   g.jobs_dy = g.want_dx || g.want_dw || g.want_db ? g.blocks * g.bn : 0;
   g.jobs_a = g.want_dw ? g.blocks * g.bk : 0;
-  g.jobs_w = g.want_dx && a.rows > 0 ? g.experts * g.bn * g.bk : 0;
+  g.scales_only = !turn_w;
+  g.jobs_w = !g.want_dx || a.rows == 0 ? 0 : turn_w ? g.experts * g.bn * g.bk : g.experts;
   const int jobs = g.jobs_dy + g.jobs_a + g.jobs_w;
   if (jobs > 4 * ncu) layout_kernel<T, 8><<<dim3((unsigned)jobs), Turn<8>::kThreads, 0, s>>>(g);
   else if (jobs > 0) layout_kernel<T, 4><<<dim3((unsigned)jobs), Turn<4>::kThreads, 0, s>>>(g);
@@ -354,11 +370,14 @@ int launch(const GradArgs &a, int ncu, hipStream_t s) {
   q.w = q.x;
   q.x.a = {g.dyr, g.sdyr, g.Np, g.spn, 0, 0};
   q.x.b = {g.wt, g.swt, g.Np, g.spn, a.K * g.Np, (int64_t)g.bk * g.spn};
+  if (!turn_w) {
+    q.x.b = {a.w, g.swt, g.Kp, g.spn, a.N * g.Kp, (int64_t)g.bk * g.spn};
+    q.x.turned = g.N;
+  }
   q.x.C = a.dx; q.x.M = g.rows; q.x.steps = g.bn;
   q.w.a = {g.dyt, g.sdyt, g.Bp, g.sbp, 0, 0};
   q.w.b = {g.xt, g.sxt, g.Bp, g.sbp, 0, 0};
   q.w.C = a.dw; q.w.M = g.N; q.w.steps = g.blocks; q.w.axis = 1;
-  const Cut cut = cut_of(T, a.rows, a.experts, a.N, a.K, a.dx, a.dw, ncu);
   if (cut.x == 3) launch_gemms<E, T, q8::Tile128Ahead, q8::Tile128Ahead>(q, a, s);
   else if (cut.x == 1 && cut.w == 1) launch_gemms<E, T, q8::Tile128, q8::Tile128>(q, a, s);
   else if (cut.x == 1) launch_gemms<E, T, q8::Tile128, q8::Tile64>(q, a, s);
@@ -370,8 +389,11 @@ int launch(const GradArgs &a, int ncu, hipStream_t s) {
 
 }  // namespace
 
-size_t grad_scratch(int, int64_t rows, int64_t experts, int64_t N, int64_t K, int) {
-  return layout_of(rows, experts, N, K).total;
+// (what is wanted is not known here: room for what any choice of it takes)
+size_t grad_scratch(int type, int64_t rows, int64_t experts, int64_t N, int64_t K, int ncu) {
+  const bool turn_w = cut_of(type, rows, experts, N, K, true, true, ncu).x != 2 ||
+                      cut_of(type, rows, experts, N, K, true, false, ncu).x != 2;
+  return layout_of(rows, experts, N, K, turn_w).total;
 }
 
 const char *grad_kernel_name(int type, int64_t rows, int64_t experts, int64_t N, int64_t K, bool dx, bool dw, int ncu) {

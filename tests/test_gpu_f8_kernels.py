@@ -1,0 +1,126 @@
+"""Each kernel that the e4m3 layers' products come in, over few steps of the contracted axis and
+many, against binary64 products on the GPU of the values that the codes stand for (the codes
+themselves are compared bit for bit in test_gpu_f8).  Bars as there."""
+from __future__ import annotations
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+HALF_ULP = {"fp32": 2.0 ** -24, "bf16": 2.0 ** -8, "fp16": 2.0 ** -11}
+TYPE = {"fp32": 0, "bf16": 1, "fp16": 2}
+
+# kernel, type, rows, experts (0: a single weight), N, K
+PRODUCTS = []
+# kernel, type, rows, experts, N, K, wanted (dX, dW)
+GRADIENTS = [
+    ("grad_kernel 256x256 256x256", "bf16", 2500, 0, 2500, 2500, (1, 1)),
+    ("grad_kernel 256x256 256x256", "fp16", 3000, 3, 1500, 2100, (1, 1)),
+    ("grad_kernel 256x256 256x256", "bf16", 1249, 0, 1238, 5005, (1, 1)),
+]
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    return torch
+
+
+@pytest.fixture(scope="module")
+def f8():
+    from paper_2609_26077_amd import f8
+    return f8
+
+
+def dtype_of(torch, t):
+    return {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[t]
+
+
+def inputs(torch, f8, t, rows, experts, N, K):
+    g = torch.Generator(device="cuda").manual_seed(rows + N + K)
+
+    def normal(*s):
+        return torch.randn(*s, generator=g, device="cuda")
+
+    x = normal(rows, K) * torch.exp(normal(rows, 1))          # rows whose scales lie apart
+    a, sa = f8.quantize(x)
+    w, sw = f8.quantize_weight(normal(max(1, experts), N, K) * 0.02)
+    va = f8.dequantize(a, sa, K).double()
+    vw = f8.dequantize(w, sw, K).double()
+    E = max(1, experts)
+    # uneven, one without rows, the first and the last rows nobody's where there are experts
+    cut = [0, rows] if not experts else sorted([rows // 9] + [rows * (3 * e * e + 1) // (3 * E * E + 2) for e in range(1, E)] + [rows - 3])
+    if E > 2:
+        cut[2] = cut[1]
+    off = torch.tensor(cut, dtype=torch.int32).cuda() if experts else None
+    bias = normal(E, N)
+    dy = (normal(rows, N) * torch.exp(normal(rows, 1)) * 0.05).to(dtype_of(torch, t))
+    return a, sa, w, sw, va, vw, off, list(zip(cut, cut[1:])), bias, dy
+
+
+def within(torch, got, want, bound, what):
+    err = (got.double() - want).abs()
+    worst = float((err / bound).max()) if err.numel() else 0.0
+    assert worst <= 1.0, f"{what}: {worst:.3g} of the bound"
+
+
+def bound(t, S, C, n):
+    own = (n * U + 2.0 ** -19) * S
+    return own + HALF_ULP[t] * (C.abs() + own) + (0 if t == "fp32" else 7 * 2.0 ** -13 * S) + 2.0 ** -24
+
+
+def product(a, b):
+    """a b^T (b copied: a transposed view is not handed to the library)."""
+    return a @ b.t().contiguous()
+
+
+@pytest.mark.parametrize("kernel,t,rows,experts,N,K", PRODUCTS)
+def test_product(torch, f8, kernel, t, rows, experts, N, K):
+    import paper_2609_26077_amd as fm
+    assert fm.fmm_f8_matmul_kernel(fm.fmm_f8_desc(rows, max(1, experts), N, K, TYPE[t])) == kernel
+    a, sa, w, sw, va, vw, off, span, bias, _ = inputs(torch, f8, t, rows, experts, N, K)
+    C = torch.full((rows, N), 7.0, dtype=dtype_of(torch, t), device="cuda")
+    if experts:
+        f8.GroupedLinearF8(rows, experts, N, K, C.dtype).matmul(a, sa, w, sw, off, bias, C=C)
+    else:
+        f8.LinearF8(rows, N, K, C.dtype).matmul(a, sa, w[0], sw[0], bias[0], C=C)
+    left = torch.ones(rows, dtype=torch.bool, device="cuda")
+    for e, (lo, hi) in enumerate(span):
+        left[lo:hi] = False
+        want, S = product(va[lo:hi], vw[e]), product(va[lo:hi].abs(), vw[e].abs())
+        b = bias[e].double()
+        within(torch, C[lo:hi], want + b, bound(t, S, want, K) + (2 * U + HALF_ULP[t]) * (want.abs() + 2 * b.abs()), f"expert {e}")
+    assert bool((C[left] == 7).all())
+
+
+@pytest.mark.parametrize("kernel,t,rows,experts,N,K,want", GRADIENTS)
+def test_gradients(torch, f8, kernel, t, rows, experts, N, K, want):
+    import paper_2609_26077_amd as fm
+    assert fm.fmm_f8_linear_backward_kernel(fm.fmm_f8_desc(rows, max(1, experts), N, K, TYPE[t]), *want) == kernel
+    a, sa, w, sw, va, vw, off, span, _, dy = inputs(torch, f8, t, rows, experts, N, K)
+    kw = dict(need_x=bool(want[0]), need_w=bool(want[1]), bias=True)
+    if experts:
+        dx, dw, db = f8.GroupedLinearF8(rows, experts, N, K, dy.dtype).backward(dy, a, sa, w, sw, off, **kw)
+    else:
+        dx, dw, db = f8.LinearF8(rows, N, K, dy.dtype).backward(dy, a, sa, w[0], sw[0], **kw)
+        dw, db = dw if dw is None else dw[None], db[None]
+
+    def rounded(v):
+        """The values of the codes of v's rows, which test_gpu_f8 compares with the rule's."""
+        return f8.dequantize(*f8.quantize(v.contiguous()), v.shape[1]).double()
+
+    yr = rounded(dy)
+    for e, (lo, hi) in enumerate(span):
+        y = dy[lo:hi]
+        if want[0]:
+            C, S = product(yr[lo:hi], vw[e].t()), product(yr[lo:hi].abs(), vw[e].abs().t())
+            within(torch, dx[lo:hi], C, bound(t, S, C, N), f"dX of expert {e}")
+        if want[1] and hi > lo:
+            yc, xc = rounded(y.t()), rounded(va[lo:hi].float().t())
+            C, S = product(yc, xc), product(yc.abs(), xc.abs())
+            within(torch, dw[e], C, bound(t, S, C, hi - lo), f"dW of expert {e}")
+        elif want[1]:
+            assert bool((dw[e] == 0).all())
+        s = y.double()
+        within(torch, db[e], s.sum(0), 2 * (hi - lo + 1) * U * s.abs().sum(0) + 1e-30, f"dbias of expert {e}")
