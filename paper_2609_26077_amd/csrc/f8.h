@@ -43,7 +43,8 @@ struct Side {
 };
 
 // C = A B^T.  Either A's rows belong to the experts, each with a B of its own
-// (axis false), or the contracted axis does, and each expert has a C (axis true).
+// (axis false), or the contracted axis does, and each expert has a C (axis true; the rows of its operands
+// then lie together, those of one expert after those of another, as long as its blocks are).
 struct Product {
   Side a, b;
   void *C;

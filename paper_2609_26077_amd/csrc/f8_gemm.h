@@ -57,6 +57,7 @@ __device__ __forceinline__ void wait_vmcnt_if(int some) {
 // of 128 codes that it contracts.
 struct Work {
   const uint8_t *a, *b, *sa, *sb;   // codes and scales of the tile's first rows, from the first step on
+  int64_t pitch_a, pitch_b, scale_pitch_a, scale_pitch_b;   // bytes of a row
   int rows_a, rows_b;               // rows that exist (of the tile and past it)
   int steps;
   void *C;                          // the matrix that the tile is of ...
@@ -134,21 +135,30 @@ __device__ __forceinline__ bool work_of(const Product &g, int id, Work &w) {
   }
   w.n0 = tn * TN;
   const int64_t e = s.expert;
-  w.a = g.a.codes + e * g.a.expert_codes + w.m0 * g.a.pitch;
-  w.sa = g.a.scales + e * g.a.expert_scales + w.m0 * g.a.scale_pitch;
-  w.b = g.b.codes + e * g.b.expert_codes + w.n0 * (TURNED ? 1 : g.b.pitch);
-  w.sb = g.b.scales + e * g.b.expert_scales + (WEIGHTS ? w.n0 / kBlock : w.n0) * g.b.scale_pitch;
   w.rows_a = w.M - w.m0;
   w.rows_b = g.N - w.n0;
-  w.steps = g.steps;
-  w.C = g.C;
   if (g.axis) {
+    // an expert's rows of both operands lie together, as long as its blocks are
     w.steps = (s.hi - s.lo + kBlock - 1) / kBlock;
-    w.a += (int64_t)s.tiles * kBlock;
-    w.b += (int64_t)s.tiles * kBlock;
-    w.sa += (int64_t)s.wides * kScalePad;
-    w.sb += (int64_t)s.wides * kScalePad;
+    w.pitch_a = w.pitch_b = (int64_t)w.steps * kBlock;
+    w.scale_pitch_a = w.scale_pitch_b = (w.steps + kScalePad - 1) / kScalePad * kScalePad;
+    const int64_t before = (int64_t)s.tiles * kBlock, scales_before = (int64_t)s.wides * kScalePad;
+    w.a = g.a.codes + before * g.M + w.m0 * w.pitch_a;
+    w.b = g.b.codes + before * g.N + w.n0 * w.pitch_b;
+    w.sa = g.a.scales + scales_before * g.M + w.m0 * w.scale_pitch_a;
+    w.sb = g.b.scales + scales_before * g.N + w.n0 * w.scale_pitch_b;
     w.C = static_cast<uint8_t *>(g.C) + e * g.M * g.N * g.out_bytes;
+  } else {
+    w.steps = g.steps;
+    w.pitch_a = g.a.pitch;
+    w.pitch_b = g.b.pitch;
+    w.scale_pitch_a = g.a.scale_pitch;
+    w.scale_pitch_b = g.b.scale_pitch;
+    w.a = g.a.codes + e * g.a.expert_codes + w.m0 * w.pitch_a;
+    w.b = g.b.codes + e * g.b.expert_codes + w.n0 * (TURNED ? 1 : w.pitch_b);
+    w.sa = g.a.scales + e * g.a.expert_scales + w.m0 * w.scale_pitch_a;
+    w.sb = g.b.scales + e * g.b.expert_scales + (WEIGHTS ? w.n0 / kBlock : w.n0) * w.scale_pitch_b;
+    w.C = g.C;
   }
   w.bias = g.bias ? g.bias + e * g.N + w.n0 : nullptr;
   return true;
@@ -171,11 +181,11 @@ __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4
   // scales of steps 4 i .. 4 i + 3, the first in the low byte
   uint32_t psa[MI], psb[SB];
 #pragma unroll
-  for (int i = 0; i < MI; ++i) psa[i] = (uint32_t)(min((wm * MI + i) * 32 + r32, w.rows_a - 1) * g.a.scale_pitch);
+  for (int i = 0; i < MI; ++i) psa[i] = (uint32_t)(min((wm * MI + i) * 32 + r32, w.rows_a - 1) * w.scale_pitch_a);
 #pragma unroll
   for (int j = 0; j < SB; ++j) {
     const int row = WEIGHTS ? min(wn * NI * 32, w.rows_b - 1) / kBlock : min((wn * NI + j) * 32 + r32, w.rows_b - 1);
-    psb[j] = (uint32_t)(row * g.b.scale_pitch);
+    psb[j] = (uint32_t)(row * w.scale_pitch_b);
   }
   uint32_t sa[MI], sb[SB], na[MI], nb[SB];
   auto load_scales = [&](int step) {
@@ -211,12 +221,12 @@ __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4
   for (int j = 0; j < J; ++j) {
     const int row = 8 * (wave * J + j) + lrow;
     const uint32_t c = 16u * (uint32_t)(lpos ^ swz128(row));
-    offa[j] = (uint32_t)(min(row, w.rows_a - 1) * g.a.pitch) + c;
+    offa[j] = (uint32_t)(min(row, w.rows_a - 1) * w.pitch_a) + c;
     // (TURNED: rows 16 wave + 4 j + lane / 16; without the row's own offset, chunks past the row's end repeat its last)
-    if (TURNED) offb[j] = 16u * (uint32_t)min((lane & 15) ^ (4 * j + (lane >> 4)), (int)((g.b.pitch - w.n0) / 16) - 1);
-    else offb[j] = (uint32_t)(min(row, w.rows_b - 1) * g.b.pitch) + c;
+    if (TURNED) offb[j] = 16u * (uint32_t)min((lane & 15) ^ (4 * j + (lane >> 4)), (int)((w.pitch_b - w.n0) / 16) - 1);
+    else offb[j] = (uint32_t)(min(row, w.rows_b - 1) * w.pitch_b) + c;
   }
-  const uint32_t rowb = (uint32_t)((16 * wave + (lane >> 4)) * g.b.pitch);
+  const uint32_t rowb = (uint32_t)((16 * wave + (lane >> 4)) * w.pitch_b);
   int leftb = g.turned;   // rows from the next step's first on
   const uint8_t *pa = w.a, *pb = w.b;   // the next step's
   const uint32_t base0 = dma::lds_addr(lds_raw), base = base0 + wave * J * 1024;
@@ -237,13 +247,13 @@ __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4
   auto start_b = [&](int q, int some) {
 #pragma unroll
     for (int j = q * J / 2; j < (q + 1) * J / 2; ++j) {
-      const uint32_t last = (uint32_t)((min(leftb, kBlock) - 1) * g.b.pitch);
-      const uint32_t off = TURNED ? min(rowb + 4 * j * (uint32_t)g.b.pitch, last) + offb[j] : offb[j];
+      const uint32_t last = (uint32_t)((min(leftb, kBlock) - 1) * w.pitch_b);
+      const uint32_t off = TURNED ? min(rowb + 4 * j * (uint32_t)w.pitch_b, last) + offb[j] : offb[j];
       copy16_if(some, off, pb, base + wb + j * 1024);
     }
     if (q == 1) {
       turn(wb);
-      pb += TURNED ? kStep * g.b.pitch : kStep;
+      pb += TURNED ? kStep * w.pitch_b : kStep;
       leftb -= kStep;
     }
   };

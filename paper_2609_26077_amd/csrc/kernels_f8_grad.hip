@@ -23,11 +23,11 @@ struct LayoutArgs {
   const uint8_t *a, *sa, *w, *sw;
   const int32_t *offsets;
   uint8_t *dyr, *sdyr;      // [rows][Np], [rows][spn]
-  uint8_t *dyt, *sdyt;      // [N][Bp], [N][sbp]: column 128 j is the first row of the j-th block of rows
-  uint8_t *xt, *sxt;        // [K][Bp], [K][sbp]
+  uint8_t *dyt, *sdyt;      // of each expert [N][128 blocks], [N][blocks, padded to 16], blocks: of 128 of its rows
+  uint8_t *xt, *sxt;        // the same with K
   uint8_t *wt, *swt;        // [experts][K][Np], [experts][K / 128][spn]
   float *colsum;            // [blocks][N]
-  int64_t Np, Kp, spn, spk, Bp, sbp;
+  int64_t Np, Kp, spn, spk;
   int rows, experts, N, K;
   int blocks, bn, bk;                // blocks of rows (at most), of N, of K
   int jobs_dy, jobs_a, jobs_w;
@@ -150,7 +150,10 @@ __global__ __launch_bounds__(Turn<R>::kThreads) void layout_kernel(LayoutArgs g)
   if (block >= x.total) return;
   const Span s = x.find(block);
   const int row0 = s.lo + (block - s.tiles) * kBlock, rows = s.hi - row0;
-  const int64_t sb = (int64_t)s.wides * kScalePad + block - s.tiles;   // the block's scales
+  // where the expert's codes by columns and their scales begin (bytes of a row before them), the rows' bytes
+  const int64_t before = (int64_t)s.tiles * kBlock, scales_before = (int64_t)s.wides * kScalePad;
+  const int mine = (s.hi - s.lo + kBlock - 1) / kBlock, at = block - s.tiles;
+  const int64_t Bp = (int64_t)mine * kBlock, sbp = (mine + kScalePad - 1) / kScalePad * kScalePad;
   float v[R][8];
   if (is_dy) {
     const elem_t<T> *src = static_cast<const elem_t<T> *>(g.dy) + (int64_t)(row0 + R * rg) * g.N + c0 + 8 * cg;
@@ -196,7 +199,7 @@ __global__ __launch_bounds__(Turn<R>::kThreads) void layout_kernel(LayoutArgs g)
       }
     }
     if (g.want_dw)
-      columns(tile, v, g.dyt + c0 * g.Bp + (int64_t)block * kBlock, g.Bp, g.sdyt + c0 * g.sbp + sb, g.sbp, cols);
+      columns(tile, v, g.dyt + before * g.N + c0 * Bp + at * kBlock, Bp, g.sdyt + scales_before * g.N + c0 * sbp + at, sbp, cols);
   } else {
     const uint8_t *src = g.a + (int64_t)(row0 + R * rg) * g.Kp + c0 + 8 * cg;
     const uint8_t *scales = g.sa + (int64_t)(row0 + R * rg) * g.spk + cb;
@@ -210,7 +213,7 @@ __global__ __launch_bounds__(Turn<R>::kThreads) void layout_kernel(LayoutArgs g)
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) values8(q[r], scale_value(b[r]), v[r]);
-    columns(tile, v, g.xt + c0 * g.Bp + (int64_t)block * kBlock, g.Bp, g.sxt + c0 * g.sbp + sb, g.sbp, cols);
+    columns(tile, v, g.xt + before * g.K + c0 * Bp + at * kBlock, Bp, g.sxt + scales_before * g.K + c0 * sbp + at, sbp, cols);
   }
 }
 
@@ -260,16 +263,15 @@ size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 struct Layout {
   size_t dyr, sdyr, dyt, sdyt, xt, sxt, wt, swt, colsum, total;
-  int64_t blocks, Np, Bp, spn, sbp;
+  int64_t blocks, Np, spn;
 };
 Layout layout_of(int64_t rows, int64_t experts, int64_t N, int64_t K, bool turn_w) {
   Layout l;
   const int64_t full = std::min(experts, rows);      // experts that may have rows
   l.blocks = rows / kBlock + full;
   l.Np = pitch_of(N);
-  l.Bp = l.blocks * kBlock;
   l.spn = scale_pitch_of(N);
-  l.sbp = kScalePad * (l.blocks / kScalePad + full);
+  const int64_t Bp = l.blocks * kBlock, sbp = kScalePad * (l.blocks / kScalePad + full);   // rows of all experts' blocks
   size_t at = 0;
   auto take = [&](int64_t bytes) {
     const size_t here = at;
@@ -278,10 +280,10 @@ Layout layout_of(int64_t rows, int64_t experts, int64_t N, int64_t K, bool turn_
   };
   l.dyr = take(rows * l.Np);
   l.sdyr = take(rows * l.spn);
-  l.dyt = take(N * l.Bp);
-  l.sdyt = take(N * l.sbp);
-  l.xt = take(K * l.Bp);
-  l.sxt = take(K * l.sbp);
+  l.dyt = take(N * Bp);
+  l.sdyt = take(N * sbp);
+  l.xt = take(K * Bp);
+  l.sxt = take(K * sbp);
   l.wt = take(turn_w ? experts * K * l.Np : 0);
   l.swt = take(experts * (pitch_of(K) / kBlock) * l.spn);
   l.colsum = take(4 * l.blocks * N);
@@ -352,7 +354,7 @@ int launch(const GradArgs &a, int ncu, hipStream_t s) {
   g.xt = a.ws + l.xt; g.sxt = a.ws + l.sxt;
   g.wt = a.ws + l.wt; g.swt = a.ws + l.swt;
   g.colsum = reinterpret_cast<float *>(a.ws + l.colsum);
-  g.Np = l.Np; g.Kp = pitch_of(a.K); g.spn = l.spn; g.spk = scale_pitch_of(a.K); g.Bp = l.Bp; g.sbp = l.sbp;
+  g.Np = l.Np; g.Kp = pitch_of(a.K); g.spn = l.spn; g.spk = scale_pitch_of(a.K);
   g.rows = (int)a.rows; g.experts = (int)a.experts; g.N = (int)a.N; g.K = (int)a.K;
   g.blocks = (int)l.blocks; g.bn = (int)(l.Np / kBlock); g.bk = (int)(g.Kp / kBlock);
   g.want_dx = a.dx != nullptr; g.want_dw = a.dw != nullptr; g.want_db = a.dbias != nullptr;
@@ -375,8 +377,8 @@ int launch(const GradArgs &a, int ncu, hipStream_t s) {
     q.x.turned = g.N;
   }
   q.x.C = a.dx; q.x.M = g.rows; q.x.steps = g.bn;
-  q.w.a = {g.dyt, g.sdyt, g.Bp, g.sbp, 0, 0};
-  q.w.b = {g.xt, g.sxt, g.Bp, g.sbp, 0, 0};
+  q.w.a.codes = g.dyt; q.w.a.scales = g.sdyt;
+  q.w.b.codes = g.xt; q.w.b.scales = g.sxt;
   q.w.C = a.dw; q.w.M = g.N; q.w.steps = g.blocks; q.w.axis = 1;
   if (cut.x == 3) launch_gemms<E, T, q8::Tile128Ahead, q8::Tile128Ahead>(q, a, s);
   else if (cut.x == 1 && cut.w == 1) launch_gemms<E, T, q8::Tile128, q8::Tile128>(q, a, s);
