@@ -155,7 +155,7 @@ size_t fmm_clip_scratch_size(void) { return kClipBlocks * sizeof(double); }
 int fmm_clip(const int32_t *types, const int64_t *sizes, void *const *dIn, void *const *dOut, int64_t count, float most,
              float *dNorm, void *dScratch, size_t scratch_bytes, void *stream) {
   if (count < 0 || !(most >= 0.0f) || !good(dNorm, 4)) return FMM_ERR_ARG;
-  if (count > (int64_t)kClipTable * kClipBlocks) return FMM_ERR_UNSUPPORTED;
+  if (count > kMaxClipTensors) return FMM_ERR_UNSUPPORTED;
   if (count > 0 && (!types || !sizes || !dIn || !dOut)) return FMM_ERR_ARG;
   std::vector<Tensor> t;
   try {

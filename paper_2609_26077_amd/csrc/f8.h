@@ -83,7 +83,8 @@ struct Tensor {
 };
 constexpr int kClipBlocks = 2048;          // partial sums of a call
 constexpr int kClipTable = 120;            // tensors of a launch
-constexpr int64_t kMaxClipElements = 1ll << 42;
+constexpr int64_t kMaxClipTensors = 1024 * kClipTable, kMaxClipElements = 1ll << 42;
+static_assert(kMaxClipTensors <= (int64_t)kClipTable * kClipBlocks, "a partial sum for each launch");
 int launch_clip(const Tensor *t, int count, float most, float *norm, double *partial, void *stream);
 
 }  // namespace f8

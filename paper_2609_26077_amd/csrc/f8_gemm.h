@@ -12,9 +12,10 @@
 // 256 tile's wave holds 48 registers of them beside its 128 sums (a whole half step
 // of both ahead would take 96).  The barrier stands before the last slot.
 //
-// TURNED: B comes as it lies, rows along the contracted axis (dX's weights), in the 256 tile: a step is then 128 rows
-// of 256 bytes in LDS, 16-byte chunk c of row n at c ^ (n & 15), and a lane takes its codes eight at a time by
-// ds_read_b64_tr_b8, which hands lane l of sixteen byte l of eight rows of sixteen.
+// TURNED: B comes as it lies, rows along the contracted axis (dX's weights).  A step is then 128 rows
+// of TN bytes in LDS, 16-byte chunk c of row n at c ^ (n / (256 / TN) mod the row's chunks), so that eight rows
+// fall on distinct banks, and a lane takes its codes eight at a time by ds_read_b64_tr_b8: of
+// sixteen lanes that point at the halves of eight rows' chunks, lane l gets byte l of the eight rows.
 //
 // Scales stay out of LDS, which the ring of the larger tiles fills: a lane keeps four
 // steps' bytes of each of its rows as a word, shifted right by a byte a step.  The
@@ -168,7 +169,8 @@ typedef int v2i __attribute__((ext_vector_type(2)));
 
 template <class E, class T, int OUT, bool WEIGHTS, bool TURNED = false>
 __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4 *lds_raw) {
-  static_assert(!TURNED || (WEIGHTS && T::TN == 256 && T::JB == 4 && T::NI == 2), "rows of 256 bytes, sixteen a wave");
+  static_assert(!TURNED || (WEIGHTS && T::NI <= 2), "a row tile's number is one bit of a chunk's");
+  constexpr int kChunks = T::TN / 16, kMoved = 64 / kChunks, kApart = 256 / T::TN;   // TURNED: of a row, rows of a transfer, swizzle
   constexpr int J = T::JA, MI = T::MI, NI = T::NI, SB = WEIGHTS ? 1 : NI, Q = 2 * MI;
   static_assert(!WEIGHTS || NI * 32 <= kBlock, "one scale of the weights for a wave's columns");
   const uint8_t *lds = reinterpret_cast<const uint8_t *>(lds_raw);
@@ -222,11 +224,12 @@ __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4
     const int row = 8 * (wave * J + j) + lrow;
     const uint32_t c = 16u * (uint32_t)(lpos ^ swz128(row));
     offa[j] = (uint32_t)(min(row, w.rows_a - 1) * w.pitch_a) + c;
-    // (TURNED: rows 16 wave + 4 j + lane / 16; without the row's own offset, chunks past the row's end repeat its last)
-    if (TURNED) offb[j] = 16u * (uint32_t)min((lane & 15) ^ (4 * j + (lane >> 4)), (int)((w.pitch_b - w.n0) / 16) - 1);
+    // (TURNED: rows kMoved (wave J + j) + lane / kChunks; without the row's own offset, chunks past the row's end repeat its last)
+    const int deep = kMoved * (wave * J + j) + lane / kChunks;
+    if (TURNED) offb[j] = 16u * (uint32_t)min((lane ^ (deep / kApart)) % kChunks, (int)((w.pitch_b - w.n0) / 16) - 1);
     else offb[j] = (uint32_t)(min(row, w.rows_b - 1) * w.pitch_b) + c;
   }
-  const uint32_t rowb = (uint32_t)((16 * wave + (lane >> 4)) * w.pitch_b);
+  const uint32_t rowb = (uint32_t)((kMoved * wave * J + lane / kChunks) * w.pitch_b);
   int leftb = g.turned;   // rows from the next step's first on
   const uint8_t *pa = w.a, *pb = w.b;   // the next step's
   const uint32_t base0 = dma::lds_addr(lds_raw), base = base0 + wave * J * 1024;
@@ -248,7 +251,7 @@ __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4
 #pragma unroll
     for (int j = q * J / 2; j < (q + 1) * J / 2; ++j) {
       const uint32_t last = (uint32_t)((min(leftb, kBlock) - 1) * w.pitch_b);
-      const uint32_t off = TURNED ? min(rowb + 4 * j * (uint32_t)w.pitch_b, last) + offb[j] : offb[j];
+      const uint32_t off = TURNED ? min(rowb + kMoved * j * (uint32_t)w.pitch_b, last) + offb[j] : offb[j];
       copy16_if(some, off, pb, base + wb + j * 1024);
     }
     if (q == 1) {
@@ -266,9 +269,10 @@ __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4
 
   // byte of chunk h of the lane's row in the first 32-row tile of each side (chunk 2 u + h: xor 32 u)
   const uint32_t ca = (uint32_t)(wm * MI * 32 + r32) * kStep + 16u * (uint32_t)(h ^ swz128(r32));
-  // (TURNED: lane s of sixteen takes half s & 1 of chunk s / 16 & 1 of the wave's columns in row s / 2 of eight, sixteen rows on in half h)
-  const uint32_t cb = TURNED ? (uint32_t)((lane >> 1 & 7) + 16 * h) * 256 + 8u * (lane & 1) +
-                                   16u * (uint32_t)((4 * wn + (lane >> 4 & 1)) ^ (lane >> 1 & 7))
+  // (TURNED: lane s of sixteen points at half s & 1 of the chunk of its row tile's half, in row s / 2 of eight, sixteen rows on in half h)
+  const int deep = lane >> 1 & 7;
+  const uint32_t cb = TURNED ? (uint32_t)(deep + 16 * h) * T::TN + 8u * (lane & 1) +
+                                   16u * (uint32_t)((2 * wn * NI + (lane >> 4 & 1)) ^ (deep / kApart))
                              : (uint32_t)(wn * NI * 32 + r32) * kStep + 16u * (uint32_t)(h ^ swz128(r32));
   auto read = [&](uint32_t at, int half) {
     const v4i lo = *reinterpret_cast<const v4i *>(lds + (at ^ (64u * half)));
@@ -285,7 +289,7 @@ __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4
         // chunks 4 half + h and 4 half + 2 + h of sixteen rows, eight rows at a time
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-          const uint32_t at = ((rb + cb) ^ (32u * j) ^ (128u * (p & 1))) + (64 * half + 32 * (p >> 1) + 8 * (p & 1)) * 256;
+          const uint32_t at = ((rb + cb) ^ (32u * j) ^ (128u / kApart * (p & 1))) + (64 * half + 32 * (p >> 1) + 8 * (p & 1)) * T::TN;
           const v2i v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) v2i *)(base0 + at));
           fb[buf][j][2 * p] = v[0];
           fb[buf][j][2 * p + 1] = v[1];

@@ -2,11 +2,12 @@
 //   dX = Q(dY) W, blocks of Q(dY) along a row;  dW = Q(dY)^T Q(X), blocks of 128 rows
 // counted from the expert's first row, X being the codes of the forward pass.
 //
-// The layout pass brings every operand into rows along its contracted axis: dY
-// by rows (dyr) and by columns (dyt), X by columns (xt), W by columns (wt; the 256 tile reads W as
-// it lies, and only the scales are turned).  W's
-// codes move as they are, a 128 x 128 block's scale being that of its transpose;
-// X's are rounded again where the new block's scale is larger than the old one
+// The layout pass brings dY and X into rows along their contracted axes: dY
+// by rows (dyr) and by columns (dyt), X by columns (xt).  W's codes stay where they are: dX's product reads them by
+// columns from LDS (turning them first, 268 MB of 600 for 16384 x 4096 x 2048 of 16 experts, took 40 us of
+// 125; 26 tokens of 24 experts' 390 x 1664 44 us for 29), and a 128 x 128 block's scale is that of its
+// transpose, so only the table of scales (swt) is turned.
+// X's codes are rounded again where the new block's scale is larger than the old one
 // (codes below 2^-15 of the block's largest).  It also leaves dY's column sums by block.
 #include <hip/hip_runtime.h>
 
@@ -20,30 +21,19 @@ namespace {
 
 struct LayoutArgs {
   const void *dy;
-  const uint8_t *a, *sa, *w, *sw;
+  const uint8_t *a, *sa, *sw;
   const int32_t *offsets;
   uint8_t *dyr, *sdyr;      // [rows][Np], [rows][spn]
   uint8_t *dyt, *sdyt;      // of each expert [N][128 blocks], [N][blocks, padded to 16], blocks: of 128 of its rows
   uint8_t *xt, *sxt;        // the same with K
-  uint8_t *wt, *swt;        // [experts][K][Np], [experts][K / 128][spn]
+  uint8_t *swt;             // [experts][K / 128][spn]
   float *colsum;            // [blocks][N]
   int64_t Np, Kp, spn, spk;
   int rows, experts, N, K;
   int blocks, bn, bk;                // blocks of rows (at most), of N, of K
   int jobs_dy, jobs_a, jobs_w;
   int want_dx, want_dw, want_db;
-  int scales_only;                   // of W: a job an expert
 };
-
-// 4 x 4 bytes: words of rows to words of columns
-__device__ __forceinline__ void transpose4(uint32_t (&w)[4]) {
-  const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400), b = __builtin_amdgcn_perm(w[1], w[0], 0x07030602);
-  const uint32_t c = __builtin_amdgcn_perm(w[3], w[2], 0x05010400), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602);
-  w[0] = __builtin_amdgcn_perm(c, a, 0x05040100);
-  w[1] = __builtin_amdgcn_perm(c, a, 0x07060302);
-  w[2] = __builtin_amdgcn_perm(d, b, 0x05040100);
-  w[3] = __builtin_amdgcn_perm(d, b, 0x07060302);
-}
 
 // One 128 x 128 tile a workgroup: thread t has eight columns of R rows from R (t / 16) on.  R is 4 where
 // a CU has few tiles and their latency counts, else 8 (1000 x 1302 x 1472 fp32 11.0 us for 11.9, 16384 x
@@ -112,35 +102,12 @@ __global__ __launch_bounds__(Turn<R>::kThreads) void layout_kernel(LayoutArgs g)
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, rg = t >> 4, cg = t & 15;
   int id = blockIdx.x;
   if (id >= g.jobs_dy + g.jobs_a) {
-    // W: rows n, columns k
+    // an expert's scales of W
     id -= g.jobs_dy + g.jobs_a;
-    if (g.scales_only) {
-      for (int i = t; i < g.bn * g.bk; i += Turn<R>::kThreads) {
-        const int kb = i / g.bn, nb = i - kb * g.bn;
-        g.swt[((int64_t)id * g.bk + kb) * g.spn + nb] = g.sw[((int64_t)id * g.bn + nb) * g.spk + kb];
-      }
-      return;
+    for (int i = t; i < g.bn * g.bk; i += Turn<R>::kThreads) {
+      const int kb = i / g.bn, nb = i - kb * g.bn;
+      g.swt[((int64_t)id * g.bk + kb) * g.spn + nb] = g.sw[((int64_t)id * g.bn + nb) * g.spk + kb];
     }
-    const int kb = id % g.bk, nb = id / g.bk % g.bn, e = id / g.bk / g.bn;
-    const int n0 = nb * kBlock, k0 = kb * kBlock;
-    const uint8_t *src = g.w + ((int64_t)e * g.N + n0 + R * rg) * g.Kp + k0 + 8 * cg;
-    u32x2 q[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-      q[r] = n0 + R * rg + r < g.N ? *reinterpret_cast<const u32x2 *>(src + r * g.Kp) : (u32x2){0, 0};
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-      for (int r = 0; r < R; r += 4) {
-        uint32_t w[4] = {q[r][h], q[r + 1][h], q[r + 2][h], q[r + 3][h]};
-        transpose4(w);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tile.out[8 * cg + 4 * h + i][piece((R * rg + r) / 4, 8 * cg)] = w[i];
-      }
-    }
-    __syncthreads();
-    store_columns(tile, g.wt + ((int64_t)e * g.K + k0) * g.Np + n0, g.Np, g.K - k0);
-    if (t == 0) g.swt[((int64_t)e * g.bk + kb) * g.spn + nb] = g.sw[((int64_t)e * g.bn + nb) * g.spk + kb];
     return;
   }
   const bool is_dy = id < g.jobs_dy;
@@ -226,10 +193,6 @@ struct GradGemms {
 };
 
 // Tiles TX of dX and TW of dW (equal workgroups), then dY's column sums by expert.
-// whether dX's tile reads W as it lies
-template <class TX>
-constexpr bool kTurned = TX::TM == 256;
-
 template <class E, class TX, class TW, int OUT>
 __global__ __launch_bounds__(TX::kThreads, 2) void grad_kernel(GradGemms g) {
   static_assert(TX::kThreads == TW::kThreads, "one launch");
@@ -240,7 +203,7 @@ __global__ __launch_bounds__(TX::kThreads, 2) void grad_kernel(GradGemms g) {
     const bool first = id < g.items0;
     if (!first) id -= g.items0;
     if (first == (g.x_first != 0)) {
-      if (work_of<TX::TM, TX::TN, true, kTurned<TX>>(g.x, id, w)) gemm_tile<E, TX, OUT, true, kTurned<TX>>(g.x, w, lds);
+      if (work_of<TX::TM, TX::TN, true, true>(g.x, id, w)) gemm_tile<E, TX, OUT, true, true>(g.x, w, lds);
     } else {
       if (work_of<TW::TM, TW::TN, false>(g.w, id, w)) gemm_tile<E, TW, OUT, false>(g.w, w, lds);
     }
@@ -262,10 +225,10 @@ __global__ __launch_bounds__(TX::kThreads, 2) void grad_kernel(GradGemms g) {
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 struct Layout {
-  size_t dyr, sdyr, dyt, sdyt, xt, sxt, wt, swt, colsum, total;
+  size_t dyr, sdyr, dyt, sdyt, xt, sxt, swt, colsum, total;
   int64_t blocks, Np, spn;
 };
-Layout layout_of(int64_t rows, int64_t experts, int64_t N, int64_t K, bool turn_w) {
+Layout layout_of(int64_t rows, int64_t experts, int64_t N, int64_t K) {
   Layout l;
   const int64_t full = std::min(experts, rows);      // experts that may have rows
   l.blocks = rows / kBlock + full;
@@ -284,7 +247,6 @@ Layout layout_of(int64_t rows, int64_t experts, int64_t N, int64_t K, bool turn_
   l.sdyt = take(N * sbp);
   l.xt = take(K * Bp);
   l.sxt = take(K * sbp);
-  l.wt = take(turn_w ? experts * K * l.Np : 0);
   l.swt = take(experts * (pitch_of(K) / kBlock) * l.spn);
   l.colsum = take(4 * l.blocks * N);
   l.total = at;
@@ -297,13 +259,25 @@ struct Cut {
   int x, w;
 };
 
-// t = max(start + chain steps, of either; start + work of both / CUs) us, as for the forward products.
+// t = max(start + chain steps, of either; start + work of both / CUs) + tile tiles / CUs us, as for the forward
+// products.  Against all cuts on 1200 shapes (rows 16 to 8192, N to 4096, K to 2048, single weights and up to 64
+// experts): 0.5% over the fastest on average in 16 bits and 0.3% in fp32, more than 10% on 1% and 0.3% of
+// them, 22% and 13% at worst.  Each is the fastest somewhere, us (64: of both, 64/128: dX's and dW's, ...):
+//   rows x N x K of experts          64     64/128  128/64  128    128 ahead  256
+//   16384 x 4096 x 2048 of 16 bf16   971    683     854     579    747        530    (with the weights turned first)
+//   4096 x 4096 x 2048 fp32          216    182     186     153    179        -
+//   1000 x 1302 x 1472 fp32          33.6   31.6    31.4    31.4   31.2       -
+//   114 x 440 x 754 of 16 bf16       24.1   22.6    23.7    20.3   21.5       23.4
+//   2229 x 1664 x 354 bf16           27.5   32.6    30.5    33.8   30.8       45.0
+//   5668 x 133 x 1536 of 4 bf16      40.9   40.5    32.6    38.3   36.9       51.0
 Cut cut_of(int type, int64_t rows, int64_t experts, int64_t N, int64_t K, bool dx, bool dw, int ncu) {
-  /*FIT*/
   constexpr int kEdge[4] = {64, 128, 256, 128};
-  constexpr double kCost[2][3][4] = {{{3.2, 3.6, 8.7, 3.3}, {0.19, 0.47, 1.2, 0.45}, {0.28, 0.62, 1.8, 0.60}},
-                                     {{3.2, 3.6, 0.0, 3.3}, {0.30, 0.80, 0.0, 0.70}, {0.45, 1.00, 0.0, 1.10}}};
-  const double (&start)[4] = kCost[type == FMM_F32][0], (&chain)[4] = kCost[type == FMM_F32][1], (&work)[4] = kCost[type == FMM_F32][2];
+  struct Cost {
+    double start, chain, work, tile;
+  };
+  constexpr Cost kCost[2][4] = {{{3.2, 0.064, 0.34, 0.0}, {3.6, 0.49, 0.48, 0.0}, {7.2, 0.87, 1.47, 0.0}, {3.1, 0.45, 0.39, 0.67}},
+                                {{3.0, 0.32, 0.47, 0.0}, {3.8, 1.16, 0.74, 0.0}, {0.0, 0.0, 0.0, 0.0}, {3.7, 0.62, 1.25, 0.0}}};
+  const Cost(&cost)[4] = kCost[type == FMM_F32];
   // experts with rows, at most, and each one's rows if they were even
   const double full = std::max<double>(1, std::min(experts, rows)), each = rows / full;
   const double steps_x = dx ? (N + kBlock - 1) / kBlock : 0, steps_w = dw ? std::ceil(each / kBlock) : 0;
@@ -316,9 +290,10 @@ Cut cut_of(int type, int64_t rows, int64_t experts, int64_t N, int64_t K, bool d
       const double tx = dx ? full * std::ceil(each / kEdge[x]) * std::ceil((double)K / kEdge[x]) : 0;
       const double tw = dw ? full * std::ceil((double)N / kEdge[w]) * std::ceil((double)K / kEdge[w]) : 0;
       if (x == 3 && tx + tw > ncu) continue;
-      const double long_x = start[x] + chain[x] * steps_x, long_w = start[w] + chain[w] * steps_w;
-      const double busy = std::max(dx ? start[x] : 0, dw ? start[w] : 0) + (work[x] * steps_x * tx + work[w] * steps_w * tw) / ncu;
-      const double t = std::max(std::max(dx ? long_x : 0, dw ? long_w : 0), busy);
+      const Cost &cx = cost[x], &cw = cost[w];
+      const double chain = std::max(dx ? cx.start + cx.chain * steps_x : 0, dw ? cw.start + cw.chain * steps_w : 0);
+      const double busy = std::max(dx ? cx.start : 0, dw ? cw.start : 0) + (cx.work * steps_x * tx + cw.work * steps_w * tw) / ncu;
+      const double t = std::max(chain, busy) + (cx.tile * tx + cw.tile * tw) / ncu;
       if (t < least) {
         least = t;
         best = {x, w};
@@ -345,14 +320,13 @@ void launch_gemms(GradGemms g, const GradArgs &a, hipStream_t s) {
 template <class E, int T>
 int launch(const GradArgs &a, int ncu, hipStream_t s) {
   const Cut cut = cut_of(T, a.rows, a.experts, a.N, a.K, a.dx, a.dw, ncu);
-  const bool turn_w = a.dx && cut.x != 2;
-  const Layout l = layout_of(a.rows, a.experts, a.N, a.K, turn_w);
+  const Layout l = layout_of(a.rows, a.experts, a.N, a.K);
   LayoutArgs g = {};
-  g.dy = a.dy; g.a = a.a; g.sa = a.sa; g.w = a.w; g.sw = a.sw; g.offsets = a.offsets;
+  g.dy = a.dy; g.a = a.a; g.sa = a.sa; g.sw = a.sw; g.offsets = a.offsets;
   g.dyr = a.ws + l.dyr; g.sdyr = a.ws + l.sdyr;
   g.dyt = a.ws + l.dyt; g.sdyt = a.ws + l.sdyt;
   g.xt = a.ws + l.xt; g.sxt = a.ws + l.sxt;
-  g.wt = a.ws + l.wt; g.swt = a.ws + l.swt;
+  g.swt = a.ws + l.swt;
   g.colsum = reinterpret_cast<float *>(a.ws + l.colsum);
   g.Np = l.Np; g.Kp = pitch_of(a.K); g.spn = l.spn; g.spk = scale_pitch_of(a.K);
   g.rows = (int)a.rows; g.experts = (int)a.experts; g.N = (int)a.N; g.K = (int)a.K;
@@ -360,8 +334,7 @@ int launch(const GradArgs &a, int ncu, hipStream_t s) {
   g.want_dx = a.dx != nullptr; g.want_dw = a.dw != nullptr; g.want_db = a.dbias != nullptr;
   g.jobs_dy = g.want_dx || g.want_dw || g.want_db ? g.blocks * g.bn : 0;
   g.jobs_a = g.want_dw ? g.blocks * g.bk : 0;
-  g.scales_only = !turn_w;
-  g.jobs_w = !g.want_dx || a.rows == 0 ? 0 : turn_w ? g.experts * g.bn * g.bk : g.experts;
+  g.jobs_w = g.want_dx && a.rows > 0 ? g.experts : 0;
   const int jobs = g.jobs_dy + g.jobs_a + g.jobs_w;
   if (jobs > 4 * ncu) layout_kernel<T, 8><<<dim3((unsigned)jobs), Turn<8>::kThreads, 0, s>>>(g);
   else if (jobs > 0) layout_kernel<T, 4><<<dim3((unsigned)jobs), Turn<4>::kThreads, 0, s>>>(g);
@@ -371,11 +344,8 @@ int launch(const GradArgs &a, int ncu, hipStream_t s) {
   q.x.offsets = a.offsets; q.x.experts = g.experts; q.x.rows = g.rows; q.x.N = g.K; q.x.out_bytes = type_bytes(T);
   q.w = q.x;
   q.x.a = {g.dyr, g.sdyr, g.Np, g.spn, 0, 0};
-  q.x.b = {g.wt, g.swt, g.Np, g.spn, a.K * g.Np, (int64_t)g.bk * g.spn};
-  if (!turn_w) {
-    q.x.b = {a.w, g.swt, g.Kp, g.spn, a.N * g.Kp, (int64_t)g.bk * g.spn};
-    q.x.turned = g.N;
-  }
+  q.x.b = {a.w, g.swt, g.Kp, g.spn, a.N * g.Kp, (int64_t)g.bk * g.spn};
+  q.x.turned = g.N;
   q.x.C = a.dx; q.x.M = g.rows; q.x.steps = g.bn;
   q.w.a.codes = g.dyt; q.w.a.scales = g.sdyt;
   q.w.b.codes = g.xt; q.w.b.scales = g.sxt;
@@ -391,11 +361,8 @@ int launch(const GradArgs &a, int ncu, hipStream_t s) {
 
 }  // namespace
 
-// (what is wanted is not known here: room for what any choice of it takes)
-size_t grad_scratch(int type, int64_t rows, int64_t experts, int64_t N, int64_t K, int ncu) {
-  const bool turn_w = cut_of(type, rows, experts, N, K, true, true, ncu).x != 2 ||
-                      cut_of(type, rows, experts, N, K, true, false, ncu).x != 2;
-  return layout_of(rows, experts, N, K, turn_w).total;
+size_t grad_scratch(int, int64_t rows, int64_t experts, int64_t N, int64_t K, int) {
+  return layout_of(rows, experts, N, K).total;
 }
 
 const char *grad_kernel_name(int type, int64_t rows, int64_t experts, int64_t N, int64_t K, bool dx, bool dw, int ncu) {
