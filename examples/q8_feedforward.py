@@ -9,7 +9,7 @@ quantized in between.  What the backward pass keeps is 8 bits an element: the
 norm's checkpoint of h, the products' operands as they are, and u's codes.  The
 master weights are float32 and are quantized after every step.
 
-    python examples/q8_feedforward.py [--tokens 4096] [--width 1024] [--hidden 4096] [--steps 30]
+    python examples/q8_feedforward.py [--tokens 4096] [--width 1024] [--hidden 4096] [--steps 30] [--max-norm 1]
 """
 from __future__ import annotations
 
@@ -25,6 +25,7 @@ if ROOT not in sys.path:
 import torch  # noqa: E402
 
 from paper_2609_26077_amd import q8  # noqa: E402
+from paper_2609_26077_amd.grads import clip  # noqa: E402
 
 
 KEPT_PLANS = 8
@@ -82,13 +83,16 @@ class FeedForward:
         dx, dgain = norm.backward(dy, rstd, self.gain_in, saved=saved, dh=dh)
         return dx, dw1, db1, dw2, db2, dgain
 
-    def step(self, grads, rate):
+    def step(self, grads, rate, max_norm=None):
+        """max_norm: the gradients are scaled down to this norm, of all of them together, first."""
+        if max_norm is not None:
+            clip(grads, max_norm)
         for p, g in zip((self.w1, self.b1, self.w2, self.b2, self.gain), grads):
             p.add_(g, alpha=-rate)
         self.quantize_weights()
 
 
-def train(layer, tokens, steps, seed=1):
+def train(layer, tokens, steps, seed=1, max_norm=None):
     """Fits out + h to a fixed random map of x by gradient descent; the losses of the steps."""
     rate = 5.0 / layer.width
     g = torch.Generator(device=layer.device).manual_seed(seed)
@@ -103,7 +107,7 @@ def train(layer, tokens, steps, seed=1):
         losses.append(err.square().mean())
         d = (err * (2.0 / tokens)).to(layer.dtype)
         _, *grads = layer.backward(d, d, kept)
-        layer.step(grads, rate)
+        layer.step(grads, rate, max_norm)
     return [float(v) for v in losses], x
 
 
@@ -113,12 +117,13 @@ def main(argv=None):
     ap.add_argument("--width", type=int, default=1024)
     ap.add_argument("--hidden", type=int, default=4096)
     ap.add_argument("--steps", type=int, default=30)
+    ap.add_argument("--max-norm", type=float, default=None, help="clip each step's gradients to this norm")
     a = ap.parse_args(argv)
     layer = FeedForward(a.width, a.hidden)
-    losses, x = train(layer, a.tokens, 2)          # (first launches)
+    losses, x = train(layer, a.tokens, 2, max_norm=a.max_norm)          # (first launches)
     torch.cuda.synchronize()
     t = time.perf_counter()
-    more, x = train(layer, a.tokens, a.steps)
+    more, x = train(layer, a.tokens, a.steps, max_norm=a.max_norm)
     torch.cuda.synchronize()
     print(f"training: loss {losses[0]:.4f} -> {more[-1]:.4f} in {a.steps + 2} steps, "
           f"{1e3 * (time.perf_counter() - t) / a.steps:.2f} ms a step of {a.tokens} tokens")

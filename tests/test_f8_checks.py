@@ -145,6 +145,30 @@ def test_clip_refuses(fm):
     assert status(fm, "fmm_clip", None, None, None, None, 122881, 1.0, P, P, need, None) == fm.FMM_ERR_UNSUPPORTED
 
 
+def test_kernels_are_named_and_each_is_tested(fm):
+    """The kernels that sizes take, over a range of sizes, against the GPU tests' lists."""
+    import test_gpu_f8_kernels as gpu
+    products, gradients = set(), set()
+    for rows in (1, 40, 300, 1300, 5000, 9000):
+        for experts in (1, 3, 8, 50):
+            for N in (8, 70, 400, 1500, 2600, 6000):
+                for K in (9, 140, 1200, 2500, 5100):
+                    for t in range(3):
+                        d = fm.fmm_f8_desc(rows, experts, N, K, t)
+                        products.add((fm.fmm_f8_matmul_kernel(d), t == 0))
+                        gradients.update((fm.fmm_f8_linear_backward_kernel(d, *w), t == 0) for w in ((1, 1), (1, 0), (0, 1)))
+    assert products == {(c[0], c[1] == "fp32") for c in gpu.PRODUCTS}
+    assert gradients == {(c[0], c[1] == "fp32") for c in gpu.GRADIENTS}
+    for kernel, t, rows, experts, N, K in gpu.PRODUCTS:
+        assert fm.fmm_f8_matmul_kernel(fm.fmm_f8_desc(rows, max(1, experts), N, K, gpu.TYPE[t])) == kernel
+    for kernel, t, rows, experts, N, K, want in gpu.GRADIENTS:
+        assert fm.fmm_f8_linear_backward_kernel(fm.fmm_f8_desc(rows, max(1, experts), N, K, gpu.TYPE[t]), *want) == kernel
+    for bad in ((-1, 1, 4, 4, 0), (4, 0, 4, 4, 0), (4, 1, 4, 1 << 23, 0), (4, 1, 4, 4, 3)):
+        assert fm.fmm_f8_matmul_kernel(fm.fmm_f8_desc(*bad)) is None
+        assert fm.fmm_f8_linear_backward_kernel(fm.fmm_f8_desc(*bad)) is None
+    assert fm.fmm_f8_matmul_kernel(None) is None and fm.fmm_f8_linear_backward_kernel(None) is None
+
+
 # ---- the torch wrappers -----------------------------------------------------------------
 def _operands(device="cpu"):
     import torch

@@ -149,3 +149,22 @@ def test_the_binding_forwards(torch, grads):
     n = fm.fmm_clip_scratch_size()
     fm.fmm_clip([fm.FMM_F32] * 2, [1000, 5], ts, out2, 0.5, norm, torch.empty(n, dtype=torch.uint8, device="cuda"), n)
     assert torch.equal(norm, want) and all(torch.equal(a, b) for a, b in zip(out, out2))
+
+
+def test_a_layers_step_clips(torch, grads):
+    """The feed-forward example's step: the weights move by the rate times the clipped gradients."""
+    from examples.q8_feedforward import FeedForward
+    g = torch.Generator(device="cuda").manual_seed(0)
+    layer = FeedForward(64, 128)
+    x = torch.randn(32, 64, generator=g, device="cuda").bfloat16()
+    out, h, kept = layer.forward(x, torch.zeros_like(x), train=True)
+    _, *got = layer.backward(out, h, kept)
+    before = [p.clone() for p in (layer.w1, layer.b1, layer.w2, layer.b2, layer.gain)]
+    norm = np.sqrt(sum(float(t.double().square().sum()) for t in got))
+    want = [t.double() * min(1.0, 0.25 / (norm + 1e-6)) for t in got]
+    assert norm > 0.25
+    layer.step(got, 0.5, max_norm=0.25)
+    for p, b, w, t in zip((layer.w1, layer.b1, layer.w2, layer.b2, layer.gain), before, want, got):
+        # the clipped gradient's own rounding, its product with the rate (exact) and the sum's
+        half = HALF_ULP[str(t.dtype).split(".")[1]] + 2.5 * 2.0 ** -24
+        assert bool(((p.double() - (b.double() - 0.5 * w)).abs() <= 0.5 * half * w.abs() + 2.0 ** -24 * (b.double().abs() + w.abs()) + 1e-40).all())

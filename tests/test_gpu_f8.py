@@ -165,7 +165,7 @@ def weight(torch, f8, seed, experts, N, K, spread=3):
     q, _ = operand(torch, f8, seed, experts * N, K, spread)
     g = torch.Generator().manual_seed(seed + 1)
     s = torch.randint(127 - spread, 128 + spread, (experts, -(-N // 128), ref.scale_pitch(K)), generator=g, dtype=torch.int32)
-    return q.view(experts, N, -1), s.to(torch.uint8).cuda().view(f8.SCALES)
+    return q.view(experts, N, ref.pitch(K)), s.to(torch.uint8).cuda().view(f8.SCALES)
 
 
 def product_bound(t, S, C, n):
@@ -337,6 +337,24 @@ def test_backward_of_some(torch, f8, t, want):
 def test_grouped_backward(torch, f8, t, rows, experts, N, K, layout):
     off, span = offsets_of(torch, layout, rows, experts)
     check_backward(torch, f8, t, rows, experts, N, K, off, span)
+
+
+def test_backward_of_nothing(torch, f8):
+    """No rows, no output channels, no input channels, no experts' rows at all."""
+    def operands(rows, E, N, K):
+        return (*operand(torch, f8, 1, rows, K), *weight(torch, f8, 2, E, N, K), torch.zeros(rows, N, device="cuda"))
+
+    a, sa, w, sw, dy = operands(0, 2, 5, 7)
+    off = torch.zeros(3, dtype=torch.int32, device="cuda")
+    dx, dw, db = f8.GroupedLinearF8(0, 2, 5, 7, torch.float32).backward(dy, a, sa, w, sw, off, bias=True)
+    assert dx.shape == (0, 7) and bool((dw == 0).all()) and bool((db == 0).all())
+    a, sa, w, sw, dy = operands(4, 1, 0, 7)
+    dx, dw, db = f8.LinearF8(4, 0, 7, torch.float32).backward(dy, a, sa, w[0], sw[0], bias=True)
+    assert bool((dx == 0).all()) and dx.shape == (4, 7) and dw.shape == (0, 7) and db.shape == (0,)
+    a, sa, w, sw, _ = operands(4, 1, 5, 0)
+    dy = torch.ones(4, 5, device="cuda")
+    dx, dw, db = f8.LinearF8(4, 5, 0, torch.float32).backward(dy, a, sa, w[0], sw[0], bias=True)
+    assert dx.shape == (4, 0) and dw.shape == (5, 0) and bool((db == 4).all())
 
 
 @pytest.mark.parametrize("t", TYPES)

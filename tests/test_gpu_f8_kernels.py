@@ -12,12 +12,38 @@ HALF_ULP = {"fp32": 2.0 ** -24, "bf16": 2.0 ** -8, "fp16": 2.0 ** -11}
 TYPE = {"fp32": 0, "bf16": 1, "fp16": 2}
 
 # kernel, type, rows, experts (0: a single weight), N, K
-PRODUCTS = []
+PRODUCTS = [
+    ("few_tokens_kernel 16x16", "fp32", 8, 0, 8, 143), ("few_tokens_kernel 16x16", "fp32", 8, 3, 9, 1445),
+    ("few_tokens_kernel 16x16", "fp16", 8, 0, 8, 1570), ("few_tokens_kernel 16x16", "bf16", 8, 8, 9, 141),
+    ("few_tokens_kernel 32x32", "fp32", 8, 8, 637, 157), ("few_tokens_kernel 32x32", "fp32", 17, 0, 3297, 1433),
+    ("few_tokens_kernel 32x32", "fp32", 3182, 3, 18, 1429), ("few_tokens_kernel 32x32", "fp16", 8, 0, 4274, 128),
+    ("few_tokens_kernel 32x32", "fp16", 2404, 0, 18, 1417), ("few_tokens_kernel 32x32", "bf16", 15, 8, 1554, 1425),
+    ("matmul_kernel 64x64", "fp32", 8, 8, 934, 121), ("matmul_kernel 64x64", "fp32", 6987, 0, 65, 1593),
+    ("matmul_kernel 64x64", "fp32", 102, 3, 3193, 2061), ("matmul_kernel 64x64", "fp16", 3590, 0, 37, 123),
+    ("matmul_kernel 64x64", "fp16", 6789, 0, 37, 1598), ("matmul_kernel 64x64", "bf16", 10, 8, 1862, 1509),
+    ("matmul_kernel 128x128 ahead", "fp32", 534, 8, 2313, 147), ("matmul_kernel 128x128 ahead", "fp32", 4694, 0, 388, 1407),
+    ("matmul_kernel 128x128 ahead", "fp32", 243, 3, 5297, 1463), ("matmul_kernel 128x128 ahead", "fp16", 6900, 0, 268, 154),
+    ("matmul_kernel 128x128 ahead", "fp16", 4694, 0, 388, 1407), ("matmul_kernel 128x128 ahead", "bf16", 10, 8, 4079, 2113),
+    ("matmul_kernel 128x128", "fp32", 6088, 0, 392, 130), ("matmul_kernel 128x128", "fp32", 142, 8, 4940, 1507),
+    ("matmul_kernel 128x128", "fp16", 729, 0, 5514, 1412), ("matmul_kernel 128x128", "bf16", 8, 8, 4348, 125),
+    ("matmul_kernel 128x128", "bf16", 9, 8, 4459, 1774), ("matmul_kernel 256x256", "fp16", 5274, 0, 6195, 273),
+    ("matmul_kernel 256x256", "bf16", 5497, 8, 4339, 390), ("matmul_kernel 256x256", "fp16", 2795, 0, 3553, 1410),
+    ("matmul_kernel 256x256", "bf16", 1042, 8, 6929, 1417),
+]
 # kernel, type, rows, experts, N, K, wanted (dX, dW)
 GRADIENTS = [
-    ("grad_kernel 256x256 256x256", "bf16", 2500, 0, 2500, 2500, (1, 1)),
-    ("grad_kernel 256x256 256x256", "fp16", 3000, 3, 1500, 2100, (1, 1)),
-    ("grad_kernel 256x256 256x256", "bf16", 1249, 0, 1238, 5005, (1, 1)),
+    ("grad_kernel 64x64 64x64", "fp32", 36, 3, 8, 11, (1, 0)), ("grad_kernel 64x64 64x64", "fp32", 12, 0, 1429, 11, (0, 1)),
+    ("grad_kernel 64x64 64x64", "bf16", 12, 0, 8, 11, (1, 0)), ("grad_kernel 64x64 64x64", "fp16", 12, 3, 1421, 11, (1, 1)),
+    ("grad_kernel 64x64 128x128", "fp32", 66, 8, 201, 1473, (1, 1)), ("grad_kernel 64x64 128x128", "fp32", 12, 0, 3813, 1136, (0, 1)),
+    ("grad_kernel 64x64 128x128", "bf16", 12, 0, 1896, 1247, (1, 1)), ("grad_kernel 64x64 128x128", "fp16", 15, 8, 1636, 134, (1, 1)),
+    ("grad_kernel 128x128 64x64", "fp32", 4295, 0, 1528, 266, (1, 1)), ("grad_kernel 128x128 64x64", "fp32", 1483, 3, 1582, 1167, (1, 1)),
+    ("grad_kernel 128x128 64x64", "fp16", 6694, 0, 1515, 72, (1, 1)), ("grad_kernel 128x128 64x64", "bf16", 12, 8, 1553, 4254, (1, 0)),
+    ("grad_kernel 128x128 128x128", "fp32", 632, 8, 9, 2911, (1, 1)), ("grad_kernel 128x128 128x128", "fp32", 391, 0, 1512, 4060, (1, 1)),
+    ("grad_kernel 128x128 128x128", "fp16", 130, 0, 1412, 6641, (1, 1)), ("grad_kernel 128x128 128x128", "bf16", 16, 8, 1544, 1764, (1, 1)),
+    ("grad_kernel 128x128 128x128 ahead", "fp32", 579, 3, 87, 3297, (1, 1)), ("grad_kernel 128x128 128x128 ahead", "fp32", 1319, 8, 2474, 81, (0, 1)),
+    ("grad_kernel 128x128 128x128 ahead", "fp16", 5959, 0, 8, 360, (1, 0)), ("grad_kernel 128x128 128x128 ahead", "bf16", 13, 3, 6052, 67, (0, 1)),
+    ("grad_kernel 256x256 256x256", "fp16", 7117, 8, 386, 4118, (1, 1)), ("grad_kernel 256x256 256x256", "bf16", 1172, 0, 1926, 4080, (1, 1)),
+    ("grad_kernel 256x256 256x256", "fp16", 1052, 8, 1787, 2507, (1, 1)), ("grad_kernel 256x256 256x256", "bf16", 2500, 0, 2500, 2500, (1, 1)),
 ]
 
 
