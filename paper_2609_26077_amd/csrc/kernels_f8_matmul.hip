@@ -24,7 +24,8 @@ __global__ __launch_bounds__(T::kThreads, 2) void matmul_kernel(Product g) {
 // a time, and waits for nobody until the waves' sums meet in LDS at the end, where they
 // are added in the waves' order.  Rows in LDS are swizzled as in the tile kernel.
 // The scales of 128 steps go through LDS too, wave 0 bringing them before its
-// first pieces.
+// first pieces.  One token of 8192 x 8192: 13.2 us, 67 MB at 5.1 TB/s; 64 tokens over 32 experts of 2048 x 4096: 41 us,
+// the weights of the experts with rows at 6 TB/s.
 template <class E, int MT, int NT, int W, int D, int OUT>
 __global__ __launch_bounds__(64 * W) void few_tokens_kernel(Product g) {
   constexpr int kPiece = 16 * (MT + NT) * kStep;

