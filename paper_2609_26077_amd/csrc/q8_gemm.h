@@ -137,8 +137,8 @@ __device__ __forceinline__ void load4(const float *p, int n, float (&v)[4]) {
 // end took 23 us, as much as 14 steps); so the tiles pass through the wave's own
 // part of LDS, free once every wave has read the last step, and leave in rows of
 // 16 bytes a lane (10 us).  16-byte chunk c of a row sits at chunk c ^ (row mod the row's
-// chunks).  FULL: the whole wave tile lies inside C.
-template <class E, class T, int OUT, bool FULL>
+// chunks).  FULL: the whole wave tile lies inside C.  STREAM: past the caches.
+template <class E, class T, int OUT, bool FULL, bool STREAM = false>
 __device__ __forceinline__ void store_tile(const GemmProblem &g, void *C, typename E::acc (&acc)[T::MI][T::NI], int m0,
                                            int n0, uint8_t *lds) {
   constexpr int B = OUT == FMM_F32 ? 4 : 2, EPC = 16 / B;          // bytes of an element, elements of a chunk
@@ -188,15 +188,19 @@ __device__ __forceinline__ void store_tile(const GemmProblem &g, void *C, typena
     const int lrow = lane / CH, c = lane % CH;
     const int n = n0 + c * EPC;
     elem_t<OUT> *out = static_cast<elem_t<OUT> *>(C) + (int64_t)(m0 + 32 * pass * MP + lrow) * g.N + n;
+    const auto put = [&](u32x4 v) {
+      if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_a2 *>(out));
+      else *reinterpret_cast<u32x4_a2 *>(out) = v;
+    };
 #pragma unroll
     for (int e = 0; e < MP * 32 * CH / 64; ++e) {
       const int row = (64 / CH) * e + lrow;
       const u32x4 v = *reinterpret_cast<const u32x4 *>(lds + row * kRow + 16 * (c ^ (row & (CH - 1))));
       if (FULL) {
-        *reinterpret_cast<u32x4_a2 *>(out) = v;
+        put(v);
       } else if (m0 + 32 * pass * MP + row < g.M && n < g.N) {
         if (n + EPC <= g.N) {
-          *reinterpret_cast<u32x4_a2 *>(out) = v;
+          put(v);
         } else {
 #pragma unroll
           for (int k = 0; k < EPC; ++k)
