@@ -46,7 +46,7 @@ template <int R>
 struct Turn {
   static constexpr int kThreads = 2048 / R, kWaves = kThreads / 64;
   uint32_t out[128][32];
-  uint32_t most[kWaves][128];
+  uint32_t most[128];
   float sum[kWaves][128];
 };
 __device__ __forceinline__ int piece(int p, int n) { return p ^ (2 * (n >> 3) & 31); }
@@ -65,11 +65,11 @@ __device__ __forceinline__ void store_columns(const Turn<R> &tile, uint8_t *dst,
   }
 }
 
-// codes by columns of v, and their scales to scales[n * pitch]
+// codes by columns of v, and their scales to scales[n * pitch]; tile.most is zero
 template <int R>
 __device__ __forceinline__ void columns(Turn<R> &tile, const float (&v)[R][8], uint8_t *dst, int64_t pitch, uint8_t *scales,
                                         int64_t scale_pitch, int cols) {
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, rg = t >> 4, cg = t & 15;
+  const int t = threadIdx.x, lane = t & 63, rg = t >> 4, cg = t & 15;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     uint32_t a = 0;
@@ -77,18 +77,14 @@ __device__ __forceinline__ void columns(Turn<R> &tile, const float (&v)[R][8], u
     for (int r = 0; r < R; ++r) a = max(a, magnitude(v[r][i]));
     a = max(a, (uint32_t)__shfl_xor((int)a, 16));
     a = max(a, (uint32_t)__shfl_xor((int)a, 32));
-    if (lane < 16) tile.most[wave][8 * cg + i] = a;
+    if (lane < 16) atomicMax(&tile.most[8 * cg + i], a);
   }
   __syncthreads();
+  if (t < 128 && t < cols) scales[t * scale_pitch] = (uint8_t)scale_byte(tile.most[t]);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int n = 8 * cg + i;
-    uint32_t a = 0;
-#pragma unroll
-    for (int k = 0; k < Turn<R>::kWaves; ++k) a = max(a, tile.most[k][n]);
-    const uint32_t b = scale_byte(a);
-    if (rg == 0 && n < cols) scales[n * scale_pitch] = (uint8_t)b;
-    const float s = scale_value(b);
+    const float s = scale_value(scale_byte(tile.most[n]));
 #pragma unroll
     for (int r = 0; r < R; r += 4)
       tile.out[n][piece((R * rg + r) / 4, n)] = codes4(v[r][i], v[r + 1][i], v[r + 2][i], v[r + 3][i], s);
@@ -123,6 +119,8 @@ __global__ __launch_bounds__(Turn<R>::kThreads) void layout_kernel(LayoutArgs g)
   const int mine = (s.hi - s.lo + kBlock - 1) / kBlock, at = block - s.tiles;
   const int64_t Bp = (int64_t)mine * kBlock, sbp = (mine + kScalePad - 1) / kScalePad * kScalePad;
   float v[R][8];
+  if (t < 128) tile.most[t] = 0;
+  __syncthreads();
   if (is_dy) {
     const elem_t<T> *src = static_cast<const elem_t<T> *>(g.dy) + (int64_t)(row0 + R * rg) * g.N + c0 + 8 * cg;
     q8::Raw8<T> raw[R];

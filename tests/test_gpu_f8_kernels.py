@@ -15,6 +15,9 @@ TYPE = {"fp32": 0, "bf16": 1, "fp16": 2}
 PRODUCTS = [
     ("few_tokens_kernel 16x16", "fp32", 8, 0, 8, 143), ("few_tokens_kernel 16x16", "fp32", 8, 3, 9, 1445),
     ("few_tokens_kernel 16x16", "fp16", 8, 0, 8, 1570), ("few_tokens_kernel 16x16", "bf16", 8, 8, 9, 141),
+    # (more than the 128 steps whose scales a workgroup holds at a time)
+    ("few_tokens_kernel 16x16", "fp32", 20, 8, 1500, 16900), ("few_tokens_kernel 32x32", "bf16", 60, 0, 3000, 17000),
+    ("few_tokens_kernel 32x32", "fp32", 60, 0, 3000, 33000),
     ("few_tokens_kernel 32x32", "fp32", 8, 8, 637, 157), ("few_tokens_kernel 32x32", "fp32", 17, 0, 3297, 1433),
     ("few_tokens_kernel 32x32", "fp32", 3182, 3, 18, 1429), ("few_tokens_kernel 32x32", "fp16", 8, 0, 4274, 128),
     ("few_tokens_kernel 32x32", "fp16", 2404, 0, 18, 1417), ("few_tokens_kernel 32x32", "bf16", 15, 8, 1554, 1425),
@@ -150,3 +153,54 @@ def test_gradients(torch, f8, kernel, t, rows, experts, N, K, want):
             assert bool((dw[e] == 0).all())
         s = y.double()
         within(torch, db[e], s.sum(0), 2 * (hi - lo + 1) * U * s.abs().sum(0) + 1e-30, f"dbias of expert {e}")
+
+
+# ---- offsets past 32 bits -----------------------------------------------------------
+def random_codes(torch, f8, rows, cols):
+    """Codes of 0.5 to 1.875 in magnitude, scales of 1."""
+    q = torch.randint(0x30, 0x40, (rows, f8.pitch(cols)), dtype=torch.uint8, device="cuda")
+    q |= torch.randint(0, 2, q.shape, dtype=torch.uint8, device="cuda") << 7
+    return q.view(f8.CODES), torch.full((rows, f8.scale_pitch(cols)), 127, dtype=torch.uint8, device="cuda").view(f8.SCALES)
+
+
+def test_activations_past_4_gb(torch, f8):
+    """4.4 GB of codes: the last rows, and the first ones, of the codes, the product and the values."""
+    rows, N, K = 270000, 16, 16384
+    a, sa = random_codes(torch, f8, rows, K)
+    w, sw = f8.quantize_weight(torch.randn(N, K, device="cuda") * 0.05)
+    C = f8.LinearF8(rows, N, K).matmul(a, sa, w, sw)
+    vw = f8.dequantize(w, sw, K).double()
+    x = torch.empty(rows, K, dtype=torch.bfloat16, device="cuda")
+    f8.dequantize(a, sa, K, torch.bfloat16, out=x)
+    again, scales = f8.quantize(x)
+    for part in (slice(0, 40), slice(rows - 40, rows)):
+        va = f8.dequantize(a[part].contiguous(), sa[part].contiguous(), K)
+        assert torch.equal(x[part].float(), va)
+        assert torch.equal(f8.dequantize(again[part].contiguous(), scales[part].contiguous(), K), va)
+        want, S = product(va.double(), vw), product(va.double().abs(), vw.abs())
+        within(torch, C[part], want, bound("bf16", S, want, K), "C")
+
+
+def test_experts_past_4_gb(torch, f8):
+    """4.4 GB of weights, 8.9 GB of their gradients: the last expert's product and gradients."""
+    rows, E, N, K = 300, 33, 8192, 16384
+    q, _ = random_codes(torch, f8, E * N, K)
+    w = q.view(E, N, K)
+    sw = torch.full((E, N // 128, f8.scale_pitch(K)), 118, dtype=torch.uint8, device="cuda").view(f8.SCALES)
+    a, sa = random_codes(torch, f8, rows, K)
+    off = torch.tensor([0] + [e * 5 for e in range(1, E)] + [rows], dtype=torch.int32).cuda()
+    dy = torch.randn(rows, N, device="cuda").bfloat16()
+    lin = f8.GroupedLinearF8(rows, E, N, K)
+    C = lin.matmul(a, sa, w, sw, off)
+    dx, dw, _ = lin.backward(dy, a, sa, w, sw, off)
+    lo = 5 * (E - 1)
+    va, vw = f8.dequantize(a, sa, K).double()[lo:], f8.dequantize(w[E - 1], sw[E - 1], K).double()
+    want, S = product(va, vw), product(va.abs(), vw.abs())
+    within(torch, C[lo:], want, bound("bf16", S, want, K), "C")
+    y = f8.dequantize(*f8.quantize(dy[lo:].contiguous()), N).double()
+    want, S = y @ vw, y.abs() @ vw.abs()
+    within(torch, dx[lo:], want, bound("bf16", S, want, N), "dX")
+    # (the scales of va are all 1 and its largest codes alike: its codes by columns are as they are)
+    yc = f8.dequantize(*f8.quantize(dy[lo:].t().contiguous()), rows - lo).double()
+    want, S = yc @ va, yc.abs() @ va.abs()
+    within(torch, dw[E - 1], want, bound("bf16", S, want, rows - lo), "dW")
