@@ -454,15 +454,19 @@ __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4
   __syncthreads();
   // Tiles that begin together end together, and their stores wait for HBM.  Past the caches they do so less
   // (8192 x 8192 with 1024 positions 86 -> 76 us, with 4096 228 -> 208; a start in turns gains nothing); such outputs, 33 MB or more,
-  // do not stay in a cache for whoever reads them anyway.
-  constexpr bool kStream = T::TM == 256;
+  // do not stay in a cache for whoever reads them anyway.  Not where rows begin off 16 bytes: lines written
+  // in pieces have to meet in the caches (10464 x 5899 with 357 positions 52 us, 75 past them).
+  const bool stream = T::TM == 256 && g.N * (OUT == FMM_F32 ? 4 : 2) % 16 == 0 && reinterpret_cast<uintptr_t>(w.C) % 16 == 0;
   q8::GemmProblem out = {};
   out.M = w.M;
   out.N = g.N;
   const int mw = w.m0 + wm * MI * 32, nw = w.n0 + wn * NI * 32;
   uint8_t *share = reinterpret_cast<uint8_t *>(lds_raw) + wave * (T::kLds / T::kWaves);
-  if (mw + MI * 32 <= out.M && nw + NI * 32 <= out.N) q8::store_tile<E, T, OUT, true, kStream>(out, w.C, acc, mw, nw, share);
-  else q8::store_tile<E, T, OUT, false, kStream>(out, w.C, acc, mw, nw, share);
+  if (mw + MI * 32 > out.M || nw + NI * 32 > out.N) return q8::store_tile<E, T, OUT, false>(out, w.C, acc, mw, nw, share);
+  if constexpr (T::TM == 256) {
+    if (stream) return q8::store_tile<E, T, OUT, true, true>(out, w.C, acc, mw, nw, share);
+  }
+  q8::store_tile<E, T, OUT, true>(out, w.C, acc, mw, nw, share);
 }
 
 }  // namespace f8

@@ -78,10 +78,11 @@ __device__ __forceinline__ double squares(const void *in, int64_t n) {
   return s;
 }
 
-// eight consecutive elements, of which those before n exist
+// eight consecutive elements, of which those before n exist; past the caches, but for tensors that begin
+// off 16 bytes, whose lines are written in pieces that have to meet there
 template <int T>
-__device__ __forceinline__ void store(elem_t<T> *p, int64_t n, const float (&v)[8]) {
-  if (n < 8) {
+__device__ __forceinline__ void store(elem_t<T> *p, int64_t n, const float (&v)[8], bool stream) {
+  if (n < 8 || !stream) {
     q8::store8<T>(p, n, v);
   } else if constexpr (T == FMM_F32) {
 #pragma unroll
@@ -99,13 +100,14 @@ template <int T>
 __device__ __forceinline__ void scale(const void *in, void *out, int64_t n, float c) {
   const Part<T> x(in, n);
   elem_t<T> *q = static_cast<elem_t<T> *>(out) + 8 * threadIdx.x;
+  const bool stream = reinterpret_cast<uintptr_t>(out) % 16 == 0;
 #pragma unroll
   for (int u = 0; u < kLoads; ++u) {
     float v[8];
     q8::floats8<T>(x.raw[u], v);
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] *= c;
-    store<T>(q + 2048 * u, n - 8 * (int)threadIdx.x - 2048 * u, v);
+    store<T>(q + 2048 * u, n - 8 * (int)threadIdx.x - 2048 * u, v, stream);
   }
 }
 

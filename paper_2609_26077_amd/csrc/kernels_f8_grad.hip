@@ -259,9 +259,9 @@ struct Cut {
 };
 
 // t = max(start + chain steps, of either; start + work of both / CUs) + tile tiles / CUs us, as for the forward
-// products.  Against all cuts on 1200 shapes (rows 16 to 8192, N to 4096, K to 2048, single weights and up to 64
-// experts): 0.5% over the fastest on average in 16 bits and 0.3% in fp32, more than 10% on 1% and 0.3% of
-// them, 22% and 13% at worst.  Each is the fastest somewhere, us (64: of both, 64/128: dX's and dW's, ...):
+// products.  Against all cuts on 2100 shapes (rows 16 to 16384, N to 8192, K to 4096, single weights and up to 64
+// experts): 0.6% over the fastest on average in 16 bits and 0.4% in fp32, more than 10% on 1% and 0.5% of
+// them, 18% and 15% at worst.  Each is the fastest somewhere, us (64: of both, 64/128: dX's and dW's, ...):
 //   rows x N x K of experts          64     64/128  128/64  128    128 ahead  256
 //   16384 x 4096 x 2048 of 16 bf16   971    683     854     579    747        530    (with the weights turned first)
 //   4096 x 4096 x 2048 fp32          216    182     186     153    179        -
@@ -274,8 +274,8 @@ Cut cut_of(int type, int64_t rows, int64_t experts, int64_t N, int64_t K, bool d
   struct Cost {
     double start, chain, work, tile;
   };
-  constexpr Cost kCost[2][4] = {{{3.2, 0.064, 0.34, 0.0}, {3.6, 0.49, 0.48, 0.0}, {7.2, 0.87, 1.47, 0.0}, {3.1, 0.45, 0.39, 0.67}},
-                                {{3.0, 0.32, 0.47, 0.0}, {3.8, 1.16, 0.74, 0.0}, {0.0, 0.0, 0.0, 0.0}, {3.7, 0.62, 1.25, 0.0}}};
+  constexpr Cost kCost[2][4] = {{{3.29, 0.03, 0.329, 0.0}, {3.56, 0.616, 0.56, 0.0}, {8.54, 1.05, 1.76, 0.0}, {3.55, 0.448, 0.698, 0.51}},
+                                {{3.11, 0.243, 0.395, 0.2}, {3.71, 0.957, 0.731, 0.0}, {0.0, 0.0, 0.0, 0.0}, {4.11, 0.688, 0.899, 0.92}}};
   const Cost(&cost)[4] = kCost[type == FMM_F32];
   // experts with rows, at most, and each one's rows if they were even
   const double full = std::max<double>(1, std::min(experts, rows)), each = rows / full;

@@ -157,11 +157,12 @@ __global__ __launch_bounds__(64 * W) void few_tokens_kernel(Product g) {
   }
 }
 
-// The shapes of workgroup: t = start + max(chain pieces, work pieces groups / CUs) us, pieces being the 128-byte
-// steps that a wave walks.  `chain` is a piece's time where the chip is not full, `work` where it is.  On 1120 shapes
-// (1 to 16384 tokens, N and K to 8192, single weights and up to 64 experts with uneven rows, which the
-// rule takes to be even) the one that it picks is 1.0% slower than the fastest on average in 16 bits and
-// 0.6% in fp32, more than 10% on 4% and 2% of them, 45% and 26% at worst.  Each is the fastest somewhere, us:
+// The shapes of workgroup: t = start + max(chain pieces, work pieces groups / CUs) + group groups / CUs us, pieces
+// being the 128-byte steps that a wave walks.  `chain` is a piece's time where the chip is not full, `work` where
+// it is, `group` what each group costs besides.  On 1800 shapes (1 to 16384 tokens, N and K to 8192, single weights and up
+// to 64 experts with uneven rows, which the rule takes to be even) the one that it picks is 1.1% slower
+// than the fastest on average in 16 bits and 0.6% in fp32, more than 10% on 4% and 2% of them, 33% and
+// 21% at worst.  Each is the fastest somewhere, us:
 //   tokens x N x K                   16x16   32x32   64x64   128 ahead  128     256
 //   1 x 8192 x 8192 bf16             13.9    19.5    19.7    24.7       36.3    48.4
 //   64 x 8192 x 8192 bf16            43.6    21.7    23.9    28.5       37.9    52.0
@@ -174,13 +175,17 @@ __global__ __launch_bounds__(64 * W) void few_tokens_kernel(Product g) {
 struct Shape {
   int tm, tn, waves;            // tile, and the waves that share its contracted axis
   bool one;                     // only where each CU has one group at most
-  float start, chain, work;     // of 16-bit outputs, and of fp32
-  float start32, chain32, work32;
+  struct Cost {
+    float start, chain, work, group;
+  } cost[2];                    // of 16-bit outputs, of fp32
 };
 constexpr Shape kShapes[] = {
-    {16, 16, 8, false, 3.12f, 0.20f, 0.58f, 3.56f, 0.41f, 0.57f},  {32, 32, 4, false, 3.34f, 0.35f, 0.72f, 3.63f, 0.50f, 0.84f},
-    {64, 64, 1, false, 3.67f, 0.30f, 0.30f, 3.73f, 0.56f, 0.43f},  {128, 128, 1, true, 3.78f, 0.55f, 0.49f, 3.77f, 0.82f, 1.22f},
-    {128, 128, 1, false, 3.62f, 0.65f, 0.60f, 3.68f, 0.92f, 0.82f}, {256, 256, 1, false, 7.3f, 1.1f, 1.75f, 0.0f, 0.0f, 0.0f},
+    {16, 16, 8, false, {{3.29f, 0.20f, 0.535f, 0.0f}, {3.55f, 0.41f, 0.57f, 0.0f}}},
+    {32, 32, 4, false, {{3.46f, 0.348f, 0.735f, 0.0f}, {3.63f, 0.50f, 0.831f, 0.0f}}},
+    {64, 64, 1, false, {{3.67f, 0.38f, 0.30f, 0.0f}, {3.73f, 0.557f, 0.43f, 0.0f}}},
+    {128, 128, 1, true, {{3.82f, 0.564f, 0.49f, 0.06f}, {3.77f, 0.82f, 1.33f, 0.0f}}},
+    {128, 128, 1, false, {{3.60f, 0.698f, 0.583f, 0.0f}, {3.73f, 1.20f, 0.83f, 0.0f}}},
+    {256, 256, 1, false, {{7.86f, 1.05f, 1.94f, 0.88f}, {0.0f, 0.0f, 0.0f, 0.0f}}},
 };
 constexpr int kShapeCount = sizeof(kShapes) / sizeof(kShapes[0]);
 // (a launch takes fewer than 2^32 threads, and tiles of uneven experts may be twice as many as of even ones)
@@ -197,8 +202,8 @@ int pick(int type, const Product &g, int ncu) {
     const double groups = experts * std::ceil(rows / p.tm) * ((g.N + p.tn - 1) / p.tn);
     if (groups > kMaxGroups || (p.one && groups > ncu)) continue;
     const double pieces = (g.steps + p.waves - 1) / p.waves;
-    const double t = type == FMM_F32 ? p.start32 + std::max(p.chain32 * pieces, p.work32 * pieces * groups / ncu)
-                                     : p.start + std::max(p.chain * pieces, p.work * pieces * groups / ncu);
+    const Shape::Cost &c = p.cost[type == FMM_F32];
+    const double t = c.start + std::max(c.chain * pieces, c.work * pieces * groups / ncu) + c.group * groups / ncu;
     if (t < least) {
       best = i;
       least = t;

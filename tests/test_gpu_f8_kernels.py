@@ -13,40 +13,103 @@ TYPE = {"fp32": 0, "bf16": 1, "fp16": 2}
 
 # kernel, type, rows, experts (0: a single weight), N, K
 PRODUCTS = [
-    ("few_tokens_kernel 16x16", "fp32", 8, 0, 8, 143), ("few_tokens_kernel 16x16", "fp32", 8, 3, 9, 1445),
-    ("few_tokens_kernel 16x16", "fp16", 8, 0, 8, 1570), ("few_tokens_kernel 16x16", "bf16", 8, 8, 9, 141),
     # (more than the 128 steps whose scales a workgroup holds at a time)
-    ("few_tokens_kernel 16x16", "fp32", 20, 8, 1500, 16900), ("few_tokens_kernel 32x32", "bf16", 60, 0, 3000, 17000),
+    ("few_tokens_kernel 16x16", "fp32", 20, 8, 1500, 16900),
+    ("few_tokens_kernel 32x32", "bf16", 60, 0, 3000, 17000),
     ("few_tokens_kernel 32x32", "fp32", 60, 0, 3000, 33000),
-    ("few_tokens_kernel 32x32", "fp32", 8, 8, 637, 157), ("few_tokens_kernel 32x32", "fp32", 17, 0, 3297, 1433),
-    ("few_tokens_kernel 32x32", "fp32", 3182, 3, 18, 1429), ("few_tokens_kernel 32x32", "fp16", 8, 0, 4274, 128),
-    ("few_tokens_kernel 32x32", "fp16", 2404, 0, 18, 1417), ("few_tokens_kernel 32x32", "bf16", 15, 8, 1554, 1425),
-    ("matmul_kernel 64x64", "fp32", 8, 8, 934, 121), ("matmul_kernel 64x64", "fp32", 6987, 0, 65, 1593),
-    ("matmul_kernel 64x64", "fp32", 102, 3, 3193, 2061), ("matmul_kernel 64x64", "fp16", 3590, 0, 37, 123),
-    ("matmul_kernel 64x64", "fp16", 6789, 0, 37, 1598), ("matmul_kernel 64x64", "bf16", 10, 8, 1862, 1509),
-    ("matmul_kernel 128x128 ahead", "fp32", 534, 8, 2313, 147), ("matmul_kernel 128x128 ahead", "fp32", 4694, 0, 388, 1407),
-    ("matmul_kernel 128x128 ahead", "fp32", 243, 3, 5297, 1463), ("matmul_kernel 128x128 ahead", "fp16", 6900, 0, 268, 154),
-    ("matmul_kernel 128x128 ahead", "fp16", 4694, 0, 388, 1407), ("matmul_kernel 128x128 ahead", "bf16", 10, 8, 4079, 2113),
-    ("matmul_kernel 128x128", "fp32", 6088, 0, 392, 130), ("matmul_kernel 128x128", "fp32", 142, 8, 4940, 1507),
-    ("matmul_kernel 128x128", "fp16", 729, 0, 5514, 1412), ("matmul_kernel 128x128", "bf16", 8, 8, 4348, 125),
-    ("matmul_kernel 128x128", "bf16", 9, 8, 4459, 1774), ("matmul_kernel 256x256", "fp16", 5274, 0, 6195, 273),
-    ("matmul_kernel 256x256", "bf16", 5497, 8, 4339, 390), ("matmul_kernel 256x256", "fp16", 2795, 0, 3553, 1410),
-    ("matmul_kernel 256x256", "bf16", 1042, 8, 6929, 1417),
+    ("few_tokens_kernel 16x16", "fp32", 8, 0, 8, 162),
+    ("few_tokens_kernel 16x16", "fp32", 9, 3, 8, 125),
+    ("few_tokens_kernel 16x16", "fp32", 9, 0, 8, 1535),
+    ("few_tokens_kernel 16x16", "fp32", 9, 8, 8, 1463),
+    ("few_tokens_kernel 16x16", "fp16", 8, 0, 8, 162),
+    ("few_tokens_kernel 16x16", "bf16", 9, 3, 8, 125),
+    ("few_tokens_kernel 16x16", "fp16", 9, 0, 8, 1535),
+    ("few_tokens_kernel 16x16", "bf16", 9, 8, 8, 1463),
+    ("few_tokens_kernel 32x32", "fp32", 4335, 0, 8, 121),
+    ("few_tokens_kernel 32x32", "fp32", 8, 8, 523, 205),
+    ("few_tokens_kernel 32x32", "fp32", 3003, 0, 18, 1421),
+    ("few_tokens_kernel 32x32", "fp32", 3341, 3, 17, 1493),
+    ("few_tokens_kernel 32x32", "fp16", 4335, 0, 8, 121),
+    ("few_tokens_kernel 32x32", "bf16", 10, 8, 546, 128),
+    ("few_tokens_kernel 32x32", "fp16", 19, 0, 2495, 1428),
+    ("few_tokens_kernel 32x32", "bf16", 130, 8, 314, 1459),
+    ("matmul_kernel 128x128", "fp32", 7193, 0, 393, 128),
+    ("matmul_kernel 128x128", "fp32", 8, 8, 5709, 126),
+    ("matmul_kernel 128x128", "fp32", 7359, 0, 385, 1841),
+    ("matmul_kernel 128x128", "fp32", 180, 8, 6007, 1564),
+    ("matmul_kernel 128x128", "fp16", 4928, 0, 438, 121),
+    ("matmul_kernel 128x128", "bf16", 8, 8, 4888, 137),
+    ("matmul_kernel 128x128", "fp16", 6767, 0, 607, 1407),
+    ("matmul_kernel 128x128", "bf16", 9, 8, 4809, 1653),
+    ("matmul_kernel 128x128 ahead", "fp32", 5448, 0, 332, 130),
+    ("matmul_kernel 128x128 ahead", "fp32", 211, 3, 5359, 146),
+    ("matmul_kernel 128x128 ahead", "fp32", 5250, 0, 348, 1421),
+    ("matmul_kernel 128x128 ahead", "fp32", 564, 8, 2080, 1572),
+    ("matmul_kernel 128x128 ahead", "fp16", 4081, 0, 520, 132),
+    ("matmul_kernel 128x128 ahead", "bf16", 194, 3, 6542, 148),
+    ("matmul_kernel 128x128 ahead", "fp16", 5250, 0, 348, 1421),
+    ("matmul_kernel 128x128 ahead", "bf16", 8, 8, 4015, 1624),
+    ("matmul_kernel 256x256", "fp16", 2704, 0, 3484, 2593),
+    ("matmul_kernel 256x256", "bf16", 2704, 0, 3520, 2593),      # (rows that begin on 16 bytes are stored past the caches)
+    ("matmul_kernel 256x256", "fp16", 16000, 3, 8200, 400),
+    ("matmul_kernel 256x256", "bf16", 1103, 8, 5021, 3020),
+    ("matmul_kernel 64x64", "fp32", 9, 0, 7343, 122),
+    ("matmul_kernel 64x64", "fp32", 9, 8, 1022, 124),
+    ("matmul_kernel 64x64", "fp32", 75, 0, 6494, 1700),
+    ("matmul_kernel 64x64", "fp32", 105, 3, 3255, 1686),
+    ("matmul_kernel 64x64", "fp16", 9, 0, 7343, 122),
+    ("matmul_kernel 64x64", "bf16", 9, 8, 1022, 124),
+    ("matmul_kernel 64x64", "fp16", 34, 0, 7811, 1644),
+    ("matmul_kernel 64x64", "bf16", 9, 8, 2440, 1457),
 ]
 # kernel, type, rows, experts, N, K, wanted (dX, dW)
 GRADIENTS = [
-    ("grad_kernel 64x64 64x64", "fp32", 36, 3, 8, 11, (1, 0)), ("grad_kernel 64x64 64x64", "fp32", 12, 0, 1429, 11, (0, 1)),
-    ("grad_kernel 64x64 64x64", "bf16", 12, 0, 8, 11, (1, 0)), ("grad_kernel 64x64 64x64", "fp16", 12, 3, 1421, 11, (1, 1)),
-    ("grad_kernel 64x64 128x128", "fp32", 66, 8, 201, 1473, (1, 1)), ("grad_kernel 64x64 128x128", "fp32", 12, 0, 3813, 1136, (0, 1)),
-    ("grad_kernel 64x64 128x128", "bf16", 12, 0, 1896, 1247, (1, 1)), ("grad_kernel 64x64 128x128", "fp16", 15, 8, 1636, 134, (1, 1)),
-    ("grad_kernel 128x128 64x64", "fp32", 4295, 0, 1528, 266, (1, 1)), ("grad_kernel 128x128 64x64", "fp32", 1483, 3, 1582, 1167, (1, 1)),
-    ("grad_kernel 128x128 64x64", "fp16", 6694, 0, 1515, 72, (1, 1)), ("grad_kernel 128x128 64x64", "bf16", 12, 8, 1553, 4254, (1, 0)),
-    ("grad_kernel 128x128 128x128", "fp32", 632, 8, 9, 2911, (1, 1)), ("grad_kernel 128x128 128x128", "fp32", 391, 0, 1512, 4060, (1, 1)),
-    ("grad_kernel 128x128 128x128", "fp16", 130, 0, 1412, 6641, (1, 1)), ("grad_kernel 128x128 128x128", "bf16", 16, 8, 1544, 1764, (1, 1)),
-    ("grad_kernel 128x128 128x128 ahead", "fp32", 579, 3, 87, 3297, (1, 1)), ("grad_kernel 128x128 128x128 ahead", "fp32", 1319, 8, 2474, 81, (0, 1)),
-    ("grad_kernel 128x128 128x128 ahead", "fp16", 5959, 0, 8, 360, (1, 0)), ("grad_kernel 128x128 128x128 ahead", "bf16", 13, 3, 6052, 67, (0, 1)),
-    ("grad_kernel 256x256 256x256", "fp16", 7117, 8, 386, 4118, (1, 1)), ("grad_kernel 256x256 256x256", "bf16", 1172, 0, 1926, 4080, (1, 1)),
-    ("grad_kernel 256x256 256x256", "fp16", 1052, 8, 1787, 2507, (1, 1)), ("grad_kernel 256x256 256x256", "bf16", 2500, 0, 2500, 2500, (1, 1)),
+    ("grad_kernel 128x128 128x128", "fp32", 129, 0, 130, 6919, (1, 1)),
+    ("grad_kernel 128x128 128x128", "fp32", 14, 8, 8, 3304, (1, 1)),
+    ("grad_kernel 128x128 128x128", "fp32", 160, 0, 1448, 8127, (1, 1)),
+    ("grad_kernel 128x128 128x128", "fp32", 13, 3, 1436, 7307, (1, 1)),
+    ("grad_kernel 128x128 128x128", "fp16", 136, 0, 138, 7239, (1, 1)),
+    ("grad_kernel 128x128 128x128", "bf16", 636, 8, 8, 2257, (1, 1)),
+    ("grad_kernel 128x128 128x128", "fp16", 286, 0, 1424, 4131, (1, 1)),
+    ("grad_kernel 128x128 128x128", "bf16", 16, 3, 1451, 5684, (1, 1)),
+    ("grad_kernel 128x128 128x128 ahead", "fp32", 432, 0, 464, 2827, (1, 1)),
+    ("grad_kernel 128x128 128x128 ahead", "fp32", 1481, 3, 459, 888, (1, 1)),
+    ("grad_kernel 128x128 128x128 ahead", "fp32", 1293, 0, 1475, 734, (1, 1)),
+    ("grad_kernel 128x128 128x128 ahead", "fp32", 5095, 3, 1673, 196, (1, 1)),
+    ("grad_kernel 128x128 128x128 ahead", "fp16", 195, 0, 197, 4980, (1, 1)),
+    ("grad_kernel 128x128 128x128 ahead", "bf16", 1675, 8, 241, 569, (1, 1)),
+    ("grad_kernel 128x128 128x128 ahead", "fp16", 1481, 0, 1555, 451, (1, 1)),
+    ("grad_kernel 128x128 128x128 ahead", "bf16", 388, 3, 6478, 73, (0, 1)),
+    ("grad_kernel 128x128 64x64", "fp32", 816, 0, 9, 16, (1, 1)),
+    ("grad_kernel 128x128 64x64", "fp32", 2525, 3, 9, 12, (1, 1)),
+    ("grad_kernel 128x128 64x64", "fp32", 6731, 0, 1408, 12, (1, 1)),
+    ("grad_kernel 128x128 64x64", "fp32", 7646, 3, 1864, 143, (1, 1)),
+    ("grad_kernel 128x128 64x64", "fp16", 3056, 0, 8, 621, (1, 1)),
+    ("grad_kernel 128x128 64x64", "bf16", 2787, 8, 8, 584, (1, 1)),
+    ("grad_kernel 128x128 64x64", "fp16", 5567, 0, 1475, 131, (1, 1)),
+    ("grad_kernel 128x128 64x64", "bf16", 3691, 8, 1567, 299, (1, 1)),
+    ("grad_kernel 256x256 256x256", "fp16", 7115, 0, 434, 7658, (1, 0)),
+    ("grad_kernel 256x256 256x256", "bf16", 7886, 8, 156, 7398, (1, 1)),
+    ("grad_kernel 256x256 256x256", "bf16", 2500, 0, 2504, 2600, (1, 1)),
+    ("grad_kernel 256x256 256x256", "fp16", 400, 3, 2300, 7400, (1, 1)),
+    ("grad_kernel 256x256 256x256", "fp16", 694, 0, 1942, 7148, (1, 1)),
+    ("grad_kernel 256x256 256x256", "bf16", 388, 3, 2279, 7403, (1, 1)),
+    ("grad_kernel 64x64 128x128", "fp32", 14, 0, 264, 6617, (1, 1)),
+    ("grad_kernel 64x64 128x128", "fp32", 17, 8, 9, 5513, (0, 1)),
+    ("grad_kernel 64x64 128x128", "fp32", 12, 0, 1428, 12, (1, 1)),
+    ("grad_kernel 64x64 128x128", "fp32", 19, 3, 1417, 12, (1, 1)),
+    ("grad_kernel 64x64 128x128", "fp16", 14, 0, 265, 5515, (1, 1)),
+    ("grad_kernel 64x64 128x128", "bf16", 31, 3, 70, 5042, (1, 1)),
+    ("grad_kernel 64x64 128x128", "fp16", 12, 0, 1624, 1171, (1, 1)),
+    ("grad_kernel 64x64 128x128", "bf16", 12, 8, 1997, 74, (1, 1)),
+    ("grad_kernel 64x64 64x64", "fp32", 11, 0, 8, 11, (1, 1)),
+    ("grad_kernel 64x64 64x64", "fp32", 18, 3, 9, 11, (1, 1)),
+    ("grad_kernel 64x64 64x64", "fp32", 16, 0, 1490, 12, (1, 0)),
+    ("grad_kernel 64x64 64x64", "fp32", 13, 3, 1578, 11, (1, 0)),
+    ("grad_kernel 64x64 64x64", "fp16", 11, 0, 8, 11, (1, 1)),
+    ("grad_kernel 64x64 64x64", "bf16", 29, 3, 8, 11, (1, 1)),
+    ("grad_kernel 64x64 64x64", "fp16", 12, 0, 1428, 12, (1, 1)),
+    ("grad_kernel 64x64 64x64", "bf16", 13, 3, 1578, 11, (1, 1)),
 ]
 
 
