@@ -22,9 +22,10 @@
 // following words are loaded at the start of the last step of four and waited for at
 // its barrier, where few of the ring's transfers are on their way.
 //
-// What bounds the 256 tile: over a long axis power (8192^3: 434 us, 2.5 PFLOP/s, the matrix cores busy 66% of the
-// cycles at 1.64 GHz); over a short one the tiles' starts and ends and the last, partial round of them (16384
-// x 4096 x 4096 of 16 experts, 4.5 rounds of 32 steps: 294 us, busy 45% at 2.1 GHz).  The smaller tiles
+// What bounds the 256 tile: over a long axis power (8192^3: 432 us, 2.5 PFLOP/s, the matrix cores busy 66% of the
+// cycles at 1.7 GHz); over a short one the tiles' ends, which write at HBM's rate (5 us a round of tiles, 7.7 through the
+// caches; a start takes 2), and the last, partial round of them (16384
+// x 4096 x 4096 of 16 experts, 4.5 rounds of 32 steps: 286 us, busy 48% at 2.0 GHz).  The smaller tiles
 // wait for each step's transfers (1000 x 1302 x 1472 fp32: 13 us for 12 steps, busy 8%, LDS reads 5%).  Measured and
 // not adopted: one workgroup a CU that walks many tiles, the next one's first steps on their way while a tile
 // leaves (grouped products 303 -> 312 us, gradients 360 -> 391: turns fixed beforehand lose what

@@ -37,8 +37,8 @@ struct LayoutArgs {
 
 // One 128 x 128 tile a workgroup: thread t has eight columns of R rows from R (t / 16) on.  R is 4 where
 // a CU has few tiles and their latency counts, else 8 (with W's tiles beside dY's and X's: 1000 x 1302 x 1472
-// fp32 11.0 us for 11.9, 16384 x 4096 x 2048 bf16 of 16 experts 120 us for 137; without them 10.1 and 80, 335
-// MB at 4.2 TB/s, LDS reads 29% of the cycles, 18% of them conflicts).
+// fp32 11.0 us for 11.9, 16384 x 4096 x 2048 bf16 of 16 experts 120 us for 137; without them, and with the
+// columns' maxima by LDS atomics, 9.4 and 78, 335 MB at 4.3 TB/s, half of them written).
 // The transpose goes through LDS in pieces of four bytes (four rows of a column);
 // piece p of column n sits at p ^ 2 (n / 8), so that both directions spread over the banks
 // and sixteen bytes stay together but for their order.
@@ -263,12 +263,12 @@ struct Cut {
 // experts): 0.6% over the fastest on average in 16 bits and 0.4% in fp32, more than 10% on 1% and 0.5% of
 // them, 18% and 15% at worst.  Each is the fastest somewhere, us (64: of both, 64/128: dX's and dW's, ...):
 //   rows x N x K of experts          64     64/128  128/64  128    128 ahead  256
-//   16384 x 4096 x 2048 of 16 bf16   971    683     854     579    747        530    (with the weights turned first)
-//   4096 x 4096 x 2048 fp32          216    182     186     153    179        -
-//   1000 x 1302 x 1472 fp32          33.6   31.6    31.4    31.4   31.2       -
-//   114 x 440 x 754 of 16 bf16       24.1   22.6    23.7    20.3   21.5       23.4
-//   2229 x 1664 x 354 bf16           27.5   32.6    30.5    33.8   30.8       45.0
-//   5668 x 133 x 1536 of 4 bf16      40.9   40.5    32.6    38.3   36.9       51.0
+//   16384 x 4096 x 2048 of 16 bf16   814    596     660     455    581        379
+//   4096 x 4096 x 2048 fp32          224    186     183     153    178        -
+//   1000 x 1302 x 1472 fp32          30.8   28.6    29.0    29.1   28.5       -
+//   114 x 440 x 754 of 16 bf16       23.3   21.9    22.9    18.9   21.0       22.4
+//   2229 x 1664 x 354 bf16           25.9   30.2    28.3    31.6   28.6       42.6
+//   5668 x 133 x 1536 of 4 bf16      37.7   37.4    29.9    35.4   34.0       48.8
 Cut cut_of(int type, int64_t rows, int64_t experts, int64_t N, int64_t K, bool dx, bool dw, int ncu) {
   constexpr int kEdge[4] = {64, 128, 256, 128};
   struct Cost {

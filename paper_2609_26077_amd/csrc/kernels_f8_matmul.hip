@@ -164,14 +164,14 @@ __global__ __launch_bounds__(64 * W) void few_tokens_kernel(Product g) {
 // than the fastest on average in 16 bits and 0.6% in fp32, more than 10% on 4% and 2% of them, 33% and
 // 21% at worst.  Each is the fastest somewhere, us:
 //   tokens x N x K                   16x16   32x32   64x64   128 ahead  128     256
-//   1 x 8192 x 8192 bf16             13.9    19.5    19.7    24.7       36.3    48.4
-//   64 x 8192 x 8192 bf16            43.6    21.7    23.9    28.5       37.9    52.0
-//   256 x 4096 x 4096 bf16           32.3    17.6    14.6    20.2       22.7    41.2
-//   1000 x 1302 x 1472 fp32          26.2    15.2    12.8    15.5       15.7    -
-//   2001 x 1030 x 1472 of 7 bf16     42.8    22.9    15.4    11.5       12.5    21.0
-//   2048 x 4096 x 4096 bf16          206     97.4    57.9    42.7       34.6    44.8
-//   16384 x 4096 x 4096 of 16 bf16   1999    903     576     427        344     290
-//   64 x 2048 x 4096 of 32 bf16      40.2    38.3    53.7    55.3       51.5    55.2
+//   1 x 8192 x 8192 bf16             14.1    19.5    19.8    25.0       36.6    48.6
+//   64 x 8192 x 8192 bf16            43.5    21.7    23.9    28.6       37.8    52.1
+//   256 x 4096 x 4096 bf16           32.4    17.7    14.5    20.4       22.9    41.6
+//   1000 x 1302 x 1472 fp32          26.3    15.1    12.7    15.6       15.9    -
+//   2001 x 1030 x 1472 of 7 bf16     43.4    23.0    15.5    11.5       12.7    21.3
+//   2048 x 4096 x 4096 bf16          208     98.0    58.4    44.1       36.0    45.2
+//   16384 x 4096 x 4096 of 16 bf16   1992    906     576     426        339     286
+//   64 x 2048 x 4096 of 32 bf16      40.9    38.7    54.2    55.7       51.4    55.0
 struct Shape {
   int tm, tn, waves;            // tile, and the waves that share its contracted axis
   bool one;                     // only where each CU has one group at most
