@@ -5,6 +5,7 @@ from __future__ import annotations
 
 import numpy as np
 import torch
+from torch.autograd.graph import increment_version
 
 from . import FMM_F32, _check, _lib, fmm_clip_scratch_size
 from .q8 import TYPES, _run
@@ -58,7 +59,8 @@ def clip(grads, max_norm, out=None, stream=None):
 
     grads: tensors of float32, bfloat16 or float16 (mixed or not) on one device.  Nothing is
     copied to the host: a norm that is not finite is for the caller to see, and gives
-    gradients of zeros (infinity) or NaN."""
+    gradients of zeros (infinity) or NaN.  What is written counts as written in place: torch's
+    version counters move, so a graph that has kept such a tensor refuses its backward pass."""
     most = float(max_norm)
     if not most >= 0.0:
         raise ValueError(f"max_norm: {max_norm}, expected a number >= 0")
@@ -84,6 +86,7 @@ def clip(grads, max_norm, out=None, stream=None):
         scratch = torch.empty(_SCRATCH, dtype=torch.uint8, device=dev)
         _check(_lib.fmm_clip(types.ctypes.data, sizes.ctypes.data, at.ctypes.data, to.ctypes.data, n, most, norm.data_ptr(),
                              scratch.data_ptr(), _SCRATCH, handle), "fmm_clip")
+        increment_version(ins if out is None else outs)      # (a graph that has kept one of them has to refuse)
         return norm
 
     return _run(dev, stream, call, *ins, *outs)
