@@ -630,7 +630,8 @@ const char *fmm_f8_linear_backward_kernel(const fmm_f8_desc *desc, int want_dx, 
  *   dNorm (fp32, one) = sqrt(sum of the squares of all elements), summed in binary64,
  *   dOut[i] = dIn[i] min(1, most / (norm + 1e-6)).
  * most >= 0.  dOut[i] may be dIn[i]; else outputs must not overlap inputs or one another.  A
- * norm of infinity gives the factor 0, NaN gives NaN everywhere.  At most 122880 tensors
+ * norm of infinity gives the factor 0, whatever most is (and NaN where the element is infinite itself), NaN gives
+ * NaN everywhere.  A finite norm past fp32's largest number is infinity in dNorm alone.  At most 122880 tensors
  * and 2^42 elements (FMM_ERR_UNSUPPORTED).  dScratch: 8-byte aligned, at least the size below
  * (FMM_ERR_WORKSPACE). */
 size_t fmm_clip_scratch_size(void);

@@ -142,7 +142,7 @@ __global__ __launch_bounds__(256) void clip_kernel(Table t, const double *partia
   for (int i = threadIdx.x; i < partials; i += 256) s += partial[i];
   s = sqrt(sum256(s, share));
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)s;
-  const double ratio = (double)most / (s + 1e-6);
+  const double ratio = s < INFINITY || isnan(s) ? (double)most / (s + 1e-6) : 0.0;   // (0 for a limit of infinity too)
   const float f = ratio > 1.0 ? 1.0f : (float)ratio;     // (NaN stays)
   for (int c = t.chunks - 1 - blockIdx.x, i = tensor_of(t, c); c >= 0; c -= gridDim.x) {
     while (c < t.first[i]) --i;

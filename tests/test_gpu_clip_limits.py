@@ -42,3 +42,17 @@ def test_autograd_sees_the_write(torch, grads):
         c = torch.randn(10, device="cuda")
     grads.clip([c], 0.0)
     assert bool((c == 0).all())
+
+
+def test_an_infinite_norm_gives_zeros(torch, grads):
+    """Whatever the limit, an infinite one too: the factor is 0 (infinity times 0 is NaN)."""
+    for most in (0.0, 1.0, float("inf")):
+        ts = [torch.ones(100, device="cuda"), torch.ones(33, device="cuda", dtype=torch.bfloat16)]
+        ts[1][5] = -float("inf")
+        norm = grads.clip(ts, most)
+        assert float(norm) == float("inf")
+        assert bool((ts[0] == 0).all()) and bool(torch.isnan(ts[1][5])) and int((ts[1] == 0).sum()) == 32
+    # a limit that nothing reaches
+    ts = [torch.full((100,), 3e38, device="cuda")]
+    grads.clip(ts, float("inf"))
+    assert bool((ts[0] == 3e38).all())
