@@ -96,8 +96,9 @@ __device__ __forceinline__ void store(elem_t<T> *p, int64_t n, const float (&v)[
   }
 }
 
+// times c, or, where c is below fp32's normal numbers and would lose digits as one, times `ratio`
 template <int T>
-__device__ __forceinline__ void scale(const void *in, void *out, int64_t n, float c) {
+__device__ __forceinline__ void scale(const void *in, void *out, int64_t n, float c, double ratio) {
   const Part<T> x(in, n);
   elem_t<T> *q = static_cast<elem_t<T> *>(out) + 8 * threadIdx.x;
   const bool stream = reinterpret_cast<uintptr_t>(out) % 16 == 0;
@@ -106,7 +107,7 @@ __device__ __forceinline__ void scale(const void *in, void *out, int64_t n, floa
     float v[8];
     q8::floats8<T>(x.raw[u], v);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] *= c;
+    for (int k = 0; k < 8; ++k) v[k] = ratio < 0x1p-126 ? (float)(v[k] * ratio) : v[k] * c;
     store<T>(q + 2048 * u, n - 8 * (int)threadIdx.x - 2048 * u, v, stream);
   }
 }
@@ -152,9 +153,9 @@ __global__ __launch_bounds__(256) void clip_kernel(Table t, const double *partia
     const int64_t bytes = at * (type == FMM_F32 ? 4 : 2);
     const uint8_t *p = static_cast<const uint8_t *>(t.in[i]) + bytes;
     uint8_t *q = static_cast<uint8_t *>(t.out[i]) + bytes;
-    if (type == FMM_F32) scale<FMM_F32>(p, q, n, f);
-    else if (type == FMM_BF16) scale<FMM_BF16>(p, q, n, f);
-    else scale<FMM_F16>(p, q, n, f);
+    if (type == FMM_F32) scale<FMM_F32>(p, q, n, f, ratio);
+    else if (type == FMM_BF16) scale<FMM_BF16>(p, q, n, f, ratio);
+    else scale<FMM_F16>(p, q, n, f, ratio);
   }
 }
 

@@ -56,3 +56,23 @@ def test_an_infinite_norm_gives_zeros(torch, grads):
     ts = [torch.full((100,), 3e38, device="cuda")]
     grads.clip(ts, float("inf"))
     assert bool((ts[0] == 3e38).all())
+
+
+@pytest.mark.parametrize("types", ["float32", "bfloat16", "mixed"])
+@pytest.mark.parametrize("scale,most", [(1e38, 1.0), (3e38, 1e-3), (1e30, 1e-12), (1e37, 1e-38), (3e38, 1e-42)])
+def test_factors_below_fp32s_normal_numbers(torch, grads, types, scale, most):
+    """The factor keeps its digits: its bar is that of any other, 2^-24 relative (in binary64 less), of the limit as fp32 holds it."""
+    dtypes = [torch.float32, torch.bfloat16] if types == "mixed" else [getattr(torch, types)]
+    g = torch.Generator().manual_seed(3)
+    ts = [(scale * (torch.rand(n, generator=g, dtype=torch.float64) * 2 - 1)).to(dtypes[i % len(dtypes)]).cuda()
+          for i, n in enumerate((3000, 1, 700))]
+    most = float(np.float32(most))
+    up = [t.double().cpu().numpy() for t in ts]
+    want = np.sqrt(sum((u ** 2).sum() for u in up))
+    c = most / (want + 1e-6)
+    assert 0 < c < 2.0 ** -126
+    out = [torch.empty_like(t) for t in ts]
+    grads.clip(ts, most, out=out)
+    for u, o in zip(up, out):
+        n = str(o.dtype).split(".")[1]
+        assert (np.abs(o.double().cpu().numpy() - u * c) <= (HALF_ULP[n] + 2.5 * 2.0 ** -24) * np.abs(u * c) + SMALLEST[n]).all()
