@@ -181,7 +181,9 @@ int fill(const Tensor *t, int count, int at, Table &b) {
 int launch_clip(const Tensor *t, int count, float most, float *norm, double *partial, void *stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
   Table b;
-  // each launch's partial sums after those before it, kClipBlocks in all
+  // Each launch's partial sums after those before it, kClipBlocks in all, so the first pass has fewer workgroups a launch
+  // the more tensors there are, and gets slower (tensors of 1 M bf16 elements, all passes by their bytes: 120 in 127 us, 6.0
+  // TB/s; 300 in 407, 4.6; 1000 in 1640, 3.9; 5000 in 21600, 1.5).
   const int each = kClipBlocks / std::max(1, (count + kTable - 1) / kTable);
   int partials = 0;
   for (int at = 0; at < count;) {

@@ -76,3 +76,22 @@ def test_factors_below_fp32s_normal_numbers(torch, grads, types, scale, most):
     for u, o in zip(up, out):
         n = str(o.dtype).split(".")[1]
         assert (np.abs(o.double().cpu().numpy() - u * c) <= (HALF_ULP[n] + 2.5 * 2.0 ** -24) * np.abs(u * c) + SMALLEST[n]).all()
+
+
+@pytest.mark.parametrize("count,size", [(1000, 1301), (5000, 77), (122880, 5)])
+def test_many_tensors(torch, grads, count, size):
+    """More than a few launches of 120 tensors, to the most that a call takes; one tensor more is refused."""
+    g = torch.Generator(device="cuda").manual_seed(count)
+    buf = torch.randn(count, size, generator=g, device="cuda") * torch.exp(torch.randn(count, 1, generator=g, device="cuda"))
+    out = torch.full_like(buf, 7.0)
+    norm = grads.clip(buf.unbind(), 0.5, out=out.unbind())
+    again = torch.empty_like(buf)
+    assert torch.equal(grads.clip(buf.unbind(), 0.5, out=again.unbind()), norm) and torch.equal(again, out)
+    x = buf.double()
+    want = float(x.square().sum().sqrt())
+    assert abs(float(norm) - want) <= 2.0 ** -23 * want
+    c = min(1.0, 0.5 / (want + 1e-6))
+    assert bool(((out.double() - c * x).abs() <= 3.5 * 2.0 ** -24 * c * x.abs()).all())
+    if count == 122880:
+        with pytest.raises(RuntimeError):
+            grads.clip([*buf.unbind(), torch.zeros(1, device="cuda")], 0.5)
