@@ -259,9 +259,10 @@ struct Cut {
 };
 
 // t = max(start + chain steps, of either; start + work of both / CUs) + tile tiles / CUs us, as for the forward
-// products.  Against all cuts on 2100 shapes (rows 16 to 16384, N to 8192, K to 4096, single weights and up to 64
-// experts): 0.6% over the fastest on average in 16 bits and 0.4% in fp32, more than 10% on 1% and 0.5% of
-// them, 18% and 15% at worst.  Each is the fastest somewhere, us (64: of both, 64/128: dX's and dW's, ...):
+// products.  Against all cuts on 2384 shapes that it was not fitted on (rows 16 to 16384, N to 8192, K to 4096, single
+// weights and up to 64 experts): 1.0% over the fastest on average in 16 bits and 0.5% in fp32, more than 10% on 3%
+// and 1.5% of them, 34% and 15% at worst (thousands of rows over a few experts).  Each is the fastest somewhere, us (64:
+// of both, 64/128: dX's and dW's, ...):
 //   rows x N x K of experts          64     64/128  128/64  128    128 ahead  256
 //   16384 x 4096 x 2048 of 16 bf16   814    596     660     455    581        379
 //   4096 x 4096 x 2048 fp32          224    186     183     153    178        -

@@ -159,10 +159,13 @@ __global__ __launch_bounds__(64 * W) void few_tokens_kernel(Product g) {
 
 // The shapes of workgroup: t = start + max(chain pieces, work pieces groups / CUs) + group groups / CUs us, pieces
 // being the 128-byte steps that a wave walks.  `chain` is a piece's time where the chip is not full, `work` where
-// it is, `group` what each group costs besides.  On 1800 shapes (1 to 16384 tokens, N and K to 8192, single weights and up
-// to 64 experts with uneven rows, which the rule takes to be even) the one that it picks is 1.1% slower
-// than the fastest on average in 16 bits and 0.6% in fp32, more than 10% on 4% and 2% of them, 33% and
-// 21% at worst.  Each is the fastest somewhere, us:
+// it is, `group` what each group costs besides: one set where several rows of tiles share a weight's tiles (through L2), one
+// where a weight's tiles come for a single row of them.  Fitted on 6187 shapes, each counting alike, and checked on 3609
+// others (1 to 16384 tokens; N and K to 8192, with 32 M weights and more to 16384; single weights and up to 256 experts with uneven
+// rows, which the rule takes to be even).  On the latter the one that it picks is, over the fastest, 1.8% slower on average in
+// 16 bits and 1.2% in fp32, more than 10% on 6% and 4% of them, 38% and 32% at worst; for few tokens over many experts 3.3%
+// and 2.4% on average.  (One set of costs for both, fitted alike: 1.8% and 1.2%, of the latter 3.6% and 2.5%, and 64 x 2048 x
+// 4096 of 32 gets the 128 tile.  Either way the shapes that the tests name keep their kernels.)  Each is the fastest somewhere, us:
 //   tokens x N x K                   16x16   32x32   64x64   128 ahead  128     256
 //   1 x 8192 x 8192 bf16             14.1    19.5    19.8    25.0       36.6    48.6
 //   64 x 8192 x 8192 bf16            43.5    21.7    23.9    28.6       37.8    52.1
@@ -176,16 +179,19 @@ struct Shape {
   int tm, tn, waves;            // tile, and the waves that share its contracted axis
   bool one;                     // only where each CU has one group at most
   struct Cost {
-    float start, chain, work, group;
+    float start;
+    struct {
+      float chain, work, group;
+    } of[2];                    // several rows of tiles for each expert, one
   } cost[2];                    // of 16-bit outputs, of fp32
 };
 constexpr Shape kShapes[] = {
-    {16, 16, 8, false, {{3.29f, 0.20f, 0.535f, 0.0f}, {3.55f, 0.41f, 0.57f, 0.0f}}},
-    {32, 32, 4, false, {{3.46f, 0.348f, 0.735f, 0.0f}, {3.63f, 0.50f, 0.831f, 0.0f}}},
-    {64, 64, 1, false, {{3.67f, 0.38f, 0.30f, 0.0f}, {3.73f, 0.557f, 0.43f, 0.0f}}},
-    {128, 128, 1, true, {{3.82f, 0.564f, 0.49f, 0.06f}, {3.77f, 0.82f, 1.33f, 0.0f}}},
-    {128, 128, 1, false, {{3.60f, 0.698f, 0.583f, 0.0f}, {3.73f, 1.20f, 0.83f, 0.0f}}},
-    {256, 256, 1, false, {{7.86f, 1.05f, 1.94f, 0.88f}, {0.0f, 0.0f, 0.0f, 0.0f}}},
+    {16, 16, 8, false, {{3.28f, {{0.665f, 0.79f, 0.0f}, {0.322f, 0.364f, 0.412f}}}, {3.56f, {{0.2f, 0.724f, 0.0f}, {0.368f, 0.61f, 0.29f}}}}},
+    {32, 32, 4, false, {{3.46f, {{0.521f, 0.745f, 0.08f}, {0.511f, 0.637f, 0.09f}}}, {3.62f, {{0.632f, 0.819f, 0.02f}, {0.765f, 0.7f, 0.18f}}}}},
+    {64, 64, 1, false, {{3.67f, {{0.376f, 0.296f, 0.0f}, {0.377f, 0.283f, 0.0f}}}, {3.73f, {{0.541f, 0.431f, 0.0f}, {0.553f, 0.789f, 0.04f}}}}},
+    {128, 128, 1, true, {{3.75f, {{0.568f, 0.636f, 0.0f}, {0.422f, 0.44f, 0.56f}}}, {3.77f, {{0.831f, 1.09f, 0.07f}, {0.806f, 1.65f, 0.02f}}}}},
+    {128, 128, 1, false, {{3.6f, {{0.672f, 0.579f, 0.0f}, {0.677f, 0.51f, 0.005f}}}, {3.6f, {{0.951f, 0.361f, 0.28f}, {1.21f, 0.815f, 0.2f}}}}},
+    {256, 256, 1, false, {{6.85f, {{1.08f, 1.73f, 1.36f}, {0.767f, 1.7f, 2.87f}}}, {0.0f, {{0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f}}}}},
 };
 constexpr int kShapeCount = sizeof(kShapes) / sizeof(kShapes[0]);
 // (a launch takes fewer than 2^32 threads, and tiles of uneven experts may be twice as many as of even ones)
@@ -202,8 +208,9 @@ int pick(int type, const Product &g, int ncu) {
     const double groups = experts * std::ceil(rows / p.tm) * ((g.N + p.tn - 1) / p.tn);
     if (groups > kMaxGroups || (p.one && groups > ncu)) continue;
     const double pieces = (g.steps + p.waves - 1) / p.waves;
-    const Shape::Cost &c = p.cost[type == FMM_F32];
-    const double t = c.start + std::max(c.chain * pieces, c.work * pieces * groups / ncu) + c.group * groups / ncu;
+    const float start = p.cost[type == FMM_F32].start;
+    const auto &c = p.cost[type == FMM_F32].of[rows <= p.tm];
+    const double t = start + std::max(c.chain * pieces, c.work * pieces * groups / ncu) + c.group * groups / ncu;
     if (t < least) {
       best = i;
       least = t;

@@ -16,7 +16,7 @@ pytestmark = pytest.mark.gpu
 PRODUCTS_OF_MANY = [
     ("few_tokens_kernel 16x16", "bf16", 64, 200, 40, 300),
     ("few_tokens_kernel 32x32", "fp32", 3000, 100, 140, 260),
-    ("matmul_kernel 64x64", "bf16", 2000, 70, 1030, 520),
+    ("matmul_kernel 64x64", "bf16", 4000, 130, 257, 300),
     ("matmul_kernel 128x128", "fp16", 9000, 130, 520, 260),
     ("matmul_kernel 128x128", "fp32", 12000, 100, 1000, 300),
     ("matmul_kernel 256x256", "bf16", 33500, 66, 1000, 900),
