@@ -453,10 +453,12 @@ __device__ __forceinline__ void gemm_tile(const Product &g, const Work &w, uint4
       }
   }
   __syncthreads();
-  // Tiles that begin together end together, and their stores wait for HBM.  Past the caches they do so less
-  // (8192 x 8192 with 1024 positions 86 -> 76 us, with 4096 228 -> 208; a start in turns gains nothing); such outputs, 33 MB or more,
-  // do not stay in a cache for whoever reads them anyway.  Not where rows begin off 16 bytes: lines written
-  // in pieces have to meet in the caches (10464 x 5899 with 357 positions 52 us, 75 past them).
+  // Tiles that begin together end together, and their stores wait for HBM.  Past the caches they do so less: over 68
+  // outputs of 12 to 500 MB 7% less time on average (8192 x 8192 with 1024 positions 85 -> 72 us; 5888 x 7136 with 640
+  // 39.6 -> 41.1).  With whoever reads the output right behind (a clamp, the quantizer) 1.4% less to 24 MB, 2.3% more from 40 to
+  // 90 MB, which the last-level cache would have kept (5888 x 7136 with 640 66 -> 72), and 2.7% less beyond.  Not where
+  // rows begin off 16 bytes: lines written in pieces have to meet in the caches (10464 x 5899 with 357 positions 52 us, 75
+  // past them).  A start in turns gains nothing.
   const bool stream = T::TM == 256 && g.N * (OUT == FMM_F32 ? 4 : 2) % 16 == 0 && reinterpret_cast<uintptr_t>(w.C) % 16 == 0;
   q8::GemmProblem out = {};
   out.M = w.M;
